@@ -76,8 +76,14 @@ typedef enum {
  *                      d2 % 16 == 0): blocks of 16 output columns x 32 inputs, each block 1 KiB laid
  *                      out lane-by-lane as the 16x16x32 matrix-core operand, blocks of one column
  *                      group consecutive along d1.  Element (j, i) of the row-major array sits at
- *                      ((j/16 * (d1/32) + i/32) * 64 + (i%32)/8 * 16 + j%16) * 8 + i%8.  */
-typedef enum { MILORA_W_ROWMAJOR = 0, MILORA_W_PACKED = 1 } milora_wlayout;
+ *                      ((j/16 * (d1/32) + i/32) * 64 + (i%32)/8 * 16 + j%16) * 8 + i%8.
+ *  MILORA_W_MX4      : 4-bit values with a scale for every 32 inputs of a column (the OCP microscaling format MXFP4;
+ *                      activations bf16, d1 % 32 == 0), as milora_quantize_weight() writes them: codes [d2][d1/2], input
+ *                      2 c of a column in the low half of its byte c, then scales [d2][d1/32], milora_quantized_weight_bytes()
+ *                      bytes in all.  A code is E2M1: bit 3 the sign, the rest 0, 0.5, 1, 1.5, 2, 3, 4 or 6; the weight is that
+ *                      times 2^(scale - 127), NaN where the scale is 255.  A power of two times four bits is a bf16 number:
+ *                      the linears compute with exactly these weights.  */
+typedef enum { MILORA_W_ROWMAJOR = 0, MILORA_W_PACKED = 1, MILORA_W_MX4 = 2 } milora_wlayout;
 
 /* Flags of milora_layer_decode. */
 #define MILORA_LAYER_RMSNORM 1u /* weightless RMS normalisation (eps 1e-5) in front of q/k/v and gate/up */
@@ -158,21 +164,25 @@ int milora_route(const void *H, int64_t M_tok, int d, int dtype, const int32_t *
  *   X           device [M][d1], `dtype`
  *   row_to_req  device [M] int32 or NULL.  NULL means row m belongs to request m and needs M == B
  *               (decode).  Prefill tokens and beams map several rows to one request.
- *   W           device, math shape d1 x d2 in `w_layout` (MILORA_W_PACKED: bf16 only)
+ *   W           device, math shape d1 x d2 in `w_layout` (MILORA_W_PACKED: bf16 only; MILORA_W_MX4: X, bias, adapters and
+ *               Y are bf16)
  *   bias        device [d2] `dtype` or NULL
  *   adapters    host struct, see milora_adapters
  *   tenant_id   device [B] int32; route: device [B] uint8 (this layer's row of the route table)
  *   Y           device [M][d2], `dtype`
- *   workspace   device, milora_routed_linear_workspace_bytes(M, d1, d2, r_max) bytes; the size never goes down when an
+ *   workspace   device, milora_routed_linear_workspace_bytes(M, d1, d2, r_max) bytes, for MILORA_W_MX4
+ *               milora_quantized_linear_workspace_bytes(M, d1, d2, r_max) (more than some hundred rows: the weight in
+ *               bf16 is part of it; what it holds before a call does not matter); the sizes never go down when an
  *               argument goes up, so one workspace sized for the largest call serves every smaller one
  * A row whose request index, tenant id or tenant rank is out of range gets the base term only.
- * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK), EUNSUPPORTED (packed layout with fp32, with
+ * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK), EUNSUPPORTED (packed or 4-bit layout with fp32, with
  * d1 % 32 != 0 or d2 % 16 != 0, or with X, W, bias or Y not 16-byte aligned), EWORKSPACE, EHIP.
  */
+size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max);
 size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max);
 /* Which family of calls these sizes belong to when the pointers are 16-byte aligned (host logic only, no device work):
- * MILORA_KERNEL_STREAM (packed weights), MILORA_KERNEL_TILES (row-major bf16 weights, M >= 64, d1 % 64 == 0, d2 % 16 == 0) or
- * MILORA_KERNEL_GENERIC (everything else).  Which kernel runs, by the same rules the call itself follows, is
+ * MILORA_KERNEL_STREAM (packed weights, 4-bit ones of up to some hundred rows), MILORA_KERNEL_TILES (row-major bf16 weights,
+ * M >= 64, d1 % 64 == 0, d2 % 16 == 0; 4-bit ones of more rows) or MILORA_KERNEL_GENERIC (everything else).  Which kernel runs, by the same rules the call itself follows, is
  * milora_routed_linear_tile's answer: the side of the matrix-core tiles (64, 128 or 256), or 0 where there are none (the
  * weight-streaming kernel: packed, up to 32 rows; the any-shape kernels: fp32 and widths the others do not take).  Packed
  * weights above 32 rows and row-major bf16 ones below 64 run on tiles of 64 or 128.  Both: negative status for arguments
@@ -210,8 +220,10 @@ int milora_routed_linear(const void *X, int64_t M, int d1, int d2, int dtype,
  *   workspace device, milora_layer_decode_workspace_bytes(B, d, F, r_max) bytes (packed weights and B > 32:
  *             this includes the tables of fp32 partial tiles of the wide-batch kernel, tens of MB)
  * Errors: EINVAL, ERANGE (B > MILORA_MAX_DECODE_BATCH, r_max > MILORA_MAX_RANK), EUNSUPPORTED
- * (packed layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
+ * (packed or 4-bit layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
  * weight not 16-byte aligned), EWORKSPACE, EHIP.
+ * MILORA_W_MX4: eight launches (ten with normalisation); the outputs of o, gate, up and down stay in fp32 up to the glue's
+ * rounding.  No wait inside a launch, and what the workspace holds before a call does not matter.
  */
 size_t milora_layer_decode_workspace_bytes(int B, int d, int F, int r_max);
 int milora_layer_decode(const void *x, int B, int d, int F, int dtype,
@@ -313,6 +325,21 @@ int milora_layer_decode_trace(const void *x, int B, int d, int F, int dtype,
  * elements each, must not overlap.  Errors: EINVAL, EUNSUPPORTED (d1 % 32 or d2 % 16 nonzero), EHIP.
  */
 int milora_pack_weight(const void *src_rowmajor, void *dst_packed, int d1, int d2, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * milora_quantize_weight - a base weight to MILORA_W_MX4 (see milora_wlayout), once, when it is loaded.  The scale of a
+ * group of 32 inputs is the power of two that puts its largest magnitude between 4 and 8, kept within 2^-125 .. 2^125; values
+ * are rounded to the nearest code, ties to the even one, magnitudes above 6 scales to 6.  A group that holds Inf or NaN
+ * becomes NaN as a whole.  Weights that already are 4-bit values with a power-of-two scale for 32 inputs in that range keep their values.
+ *   src_rowmajor  device [d2][d1] `dtype` (bf16 or fp32), at any alignment of its type
+ *   dst           device, milora_quantized_weight_bytes(d1, d2) bytes (0 where d1 % 32 != 0), 16-byte aligned; must not overlap src
+ * milora_dequantize_weight - the values the codes stand for, exactly, to device [d2][d1] `dtype`.  Any scale byte is
+ * taken (bf16 and fp32 results beyond their range are Inf).
+ * Errors: EINVAL, EUNSUPPORTED (d1 % 32 != 0, codes not 16-byte aligned), EHIP.
+ */
+size_t milora_quantized_weight_bytes(int d1, int d2);
+int milora_quantize_weight(const void *src_rowmajor, int dtype, void *dst, int d1, int d2, void *stream);
+int milora_dequantize_weight(const void *src, void *dst_rowmajor, int dtype, int d1, int d2, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Measurement helpers (not part of the method; for callers that report a kernel's rate against what the

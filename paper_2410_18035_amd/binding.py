@@ -21,7 +21,7 @@ NUM_SITES = 7
 BF16, F32 = 0, 1
 POOL = {"mean": 0, "last": 1, "max": 2, "selfattn": 3}
 ACT = {"identity": 0, "tanh": 1, "relu": 2, "gelu": 3, "rational": 4}
-W_ROWMAJOR, W_PACKED = 0, 1
+W_ROWMAJOR, W_PACKED, W_MX4 = 0, 1, 2
 LAYER_RMSNORM = 1
 ROUTE_NONE = 255
 ROUTE_SET = 0x80
@@ -31,10 +31,11 @@ MAX_DECODE_BATCH = 128
 EXPORTS = (
     "milora_version", "milora_status_string", "milora_last_hip_error",
     "milora_route_workspace_bytes", "milora_route",
-    "milora_routed_linear_workspace_bytes", "milora_routed_linear_kernel", "milora_routed_linear_tile", "milora_routed_linear",
+    "milora_routed_linear_workspace_bytes", "milora_quantized_linear_workspace_bytes", "milora_routed_linear_kernel", "milora_routed_linear_tile", "milora_routed_linear",
     "milora_layer_decode_workspace_bytes", "milora_layer_decode", "milora_layer_decode_noalloc",
     "milora_layer_decode_profile", "milora_layer_decode_trace_bytes", "milora_layer_decode_trace",
-    "milora_pack_weight", "milora_packed_workspace_status", "milora_set_wait_limit",
+    "milora_pack_weight", "milora_quantized_weight_bytes", "milora_quantize_weight", "milora_dequantize_weight",
+    "milora_packed_workspace_status", "milora_set_wait_limit",
     "milora_measure_workspace_bytes", "milora_measure_matrix_rate", "milora_measure_read_rate",
 )
 
@@ -77,6 +78,8 @@ def lib() -> ctypes.CDLL:
                                    i32, vp, vp, vp, sz, vp]
         L.milora_routed_linear_workspace_bytes.restype = sz
         L.milora_routed_linear_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        L.milora_quantized_linear_workspace_bytes.restype = sz
+        L.milora_quantized_linear_workspace_bytes.argtypes = [i64, i32, i32, i32]
         L.milora_routed_linear_kernel.restype = i32
         L.milora_routed_linear_kernel.argtypes = [i64, i32, i32, i32, i32]
         L.milora_routed_linear_tile.restype = i32
@@ -99,6 +102,12 @@ def lib() -> ctypes.CDLL:
         L.milora_layer_decode_trace.argtypes = L.milora_layer_decode.argtypes + [vp, sz, ctypes.POINTER(ctypes.c_int32)]
         L.milora_pack_weight.restype = i32
         L.milora_pack_weight.argtypes = [vp, vp, i32, i32, vp]
+        L.milora_quantized_weight_bytes.restype = sz
+        L.milora_quantized_weight_bytes.argtypes = [i32, i32]
+        L.milora_quantize_weight.restype = i32
+        L.milora_quantize_weight.argtypes = [vp, i32, vp, i32, i32, vp]
+        L.milora_dequantize_weight.restype = i32
+        L.milora_dequantize_weight.argtypes = [vp, vp, i32, i32, i32, vp]
         L.milora_packed_workspace_status.restype = i32
         L.milora_packed_workspace_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int), vp]
         L.milora_set_wait_limit.restype = i32
@@ -231,6 +240,11 @@ def routed_linear_workspace_bytes(M: int, d1: int, d2: int, r_max: int) -> int:
     return int(lib().milora_routed_linear_workspace_bytes(M, d1, d2, r_max))
 
 
+def quantized_linear_workspace_bytes(M: int, d1: int, d2: int, r_max: int) -> int:
+    """Workspace of milora_routed_linear on W_MX4 weights."""
+    return int(lib().milora_quantized_linear_workspace_bytes(M, d1, d2, r_max))
+
+
 KERNEL_GENERIC, KERNEL_STREAM, KERNEL_TILES = 0, 1, 2
 
 
@@ -245,26 +259,39 @@ def milora_routed_linear_tile(M: int, d1: int, d2: int, dtype: torch.dtype, w_la
     return int(lib().milora_routed_linear_tile(M, d1, d2, code, w_layout))
 
 
+def _check_weight(W: torch.Tensor, d1: int, d2: int, w_layout: int, dtype: torch.dtype) -> None:
+    """Shape and type of a base weight of d1 inputs and d2 columns in a layout."""
+    if w_layout == W_MX4:
+        if W.dtype != torch.uint8 or W.numel() != quantized_weight_bytes(d1, d2) or W.numel() == 0:
+            raise ValueError("a quantised W holds quantized_weight_bytes(d1, d2) bytes")
+        return
+    if w_layout == W_ROWMAJOR:
+        if W.shape != (d2, d1):
+            raise ValueError("W must be [d2, d1]")
+    elif W.numel() != d1 * d2:
+        raise ValueError("a packed W needs d2 and d1*d2 elements")
+    if W.dtype != dtype:
+        raise TypeError("W and X must share a dtype")
+
+
 def milora_routed_linear(X: torch.Tensor, W: torch.Tensor, adapters: AdapterTable, site: int,
                          tenant_id: torch.Tensor, route: torch.Tensor, row_to_req: Optional[torch.Tensor] = None,
                          bias: Optional[torch.Tensor] = None, w_layout: int = W_ROWMAJOR,
                          d2: Optional[int] = None, out: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Y = X W + bias + [route == site] (X A) B.  W is [d2, d1] row-major, or packed (then pass d2)."""
+    """Y = X W + bias + [route == site] (X A) B.  W is [d2, d1] row-major, or packed or quantised (then pass d2)."""
     M, d1 = X.shape
     if w_layout == W_ROWMAJOR:
         d2 = W.shape[0]
-        if W.shape != (d2, d1):
-            raise ValueError("W must be [d2, d1]")
-    elif d2 is None or W.numel() != d1 * d2:
-        raise ValueError("a packed W needs d2 and d1*d2 elements")
-    if W.dtype != X.dtype:
-        raise TypeError("W and X must share a dtype")
+    elif d2 is None:
+        raise ValueError("a packed or quantised W needs d2")
+    _check_weight(W, d1, d2, w_layout, X.dtype)
     B = tenant_id.numel()
     if out is None:
         out = torch.empty(M, d2, dtype=X.dtype, device=X.device)
     if workspace is None:
-        workspace = _workspace(routed_linear_workspace_bytes(M, d1, d2, adapters.r_max), X.device)
+        need = quantized_linear_workspace_bytes if w_layout == W_MX4 else routed_linear_workspace_bytes
+        workspace = _workspace(need(M, d1, d2, adapters.r_max), X.device)
     ad = adapters.c_struct()
     rc = lib().milora_routed_linear(_dev(X), M, d1, d2, _dtype_code(X), _dev(row_to_req, torch.int32), _dev(W),
                                     w_layout, _dev(bias, X.dtype), ctypes.byref(ad), site,
@@ -295,7 +322,9 @@ def milora_layer_decode(x: torch.Tensor, weights: Sequence[torch.Tensor], adapte
         raise ValueError("seven base weights expected")
     lw = _LayerWeights()
     for m, w in enumerate(weights):
-        if w.dtype != x.dtype:
+        if w_layout == W_MX4:
+            _check_weight(w, F if m == 6 else d, F if m in (4, 5) else d, w_layout, x.dtype)
+        elif w.dtype != x.dtype:
             raise TypeError("weights and x must share a dtype")
         lw.W[m] = _dev(w)
     lw.layout = w_layout
@@ -373,6 +402,40 @@ def milora_pack_weight(W: torch.Tensor) -> torch.Tensor:
     rc = lib().milora_pack_weight(_dev(W, torch.bfloat16), _dev(out), d1, d2, _stream())
     if rc != 0:
         raise MiloraError(rc, "milora_pack_weight")
+    return out
+
+
+def quantized_weight_bytes(d1: int, d2: int) -> int:
+    """Bytes of a W_MX4 weight of d1 inputs and d2 columns (0 where d1 is no multiple of 32)."""
+    return int(lib().milora_quantized_weight_bytes(d1, d2))
+
+
+def milora_quantize_weight(W: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A row-major [d2, d1] weight (bf16 or fp32) to 4-bit values with a power-of-two scale for every 32 inputs: uint8
+    codes [d2, d1/2], then scales [d2, d1/32]."""
+    d2, d1 = W.shape
+    nbytes = quantized_weight_bytes(d1, d2)
+    if out is None:
+        out = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+    elif out.dtype != torch.uint8 or out.numel() != nbytes:
+        raise ValueError("out holds quantized_weight_bytes(d1, d2) bytes")
+    rc = lib().milora_quantize_weight(_dev(W), _dtype_code(W), _dev(out), d1, d2, _stream())
+    if rc != 0:
+        raise MiloraError(rc, "milora_quantize_weight")
+    return out
+
+
+def milora_dequantize_weight(Wq: torch.Tensor, d1: int, d2: int, dtype: torch.dtype = torch.bfloat16,
+                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values a quantised weight stands for, [d2, d1] row-major."""
+    _check_weight(Wq, d1, d2, W_MX4, dtype)
+    if out is None:
+        out = torch.empty(d2, d1, dtype=dtype, device=Wq.device)
+    elif out.shape != (d2, d1):
+        raise ValueError("out must be [d2, d1]")
+    rc = lib().milora_dequantize_weight(_dev(Wq), _dev(out), _dtype_code(out), d1, d2, _stream())
+    if rc != 0:
+        raise MiloraError(rc, "milora_dequantize_weight")
     return out
 
 

@@ -1,6 +1,7 @@
 // C ABI of the routed-LoRA library: argument validation, workspace carving and dispatch between
 // the decode kernels (bf16, packed weights), the matrix-core tiles (bf16, row-major weights or packed ones
 // of many rows) and the any-shape path (fp32 and everything else).
+#include "mx4.h"
 #include "tiles.h"
 
 namespace milora {
@@ -30,6 +31,8 @@ bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, 
 int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site,
                         const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear,
                         hipStream_t stream);
+int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
+                        const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream);
 int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const bf16_t* W,
                           const bf16_t* bias, const AdapterView& ad, int site, const int32_t* tenant_id,
                           const uint8_t* route, int B, const float* t, bf16_t* Y, hipStream_t st);
@@ -230,7 +233,82 @@ int layer_decode_generic(const void* x, int B, int d, int F, int dtype, const mi
   return check_launch();
 }
 
+// ---- a decode step on 4-bit weights: the linears of a level in one launch, the glue in their stores ----
+struct MxLayerWs {
+  float* h;      // [B][d]
+  bf16_t* xn;    // [B][d]
+  bf16_t* qkv;   // [B][3 d]
+  bf16_t* hn;    // [B][d]
+  bf16_t* mm;    // [B][F]
+  char* shrink;  // of up to three sites
+  size_t bytes;
+};
+
+size_t mx4_few_workspace(int64_t M, int d1, int r_max, int sites);
+int mx4_shrink(MxArgs* g, const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, int sites, const int32_t* tenant_id,
+               const uint8_t* route, int B, void* workspace, hipStream_t st);
+int mx4_few(MxArgs g, int64_t M, int sites, bool gated, hipStream_t st);
+
+MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
+  size_t off = 0;
+  auto take = [&](size_t n) { size_t o = off; off += align_up(n, 256); return o; };
+  char* b = (char*)base;
+  MxLayerWs w;
+  w.h = (float*)(b + take((size_t)B * d * 4));
+  w.xn = (bf16_t*)(b + take((size_t)B * d * 2));
+  w.qkv = (bf16_t*)(b + take((size_t)B * d * 6));
+  w.hn = (bf16_t*)(b + take((size_t)B * d * 2));
+  w.mm = (bf16_t*)(b + take((size_t)B * F * 2));
+  w.shrink = b + take(mx4_few_workspace(B, d > F ? d : F, r_max, 3));
+  w.bytes = off;
+  return w;
+}
+
+int layer_decode_mx4(const bf16_t* x, int B, int d, int F, const milora_layer_weights* wts, const AdapterView& ad, const int32_t* tenant_id,
+                     const uint8_t* route, uint32_t flags, const bf16_t* attn_out, bf16_t* y, bf16_t* qkv_out, void* workspace, hipStream_t st) {
+  const MxLayerWs w = carve_mx4(workspace, B, d, F, ad.r_max);
+  const bool norm = (flags & MILORA_LAYER_RMSNORM) != 0;
+  int rc = MILORA_OK;
+  MxArgs g{};
+  // level of `sites` linears from site0 on
+  auto level = [&](int site0, int sites, const bf16_t* in, int64_t ldx, bool gated, int64_t ldy) {
+    if (rc) return;
+    int d1, d2;
+    site_dims(site0, d, F, &d1, &d2);
+    g.X = in; g.ldx = ldx; g.d1 = d1; g.d2 = d2; g.ldy = ldy; g.ad = ad;
+    for (int s = 0; s < sites; ++s) { g.site[s] = site0 + s; g.W[s] = (const unsigned char*)wts->W[site0 + s]; }
+    rc = mx4_shrink(&g, in, ldx, B, d1, nullptr, sites, tenant_id, route, B, w.shrink, st);
+    if (!rc) rc = mx4_few(g, B, sites, gated, st);
+  };
+  if (norm) {
+    hipLaunchKernelGGL((rmsnorm_rows_kernel<bf16_t, bf16_t>), dim3(B), dim3(kThreads), 0, st, x, d, w.xn);
+    if ((rc = check_launch())) return rc;
+  }
+  bf16_t* const qkv = qkv_out ? qkv_out : w.qkv;
+  for (int s = 0; s < 3; ++s) g.Y[s] = qkv + (size_t)s * d;
+  level(0, 3, norm ? w.xn : x, d, false, 3 * (int64_t)d);
+  g.Y[1] = g.Y[2] = nullptr;
+  g.Y[0] = norm ? nullptr : w.hn;
+  g.res = x;
+  g.h_out = w.h;
+  if (attn_out) level(3, 1, attn_out, d, false, d);
+  else level(3, 1, qkv + 2 * (size_t)d, 3 * (int64_t)d, false, d);
+  g.res = nullptr;
+  if (rc) return rc;
+  if (norm) {
+    hipLaunchKernelGGL((rmsnorm_rows_kernel<float, bf16_t>), dim3(B), dim3(kThreads), 0, st, w.h, d, w.hn);
+    if ((rc = check_launch())) return rc;
+  }
+  g.Y[0] = w.mm;
+  level(4, 2, w.hn, d, true, F);
+  g.Y[0] = y;
+  g.h_in = w.h;
+  level(6, 1, w.mm, F, false, d);
+  return rc;
+}
+
 bool valid_dtype(int dt) { return dt == MILORA_BF16 || dt == MILORA_F32; }
+bool valid_layout(int l) { return l == MILORA_W_ROWMAJOR || l == MILORA_W_PACKED || l == MILORA_W_MX4; }
 
 int check_adapters(const milora_adapters* a) {
   if (!a || !a->rank || !a->A || !a->B) return MILORA_EINVAL;
@@ -266,81 +344,11 @@ LinearPlan plan_linear(int64_t M, int d1, int d2, int dtype, bool packed, const 
 bool packed_shape_ok(int d1, int d2) { return d1 % 32 == 0 && d2 % 16 == 0; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-}  // namespace
-}  // namespace milora
-
-using namespace milora;
-
-extern "C" const char* milora_version(void) { return "milora-mi355x 0.1 (gfx950)"; }
-
-extern "C" const char* milora_status_string(int status) {
-  switch (status) {
-    case MILORA_OK: return "ok";
-    case MILORA_EINVAL: return "invalid argument";
-    case MILORA_ERANGE: return "size beyond a documented limit";
-    case MILORA_EUNSUPPORTED: return "combination not supported";
-    case MILORA_EHIP: return "HIP call failed";
-    case MILORA_EWORKSPACE: return "workspace missing or too small";
-    default: return "unknown status";
-  }
-}
-
-extern "C" int milora_last_hip_error(void) { return g_last_hip_error; }
-
-extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
-  if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
-  // Control words, LoRA shrinks, the rows' look-ups, partial tiles.  What a call needs of shrinks and tiles goes up and down with M (fewer rows are cut
-  // into more parts); a caller sizes once for the largest call, so each is bounded by something that no size lowers.
-  const size_t t_bytes = align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256);
-  const size_t tiles = kStreamCtrlBytes + t_bytes + align_up((size_t)M * sizeof(int2), 256) + partial_bytes_bound(M, d1, d2);
-  const size_t packed = routed_linear_packed_workspace_bytes(M <= kStreamRows ? (int)M : kStreamRows, d1, d2, r_max);
-  return tiles > packed ? tiles : packed;
-}
-
-extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype, int w_layout) {
-  if (M < 1 || d1 < 1 || d2 < 1 || !valid_dtype(dtype)) return MILORA_EINVAL;
-  if (w_layout != MILORA_W_ROWMAJOR && w_layout != MILORA_W_PACKED) return MILORA_EINVAL;
-  if (w_layout == MILORA_W_PACKED) {
-    if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2)) return MILORA_EUNSUPPORTED;
-    return MILORA_KERNEL_STREAM;
-  }
-  const void* aligned = (const void*)(uintptr_t)256;
-  if (dtype == MILORA_BF16 && prefill_supported(M, d1, d2, aligned, aligned, aligned)) return MILORA_KERNEL_TILES;
-  return MILORA_KERNEL_GENERIC;
-}
-
-extern "C" int milora_routed_linear_tile(int64_t M, int d1, int d2, int dtype, int w_layout) {
-  const int kernel = milora_routed_linear_kernel(M, d1, d2, dtype, w_layout);
-  if (kernel < 0) return kernel;
-  const void* aligned = (const void*)(uintptr_t)256;
-  const LinearPlan p = plan_linear(M, d1, d2, dtype, w_layout == MILORA_W_PACKED, aligned, aligned, aligned);
-  if (p.kind != MILORA_KERNEL_TILES) return 0;
-  return p.tiles.shape == kTiles256 ? 256 : p.tiles.shape == kTiles128 ? 128 : 64;
-}
-
-extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req,
-                                    const void* W, int w_layout, const void* bias, const milora_adapters* adapters,
-                                    int site, const int32_t* tenant_id, const uint8_t* route, int B, void* Y,
-                                    void* workspace, size_t workspace_bytes, void* stream) {
-  if (!X || !W || !Y || !tenant_id || !route) return MILORA_EINVAL;
-  if (M < 1 || d1 < 1 || d2 < 1 || B < 1) return MILORA_EINVAL;
-  if (!valid_dtype(dtype) || site < 0 || site >= MILORA_NUM_SITES) return MILORA_EINVAL;
-  if (w_layout != MILORA_W_ROWMAJOR && w_layout != MILORA_W_PACKED) return MILORA_EINVAL;
-  if (!row_to_req && M != B) return MILORA_EINVAL;
-  int rc = check_adapters(adapters);
-  if (rc) return rc;
-  if (M > 0x7fffffffLL) return MILORA_ERANGE;
-  if (!workspace || workspace_bytes < milora_routed_linear_workspace_bytes(M, d1, d2, adapters->r_max))
-    return MILORA_EWORKSPACE;
-  hipStream_t st = (hipStream_t)stream;
-  const AdapterView ad = view_of(adapters);
-  const bool packed = w_layout == MILORA_W_PACKED;
-  if (packed) {
-    if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2) || !aligned16(X) || !aligned16(W) || !aligned16(Y) ||
-        (bias && !aligned16(bias)))
-      return MILORA_EUNSUPPORTED;
-    if (!row_to_req && M > MILORA_MAX_DECODE_BATCH) return MILORA_ERANGE;
-  }
+// A call whose arguments have been accepted.
+int run_linear(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req, const void* W, bool packed,
+               const void* bias, const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, void* Y,
+               void* workspace, hipStream_t st) {
+  int rc = MILORA_OK;
   const LinearPlan pl = plan_linear(M, d1, d2, dtype, packed, X, W, Y);
   if (pl.kind == MILORA_KERNEL_STREAM)
     // (more rows on reductions too long for the tiles: rows are independent, slices of them each read W again)
@@ -383,6 +391,162 @@ extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, in
   return launch_linear_generic(X, M, d1, d2, dtype, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, st);
 }
 
+// ---- 4-bit weights ----
+// Up to kMxFewRows rows the few-row kernel reads the codes again for every kMxRows rows (from the L2 and the cache behind it);
+// beyond, the weight is written out in bf16 once per call, row-major or, where the row-major tiles do not take its reduction, packed.
+constexpr int64_t kMxFewRows = 128;
+
+size_t mx4_few_workspace(int64_t M, int d1, int r_max, int sites) {
+  return align_up(shrink_rows_bound(M, d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256);
+}
+
+// Shrinks of the rows at `sites` consecutive sites from g.site[0] on, into the workspace, and what the few-row kernel reads of them.
+int mx4_shrink(MxArgs* g, const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, int sites, const int32_t* tenant_id,
+               const uint8_t* route, int B, void* workspace, hipStream_t st) {
+  const int parts = shrink_parts(M, d1);
+  float* const t = (float*)workspace;
+  int2* const lora = (int2*)((char*)t + align_up((size_t)M * g->ad.r_max * parts * sites * sizeof(float), 256));
+  g->t = t;
+  g->t_part = (size_t)M * g->ad.r_max;
+  g->t_site = g->t_part * parts;
+  g->parts = parts;
+  g->row_lora = lora;
+  g->lora_site = (size_t)M;
+  return launch_shrink_sites(X, ldx, M, d1, row_to_req, g->ad, g->site[0], sites, tenant_id, route, B, t, lora, nullptr, st);
+}
+
+// The rows of a call in slices of what a launch takes.
+int mx4_few(MxArgs g, int64_t M, int sites, bool gated, hipStream_t st) {
+  for (int64_t m0 = 0; m0 < M; m0 += kMxRows) {
+    MxArgs s = g;
+    s.M = (int)(M - m0 < kMxRows ? M - m0 : kMxRows);
+    s.X += m0 * g.ldx;
+    for (int i = 0; i < 3; ++i)
+      if (s.Y[i]) s.Y[i] += m0 * g.ldy;
+    if (s.gate_out) s.gate_out += m0 * g.d2;
+    if (s.up_out) s.up_out += m0 * g.d2;
+    if (s.res) { s.res += m0 * g.d2; s.h_out += m0 * g.d2; }
+    if (s.h_in) s.h_in += m0 * g.d2;
+    s.t += m0 * g.ad.r_max;
+    s.row_lora += m0;
+    const int rc = launch_mx4_rows(s, sites, gated, st);
+    if (rc) return rc;
+  }
+  return MILORA_OK;
+}
+
+bool mx4_rowmajor(int d1) { return d1 % 64 == 0; }  // the layout a weight is written out in
+
+int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const bf16_t* bias,
+                   const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, bf16_t* Y, void* workspace,
+                   hipStream_t st) {
+  if (M <= kMxFewRows) {
+    MxArgs g{};
+    g.X = X; g.ldx = d1; g.d1 = d1; g.d2 = d2; g.W[0] = (const unsigned char*)W; g.bias = bias; g.Y[0] = Y; g.ldy = d2; g.ad = ad; g.site[0] = site;
+    const int rc = mx4_shrink(&g, X, d1, M, d1, row_to_req, 1, tenant_id, route, B, workspace, st);
+    return rc ? rc : mx4_few(g, M, 1, false, st);
+  }
+  const bool packed = !mx4_rowmajor(d1);
+  const int rc = mx4_dequantize(W, workspace, MILORA_BF16, d1, d2, packed, st);
+  if (rc) return rc;
+  return run_linear(X, M, d1, d2, MILORA_BF16, row_to_req, workspace, packed, bias, ad, site, tenant_id, route, B, Y,
+                    (char*)workspace + align_up((size_t)d1 * d2 * 2, 256), st);
+}
+
+}  // namespace
+}  // namespace milora
+
+using namespace milora;
+
+extern "C" const char* milora_version(void) { return "milora-mi355x 0.1 (gfx950)"; }
+
+extern "C" const char* milora_status_string(int status) {
+  switch (status) {
+    case MILORA_OK: return "ok";
+    case MILORA_EINVAL: return "invalid argument";
+    case MILORA_ERANGE: return "size beyond a documented limit";
+    case MILORA_EUNSUPPORTED: return "combination not supported";
+    case MILORA_EHIP: return "HIP call failed";
+    case MILORA_EWORKSPACE: return "workspace missing or too small";
+    default: return "unknown status";
+  }
+}
+
+extern "C" int milora_last_hip_error(void) { return g_last_hip_error; }
+
+extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
+  if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
+  // Control words, LoRA shrinks, the rows' look-ups, partial tiles.  What a call needs of shrinks and tiles goes up and down with M (fewer rows are cut
+  // into more parts); a caller sizes once for the largest call, so each is bounded by something that no size lowers.
+  const size_t t_bytes = align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256);
+  const size_t tiles = kStreamCtrlBytes + t_bytes + align_up((size_t)M * sizeof(int2), 256) + partial_bytes_bound(M, d1, d2);
+  const size_t packed = routed_linear_packed_workspace_bytes(M <= kStreamRows ? (int)M : kStreamRows, d1, d2, r_max);
+  return tiles > packed ? tiles : packed;
+}
+
+extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
+  if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
+  const size_t few = mx4_few_workspace(M < kMxFewRows ? M : kMxFewRows, d1, r_max, 1);
+  if (M <= kMxFewRows) return few;
+  const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
+  return many > few ? many : few;
+}
+
+extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype, int w_layout) {
+  if (M < 1 || d1 < 1 || d2 < 1 || !valid_dtype(dtype)) return MILORA_EINVAL;
+  if (!valid_layout(w_layout)) return MILORA_EINVAL;
+  if (w_layout != MILORA_W_ROWMAJOR) {
+    if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2)) return MILORA_EUNSUPPORTED;
+    if (w_layout == MILORA_W_PACKED || M <= kMxFewRows) return MILORA_KERNEL_STREAM;
+    return MILORA_KERNEL_TILES;
+  }
+  const void* aligned = (const void*)(uintptr_t)256;
+  if (dtype == MILORA_BF16 && prefill_supported(M, d1, d2, aligned, aligned, aligned)) return MILORA_KERNEL_TILES;
+  return MILORA_KERNEL_GENERIC;
+}
+
+extern "C" int milora_routed_linear_tile(int64_t M, int d1, int d2, int dtype, int w_layout) {
+  const int kernel = milora_routed_linear_kernel(M, d1, d2, dtype, w_layout);
+  if (kernel < 0) return kernel;
+  const void* aligned = (const void*)(uintptr_t)256;
+  if (w_layout == MILORA_W_MX4 && kernel == MILORA_KERNEL_STREAM) return 0;
+  const bool packed = w_layout == MILORA_W_PACKED || (w_layout == MILORA_W_MX4 && !mx4_rowmajor(d1));
+  const LinearPlan p = plan_linear(M, d1, d2, dtype, packed, aligned, aligned, aligned);
+  if (p.kind != MILORA_KERNEL_TILES) return 0;
+  return p.tiles.shape == kTiles256 ? 256 : p.tiles.shape == kTiles128 ? 128 : 64;
+}
+
+extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req,
+                                    const void* W, int w_layout, const void* bias, const milora_adapters* adapters,
+                                    int site, const int32_t* tenant_id, const uint8_t* route, int B, void* Y,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  if (!X || !W || !Y || !tenant_id || !route) return MILORA_EINVAL;
+  if (M < 1 || d1 < 1 || d2 < 1 || B < 1) return MILORA_EINVAL;
+  if (!valid_dtype(dtype) || site < 0 || site >= MILORA_NUM_SITES) return MILORA_EINVAL;
+  if (!valid_layout(w_layout)) return MILORA_EINVAL;
+  if (!row_to_req && M != B) return MILORA_EINVAL;
+  int rc = check_adapters(adapters);
+  if (rc) return rc;
+  if (M > 0x7fffffffLL) return MILORA_ERANGE;
+  const bool mx4 = w_layout == MILORA_W_MX4;
+  if (!workspace || workspace_bytes < (mx4 ? milora_quantized_linear_workspace_bytes(M, d1, d2, adapters->r_max)
+                                           : milora_routed_linear_workspace_bytes(M, d1, d2, adapters->r_max)))
+    return MILORA_EWORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  const AdapterView ad = view_of(adapters);
+  const bool packed = w_layout == MILORA_W_PACKED;
+  if (packed || mx4) {
+    if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2) || !aligned16(X) || !aligned16(W) || !aligned16(Y) ||
+        (bias && !aligned16(bias)))
+      return MILORA_EUNSUPPORTED;
+    if (packed && !row_to_req && M > MILORA_MAX_DECODE_BATCH) return MILORA_ERANGE;
+  }
+  if (mx4)
+    return run_linear_mx4((const bf16_t*)X, M, d1, d2, row_to_req, W, (const bf16_t*)bias, ad, site, tenant_id, route, B, (bf16_t*)Y,
+                          workspace, st);
+  return run_linear(X, M, d1, d2, dtype, row_to_req, W, packed, bias, ad, site, tenant_id, route, B, Y, workspace, st);
+}
+
 extern "C" int milora_packed_workspace_status(const void* workspace, int* status, void* stream) {
   if (!status) return MILORA_EINVAL;
   if (!workspace) return static_scratch_status(status, (hipStream_t)stream);
@@ -395,7 +559,9 @@ extern "C" size_t milora_layer_decode_workspace_bytes(int B, int d, int F, int r
   if (B < 1 || d < 1 || F < 1 || r_max < 1 || B > MILORA_MAX_DECODE_BATCH) return 0;
   size_t a = carve_generic(nullptr, B, d, F, r_max, 4).bytes;
   size_t b = decode_packed_workspace_bytes(B, d, F, r_max);
-  return a > b ? a : b;
+  const size_t c = carve_mx4(nullptr, B, d, F, r_max).bytes;
+  a = a > b ? a : b;
+  return a > c ? a : c;
 }
 
 static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, const milora_layer_weights* weights,
@@ -407,7 +573,7 @@ static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, cons
   if (flags & ~MILORA_LAYER_RMSNORM) return MILORA_EINVAL;
   for (int m = 0; m < MILORA_NUM_SITES; ++m)
     if (!weights->W[m]) return MILORA_EINVAL;
-  if (weights->layout != MILORA_W_ROWMAJOR && weights->layout != MILORA_W_PACKED) return MILORA_EINVAL;
+  if (!valid_layout(weights->layout)) return MILORA_EINVAL;
   int rc = check_adapters(adapters);
   if (rc) return rc;
   if (B > MILORA_MAX_DECODE_BATCH) return MILORA_ERANGE;
@@ -415,12 +581,17 @@ static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, cons
     return MILORA_EWORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   const AdapterView ad = view_of(adapters);
-  if (weights->layout == MILORA_W_PACKED) {
+  if (weights->layout != MILORA_W_ROWMAJOR) {
     if (dtype != MILORA_BF16 || d % 32 != 0 || F % 32 != 0) return MILORA_EUNSUPPORTED;
     if (!aligned16(x) || (attn_out && !aligned16(attn_out)) || !aligned16(y) || (qkv_out && !aligned16(qkv_out)))
       return MILORA_EUNSUPPORTED;
     for (int m = 0; m < MILORA_NUM_SITES; ++m)
       if (!aligned16(weights->W[m])) return MILORA_EUNSUPPORTED;
+    if (weights->layout == MILORA_W_MX4) {
+      if (marks) return MILORA_EUNSUPPORTED;
+      return layer_decode_mx4((const bf16_t*)x, B, d, F, weights, ad, tenant_id, route, flags, (const bf16_t*)attn_out, (bf16_t*)y,
+                              (bf16_t*)qkv_out, workspace, st);
+    }
     return layer_decode_packed((const bf16_t*)x, B, d, F, weights, ad, tenant_id, route, flags,
                                (const bf16_t*)attn_out, (bf16_t*)y, (bf16_t*)qkv_out, workspace, st, marks);
   }
@@ -511,6 +682,20 @@ extern "C" int milora_layer_decode_trace(const void* x, int B, int d, int F, int
   decode_trace_dims(&smax, &waves, &slots);
   dims[0] = marks.grid; dims[1] = marks.stages; dims[2] = smax; dims[3] = waves; dims[4] = slots;
   return MILORA_OK;
+}
+
+extern "C" size_t milora_quantized_weight_bytes(int d1, int d2) { return mx4_shape_ok(d1, d2) ? mx4_bytes(d1, d2) : 0; }
+
+extern "C" int milora_quantize_weight(const void* src_rowmajor, int dtype, void* dst, int d1, int d2, void* stream) {
+  if (!src_rowmajor || !dst || d1 < 1 || d2 < 1 || !valid_dtype(dtype)) return MILORA_EINVAL;
+  if (!mx4_shape_ok(d1, d2) || !aligned16(dst)) return MILORA_EUNSUPPORTED;
+  return mx4_quantize(src_rowmajor, dtype, dst, d1, d2, (hipStream_t)stream);
+}
+
+extern "C" int milora_dequantize_weight(const void* src, void* dst_rowmajor, int dtype, int d1, int d2, void* stream) {
+  if (!src || !dst_rowmajor || d1 < 1 || d2 < 1 || !valid_dtype(dtype)) return MILORA_EINVAL;
+  if (!mx4_shape_ok(d1, d2) || !aligned16(src)) return MILORA_EUNSUPPORTED;
+  return mx4_dequantize(src, dst_rowmajor, dtype, d1, d2, false, (hipStream_t)stream);
 }
 
 extern "C" int milora_pack_weight(const void* src_rowmajor, void* dst_packed, int d1, int d2, void* stream) {

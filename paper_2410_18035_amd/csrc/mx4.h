@@ -1,0 +1,43 @@
+// Interface of the 4-bit base weights (mx4.hip): storage, conversion, the few-row linears.
+#pragma once
+#include "common.h"
+
+namespace milora {
+
+// Storage of a weight of d1 inputs and d2 columns (MILORA_W_MX4): codes [d2][d1 / 2], the even input of a byte in its low
+// half, then one scale byte for 32 inputs of a column, [d2][d1 / 32].
+constexpr int kMxGroup = 32;
+inline bool mx4_shape_ok(int d1, int d2) { return d1 >= 1 && d2 >= 1 && d1 % kMxGroup == 0; }
+inline size_t mx4_code_bytes(int d1, int d2) { return (size_t)d1 * d2 / 2; }
+inline size_t mx4_bytes(int d1, int d2) { return mx4_code_bytes(d1, d2) + (size_t)d1 * d2 / kMxGroup; }
+
+int mx4_quantize(const void* src, int dtype, void* dst, int d1, int d2, hipStream_t st);
+// To [d2][d1] of `dtype`, or (bf16, d2 % 16 == 0) to the packed layout.
+int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool packed, hipStream_t st);
+
+// Few rows: up to kMxRows in one launch.
+constexpr int kMxRows = 32;
+struct MxArgs {
+  const bf16_t* X;  // M rows of ldx elements
+  int64_t ldx;
+  int M, d1, d2;
+  const unsigned char* W[3];  // of the sites of the launch; gated: W[0] gate, W[1] up
+  const bf16_t* bias;
+  bf16_t* Y[3];     // rows of ldy elements, or null (with res)
+  int64_t ldy;
+  float* gate_out;  // gated: [M][d2] or null
+  float* up_out;
+  const bf16_t* res;   // [M][d2] or null: h_out = res + linear, in fp32 (Y gets it rounded)
+  float* h_out;
+  const float* h_in;   // [M][d2] or null: Y = h_in + linear
+  const float* t;   // [site][part][t_rows][r_max] partial shrinks, to be added in part order
+  size_t t_part, t_site;  // floats from a part, a site to the next
+  int parts;
+  const int2* row_lora;   // [site][lora_rows] tenant and rank of each row
+  size_t lora_site;
+  AdapterView ad;
+  int site[3];
+};
+int launch_mx4_rows(const MxArgs& g, int sites, bool gated, hipStream_t st);
+
+}  // namespace milora

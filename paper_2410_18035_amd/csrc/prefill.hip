@@ -440,20 +440,36 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   }
 }
 
-template <int RT, bool INFO>
+// SITES: several sites in one launch, blockIdx.z = site x shares + share.
+template <int RT, bool INFO, bool SITES>
 __global__ void __launch_bounds__(512, 4) shrink_tiles_kernel(const ShrinkArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char smem[8 * kShrinkWaveBytes];
   __shared__ int row_ten[RT * 16 * (INFO ? 2 : 1)];
-  shrink_block<RT, 8, INFO>(g, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z, gridDim.z, smem, row_ten,
-                            [](float* p, float v) { *p = v; });
+  auto store = [](float* p, float v) { *p = v; };
+  if constexpr (SITES) {
+    const int shares = gridDim.z / g.sites, s = blockIdx.z / shares;
+    ShrinkArgs one = g;
+    one.site += s;
+    one.t += s * g.t_site;
+    if (one.row_lora) one.row_lora += s * g.lora_site;
+    shrink_block<RT, 8, INFO>(one, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z % shares, shares, smem, row_ten, store);
+  } else {
+    shrink_block<RT, 8, INFO>(g, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z, gridDim.z, smem, row_ten, store);
+  }
   static_assert(kShrinkClear == 512, "one word per thread");
   if (INFO && g.clear && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) g.clear[threadIdx.x] = 0;
 }
 
 template <int RT>
 void launch_shrink_block(const ShrinkArgs& g, dim3 grid, hipStream_t st) {
-  if (g.row_lora || g.clear) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true>), grid, dim3(512), 0, st, g);
-  else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false>), grid, dim3(512), 0, st, g);
+  const bool info = g.row_lora || g.clear;
+  if (g.sites > 1) {
+    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, true>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, true>), grid, dim3(512), 0, st, g);
+  } else {
+    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, false>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, false>), grid, dim3(512), 0, st, g);
+  }
 }
 
 }  // namespace
@@ -510,16 +526,18 @@ int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int3
   return MILORA_OK;
 }
 
-// LoRA shrink of the rows the tile kernel serves (same conditions as prefill_supported): t receives
-// shrink_parts(M, d1) partial results [part][M][r_max], to be added in part order, row_lora (or null) what the look-ups found of
-// each row; `clear` (or null) is zeroed.
-int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site,
+// LoRA shrink of the rows the tile kernel serves (same conditions as prefill_supported) at `sites` consecutive sites: t receives
+// shrink_parts(M, d1) partial results [site][part][M][r_max], to be added in part order, row_lora (or null) [site][M] what the
+// look-ups found of each row; `clear` (or null) is zeroed.
+int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
                         const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream) {
   const int parts = shrink_parts(M, d1);
   const int64_t slice = (int64_t)1 << 28;  // rows per launch: 512 threads for 64 rows, a grid has to stay below 2^32 threads
+  const size_t t_stride = (size_t)M * ad.r_max;
   for (int64_t r0 = 0; r0 < M; r0 += slice) {
-    ShrinkArgs g{X + (size_t)r0 * d1, M - r0 < slice ? M - r0 : slice, r0, d1, site, B, row_to_req ? row_to_req + r0 : nullptr,
-                 tenant_id, route, ad, t + (size_t)r0 * ad.r_max, (size_t)M * ad.r_max, row_lora ? row_lora + r0 : nullptr, clear};
+    ShrinkArgs g{X + (size_t)r0 * ldx, ldx, M - r0 < slice ? M - r0 : slice, r0, d1, site, B, row_to_req ? row_to_req + r0 : nullptr,
+                 tenant_id, route, ad, t + (size_t)r0 * ad.r_max, t_stride, row_lora ? row_lora + r0 : nullptr, clear,
+                 sites, t_stride * parts, (size_t)M};
     if (M <= kTileMaxRows) {
       // Workgroups share the units of a block (32 ranks of a tenant each) while there can be units for them and all are resident
       // at once, two per compute unit.  64 packed rows of 64 tenants, rank 256, 4096 x 4096, a call: 189 us with four at
@@ -528,15 +546,20 @@ int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_t
       const int tenants = B < ad.n_tenants ? B : ad.n_tenants;
       const int units = (tenants < 16 ? tenants : 16) * ((ad.r_max + kShrinkC - 1) / kShrinkC);
       int shares = 1;
-      while (shares < units && blocks * parts * shares * 2 <= 512) shares *= 2;
-      launch_shrink_block<1>(g, dim3((unsigned)blocks, parts, shares), stream);
+      while (shares < units && blocks * parts * sites * shares * 2 <= 512) shares *= 2;
+      launch_shrink_block<1>(g, dim3((unsigned)blocks, parts, shares * sites), stream);
     }
     else
-      launch_shrink_block<4>(g, dim3((unsigned)((g.M + 63) / 64), parts), stream);
+      launch_shrink_block<4>(g, dim3((unsigned)((g.M + 63) / 64), parts, sites), stream);
     const int rc = check_launch();
     if (rc) return rc;
   }
   return MILORA_OK;
+}
+
+int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site,
+                        const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream) {
+  return launch_shrink_sites(X, d1, M, d1, row_to_req, ad, site, 1, tenant_id, route, B, t, row_lora, clear, stream);
 }
 
 }  // namespace milora

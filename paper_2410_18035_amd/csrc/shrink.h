@@ -28,6 +28,7 @@ constexpr int kShrinkWaveBytes = kShrinkC * kShrinkLd * 2;      // 8.5 KiB: the 
 
 struct ShrinkArgs {
   const bf16_t* X;
+  int64_t ldx;          // elements from a row of X to the next
   int64_t M, row_base;  // rows, and the index of the first one in the caller's matrix (requests of unmapped rows)
   int d1, site, B;
   const int32_t* row_to_req;
@@ -38,6 +39,8 @@ struct ShrinkArgs {
   size_t t_stride;
   int2* row_lora;  // INFO: [M] receives tenant and rank of each row (rank 0: no LoRA term), or null
   int* clear;      // INFO: [kShrinkClear] words of the launch behind this one that have to start from zero, or null
+  int sites;       // consecutive sites of the launch, from `site` on; each has its own t and row_lora
+  size_t t_site, lora_site;  // elements from one site's to the next's
 };
 
 // Two by two bf16 of two words a (k) and b (k + 1): the pair of low halves, the pair of high halves.
@@ -115,7 +118,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& g, int row_block,
   for (int rt = 0; rt < RT; ++rt) {
     int64_t m = m0 + rt * 16 + (lane & 15);
     m = m < g.M ? m : g.M - 1;
-    xp[rt] = g.X + (size_t)m * g.d1 + (lane >> 4) * 8;
+    xp[rt] = g.X + (size_t)m * g.ldx + (lane >> 4) * 8;
   }
   int last = -1, unit = 0;  // (unit % shares)
   for (;;) {
