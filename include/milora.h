@@ -199,6 +199,63 @@ int milora_routed_linear(const void *X, int64_t M, int d1, int d2, int dtype,
                          size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * milora_gated_linear - the gated block of a layer for M rows: both projections with the LoRA terms of the requests routed
+ * to them, the activation and the product (Sec. 3.1; sites 4 and 5 with Eq. 1 and the layer-level gate of Sec. 3.3):
+ *   g = X W_gate + [route selects 4] (X W^A_4) W^B_4,  u = X W_up + [route selects 5] (X W^A_5) W^B_5
+ *   Y = silu(g) * u,  silu(g) = g / (1 + exp(-g))
+ * g and u are formed as milora_routed_linear forms its results and stay in fp32; Y is rounded once.  Inf and NaN in a tenant's
+ * matrices reach that tenant's rows only.
+ *
+ *   X          device [M][d], `dtype`
+ *   row_to_req, tenant_id, route, B, adapters: as for milora_routed_linear (the matrices of sites 4 and 5 are read)
+ *   W_gate, W_up  device, math shape d x F in `w_layout`: MILORA_W_ROWMAJOR, or MILORA_W_MX4 (dtype bf16)
+ *   Y          device [M][F], `dtype`; must not overlap any input
+ *   gate_out, up_out  device [M][F] float or NULL: g and u, for milora_gated_linear_backward
+ *   workspace  device, milora_gated_linear_workspace_bytes() bytes (the size never goes down when M, d, F or r_max go up by steps
+ *              that keep the kind of call); what it holds before a call does not matter
+ * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK, F >= 2^30, sizes beyond a launch), EUNSUPPORTED (MILORA_W_PACKED; 4-bit weights with fp32,
+ * with d % 32 != 0 or F % 16 != 0, or with X, Y or a weight not 16-byte aligned), EWORKSPACE, EHIP.
+ */
+size_t milora_gated_linear_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max);
+int milora_gated_linear(const void *X, int64_t M, int d, int F, int dtype, const int32_t *row_to_req,
+                        const void *W_gate, const void *W_up, int w_layout, const milora_adapters *adapters,
+                        const int32_t *tenant_id, const uint8_t *route, int B, void *Y, float *gate_out,
+                        float *up_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of the tenants' matrices (host struct; both arrays are device memory, as those of milora_adapters): entry t*7+m is the
+ * address of the gradient of W^A [d1][r_t] or W^B [r_t][d2] of (tenant t, site m) in `dtype`, NULL where it is not wanted. */
+typedef struct {
+  void *const *dA; /* device [T*7], or NULL: none */
+  void *const *dB; /* device [T*7], or NULL: none */
+} milora_gradients;
+
+/* ------------------------------------------------------------------------------------------------
+ * milora_gated_linear_backward - gradients behind milora_gated_linear: the base weights are frozen (Sec. 3.1), what
+ * learns are the LoRA matrices.  With s = 1 / (1 + exp(-g)):
+ *   dg = dY u s (1 + g (1 - s)),  du = dY g s
+ *   dX = dg W_gate^T + du W_up^T + sum over both sites of [routed] (dz (W^B)^T) (W^A)^T,  dz = dg at site 4, du at site 5
+ *   dW^A = sum over the tenant's routed rows of x^T (dz (W^B)^T),  dW^B = sum of (x W^A)^T dz
+ * dg and du are rounded to `dtype` for the matrix products (bf16: half of what separates the results from exact ones, the other half
+ * is their own rounding); sums are fp32, in an order that depends on the sizes and rows alone.
+ *
+ *   dY         device [M][F], `dtype`;  X: as in the forward call
+ *   gate, up   device [M][F] float: gate_out and up_out of the forward call
+ *   the others as in the forward call
+ *   dX         device [M][d], `dtype`, or NULL: not wanted
+ *   gradients  host struct or NULL: the wanted gradients of sites 4 and 5 are overwritten (zero for a tenant without rows); those of
+ *              other sites and of a tenant whose rank is out of range are left as they are.  No two entries may overlap.
+ *   workspace  device, milora_gated_linear_backward_workspace_bytes() bytes; what it holds before a call does not matter
+ * Errors: those of milora_gated_linear (X, dY and dX may have any alignment of their type); ERANGE also for more than 32767 tenants and more
+ * than 4194240 rows.
+ */
+size_t milora_gated_linear_backward_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max);
+int milora_gated_linear_backward(const void *dY, const void *X, const float *gate, const float *up, int64_t M, int d,
+                                 int F, int dtype, const int32_t *row_to_req, const void *W_gate, const void *W_up,
+                                 int w_layout, const milora_adapters *adapters, const int32_t *tenant_id,
+                                 const uint8_t *route, int B, void *dX, const milora_gradients *gradients,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
  * milora_layer_decode - one decode step of B requests through the seven routed linears of a layer,
  * using the cached routes (Sec. 3.3: the routing decisions of the prompt are reused for every
  * generated token; nothing here reads prompts or router weights, and `route` is read-only).

@@ -32,6 +32,8 @@ EXPORTS = (
     "milora_version", "milora_status_string", "milora_last_hip_error",
     "milora_route_workspace_bytes", "milora_route",
     "milora_routed_linear_workspace_bytes", "milora_quantized_linear_workspace_bytes", "milora_routed_linear_kernel", "milora_routed_linear_tile", "milora_routed_linear",
+    "milora_gated_linear_workspace_bytes", "milora_gated_linear",
+    "milora_gated_linear_backward_workspace_bytes", "milora_gated_linear_backward",
     "milora_layer_decode_workspace_bytes", "milora_layer_decode", "milora_layer_decode_noalloc",
     "milora_layer_decode_profile", "milora_layer_decode_trace_bytes", "milora_layer_decode_trace",
     "milora_pack_weight", "milora_quantized_weight_bytes", "milora_quantize_weight", "milora_dequantize_weight",
@@ -49,6 +51,10 @@ class MiloraError(RuntimeError):
 class _Adapters(ctypes.Structure):
     _fields_ = [("n_tenants", ctypes.c_int32), ("r_max", ctypes.c_int32), ("rank", ctypes.c_void_p),
                 ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
+
+
+class _Gradients(ctypes.Structure):
+    _fields_ = [("dA", ctypes.c_void_p), ("dB", ctypes.c_void_p)]
 
 
 class _LayerWeights(ctypes.Structure):
@@ -87,6 +93,16 @@ def lib() -> ctypes.CDLL:
         L.milora_routed_linear.restype = i32
         L.milora_routed_linear.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, vp, ctypes.POINTER(_Adapters), i32,
                                            vp, vp, i32, vp, vp, sz, vp]
+        L.milora_gated_linear_workspace_bytes.restype = sz
+        L.milora_gated_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+        L.milora_gated_linear.restype = i32
+        L.milora_gated_linear.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, i32, ctypes.POINTER(_Adapters), vp, vp, i32, vp, vp, vp,
+                                          vp, sz, vp]
+        L.milora_gated_linear_backward_workspace_bytes.restype = sz
+        L.milora_gated_linear_backward_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+        L.milora_gated_linear_backward.restype = i32
+        L.milora_gated_linear_backward.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, i32, ctypes.POINTER(_Adapters), vp,
+                                                   vp, i32, vp, ctypes.POINTER(_Gradients), vp, sz, vp]
         L.milora_layer_decode_workspace_bytes.restype = sz
         L.milora_layer_decode_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.milora_layer_decode.restype = i32
@@ -300,6 +316,117 @@ def milora_routed_linear(X: torch.Tensor, W: torch.Tensor, adapters: AdapterTabl
     if rc != 0:
         raise MiloraError(rc, "milora_routed_linear")
     return out
+
+
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def gated_linear_workspace_bytes(M: int, d: int, F: int, dtype: torch.dtype, w_layout: int, r_max: int) -> int:
+    return int(lib().milora_gated_linear_workspace_bytes(M, d, F, _CODES[dtype], w_layout, r_max))
+
+
+def gated_linear_backward_workspace_bytes(M: int, d: int, F: int, dtype: torch.dtype, w_layout: int, r_max: int) -> int:
+    return int(lib().milora_gated_linear_backward_workspace_bytes(M, d, F, _CODES[dtype], w_layout, r_max))
+
+
+def _shaped(t: Optional[torch.Tensor], shape, what: str) -> None:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {list(shape)}")
+
+
+def _gated_sizes(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, w_layout: int, F: Optional[int],
+                 row_to_req: Optional[torch.Tensor], route: torch.Tensor, B: int):
+    M, d = X.shape
+    if w_layout == W_ROWMAJOR:
+        F = W_gate.shape[0]
+    elif F is None:
+        raise ValueError("quantised weights need F")
+    _check_weight(W_gate, d, F, w_layout, X.dtype)
+    _check_weight(W_up, d, F, w_layout, X.dtype)
+    _shaped(row_to_req, (M,), "row_to_req")
+    _shaped(route, (B,), "route")
+    return M, d, F
+
+
+def milora_gated_linear(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, adapters: AdapterTable, tenant_id: torch.Tensor,
+                        route: torch.Tensor, row_to_req: Optional[torch.Tensor] = None, w_layout: int = W_ROWMAJOR,
+                        F: Optional[int] = None, out: Optional[torch.Tensor] = None, gate_out: Optional[torch.Tensor] = None,
+                        up_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = silu(X W_gate + its LoRA term) * (X W_up + its LoRA term).  Weights [F, d] row-major, or W_MX4 (then pass F);
+    gate_out and up_out, float32 [M, F], receive both projections for the backward pass."""
+    B = tenant_id.numel()
+    M, d, F = _gated_sizes(X, W_gate, W_up, w_layout, F, row_to_req, route, B)
+    if out is None:
+        out = torch.empty(M, F, dtype=X.dtype, device=X.device)
+    for t, what in ((out, "out"), (gate_out, "gate_out"), (up_out, "up_out")):
+        _shaped(t, (M, F), what)
+    if workspace is None:
+        workspace = _workspace(gated_linear_workspace_bytes(M, d, F, X.dtype, w_layout, adapters.r_max), X.device)
+    ad = adapters.c_struct()
+    rc = lib().milora_gated_linear(_dev(X), M, d, F, _dtype_code(X), _dev(row_to_req, torch.int32), _dev(W_gate), _dev(W_up), w_layout,
+                                   ctypes.byref(ad), _dev(tenant_id, torch.int32), _dev(route, torch.uint8), B, _dev(out, X.dtype),
+                                   _dev(gate_out, torch.float32), _dev(up_out, torch.float32), _dev(workspace), workspace.numel(), _stream())
+    if rc != 0:
+        raise MiloraError(rc, "milora_gated_linear")
+    return out
+
+
+@dataclass
+class GradientTable:
+    """Device-side pointer tables of one layer's per-tenant LoRA gradients (keeps them alive)."""
+
+    dA_ptrs: torch.Tensor  # int64 [T*7] device
+    dB_ptrs: torch.Tensor  # int64 [T*7] device
+    n_tenants: int
+    dtype: torch.dtype
+    keep: tuple
+
+    @staticmethod
+    def from_tensors(dA: Sequence[Sequence[Optional[torch.Tensor]]], dB: Sequence[Sequence[Optional[torch.Tensor]]]) -> "GradientTable":
+        """dA[t][m], dB[t][m] as the matrices of AdapterTable, or None where no gradient is wanted."""
+        if len(dA) != len(dB) or any(len(row) != NUM_SITES for rows in (dA, dB) for row in rows):
+            raise ValueError("a gradient, or None, for each of the seven sites of every tenant")
+        every = [g for rows in (dA, dB) for row in rows for g in row if g is not None]
+        if not every:
+            raise ValueError("no gradient wanted: pass grads=None")
+        if any(g.dtype != every[0].dtype for g in every):
+            raise TypeError("gradients must share a dtype")
+        ptrs = lambda rows: torch.tensor([_dev(g) or 0 for row in rows for g in row], dtype=torch.int64, device=every[0].device)
+        return GradientTable(ptrs(dA), ptrs(dB), len(dA), every[0].dtype, (dA, dB))
+
+    def c_struct(self) -> _Gradients:
+        return _Gradients(self.dA_ptrs.data_ptr(), self.dB_ptrs.data_ptr())
+
+
+def milora_gated_linear_backward(dY: torch.Tensor, X: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, W_gate: torch.Tensor,
+                                 W_up: torch.Tensor, adapters: AdapterTable, tenant_id: torch.Tensor, route: torch.Tensor,
+                                 row_to_req: Optional[torch.Tensor] = None, w_layout: int = W_ROWMAJOR, F: Optional[int] = None,
+                                 dX: Optional[torch.Tensor] = None, want_dx: bool = True, grads: Optional[GradientTable] = None,
+                                 workspace: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Gradients behind milora_gated_linear, whose gate_out and up_out are gate and up: returns dX (None without want_dx) and
+    overwrites the LoRA gradients of sites 4 and 5 that `grads` names."""
+    B = tenant_id.numel()
+    M, d, F = _gated_sizes(X, W_gate, W_up, w_layout, F, row_to_req, route, B)
+    if dX is None and want_dx:
+        dX = torch.empty_like(X)
+    if not want_dx:
+        dX = None
+    for t, what in ((dY, "dY"), (gate, "gate"), (up, "up")):
+        _shaped(t, (M, F), what)
+    _shaped(dX, (M, d), "dX")
+    if grads is not None and (grads.n_tenants != adapters.n_tenants or grads.dtype != X.dtype):
+        raise ValueError("gradients must cover the adapters' tenants in the dtype of X")
+    if workspace is None:
+        workspace = _workspace(gated_linear_backward_workspace_bytes(M, d, F, X.dtype, w_layout, adapters.r_max), X.device)
+    ad = adapters.c_struct()
+    gr = grads.c_struct() if grads is not None else None
+    rc = lib().milora_gated_linear_backward(
+        _dev(dY, X.dtype), _dev(X), _dev(gate, torch.float32), _dev(up, torch.float32), M, d, F, _dtype_code(X), _dev(row_to_req, torch.int32),
+        _dev(W_gate), _dev(W_up), w_layout, ctypes.byref(ad), _dev(tenant_id, torch.int32), _dev(route, torch.uint8), B, _dev(dX, X.dtype),
+        ctypes.byref(gr) if gr is not None else None, _dev(workspace), workspace.numel(), _stream())
+    if rc != 0:
+        raise MiloraError(rc, "milora_gated_linear_backward")
+    return dX
 
 
 def layer_decode_workspace_bytes(B: int, d: int, F: int, r_max: int) -> int:

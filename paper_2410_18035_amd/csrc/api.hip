@@ -1,6 +1,7 @@
 // C ABI of the routed-LoRA library: argument validation, workspace carving and dispatch between
 // the decode kernels (bf16, packed weights), the matrix-core tiles (bf16, row-major weights or packed ones
 // of many rows) and the any-shape path (fp32 and everything else).
+#include "gated.h"
 #include "mx4.h"
 #include "tiles.h"
 
@@ -545,6 +546,58 @@ extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, in
     return run_linear_mx4((const bf16_t*)X, M, d1, d2, row_to_req, W, (const bf16_t*)bias, ad, site, tenant_id, route, B, (bf16_t*)Y,
                           workspace, st);
   return run_linear(X, M, d1, d2, dtype, row_to_req, W, packed, bias, ad, site, tenant_id, route, B, Y, workspace, st);
+}
+
+// Arguments that the gated block and its backward pass share.
+static int check_gated(int64_t M, int d, int F, int dtype, const int32_t* row_to_req, const void* Wg, const void* Wu, int w_layout,
+                       const milora_adapters* adapters, const int32_t* tenant_id, const uint8_t* route, int B) {
+  if (!Wg || !Wu || !tenant_id || !route) return MILORA_EINVAL;
+  if (M < 1 || d < 1 || F < 1 || B < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return MILORA_EINVAL;
+  if (!row_to_req && M != B) return MILORA_EINVAL;
+  const int rc = check_adapters(adapters);
+  if (rc) return rc;
+  if (M > 0x7fffffffLL || F > 0x3fffffff) return MILORA_ERANGE;
+  if (w_layout == MILORA_W_PACKED) return MILORA_EUNSUPPORTED;
+  if (w_layout == MILORA_W_MX4 && (dtype != MILORA_BF16 || !packed_shape_ok(d, F) || !aligned16(Wg) || !aligned16(Wu))) return MILORA_EUNSUPPORTED;
+  return MILORA_OK;
+}
+
+extern "C" size_t milora_gated_linear_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max) {
+  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
+  return gated_workspace_bytes(M, d, F, dtype, w_layout == MILORA_W_MX4, r_max);
+}
+
+extern "C" int milora_gated_linear(const void* X, int64_t M, int d, int F, int dtype, const int32_t* row_to_req, const void* W_gate,
+                                   const void* W_up, int w_layout, const milora_adapters* adapters, const int32_t* tenant_id,
+                                   const uint8_t* route, int B, void* Y, float* gate_out, float* up_out, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (!X || !Y) return MILORA_EINVAL;
+  const int rc = check_gated(M, d, F, dtype, row_to_req, W_gate, W_up, w_layout, adapters, tenant_id, route, B);
+  if (rc) return rc;
+  if (w_layout == MILORA_W_MX4 && (!aligned16(X) || !aligned16(Y))) return MILORA_EUNSUPPORTED;
+  if (!workspace || workspace_bytes < milora_gated_linear_workspace_bytes(M, d, F, dtype, w_layout, adapters->r_max)) return MILORA_EWORKSPACE;
+  const GatedCall g{X, M, d, F, dtype, w_layout == MILORA_W_MX4, row_to_req, W_gate, W_up, view_of(adapters), tenant_id, route, B};
+  return run_gated(g, Y, gate_out, up_out, workspace, (hipStream_t)stream);
+}
+
+extern "C" size_t milora_gated_linear_backward_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max) {
+  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
+  return gated_backward_workspace_bytes(M, d, F, dtype, w_layout == MILORA_W_MX4, r_max);
+}
+
+extern "C" int milora_gated_linear_backward(const void* dY, const void* X, const float* gate, const float* up, int64_t M, int d, int F,
+                                            int dtype, const int32_t* row_to_req, const void* W_gate, const void* W_up, int w_layout,
+                                            const milora_adapters* adapters, const int32_t* tenant_id, const uint8_t* route, int B,
+                                            void* dX, const milora_gradients* gradients, void* workspace, size_t workspace_bytes,
+                                            void* stream) {
+  if (!dY || !X || !gate || !up) return MILORA_EINVAL;
+  const int rc = check_gated(M, d, F, dtype, row_to_req, W_gate, W_up, w_layout, adapters, tenant_id, route, B);
+  if (rc) return rc;
+  if (!workspace || workspace_bytes < milora_gated_linear_backward_workspace_bytes(M, d, F, dtype, w_layout, adapters->r_max))
+    return MILORA_EWORKSPACE;
+  const GatedCall g{X, M, d, F, dtype, w_layout == MILORA_W_MX4, row_to_req, W_gate, W_up, view_of(adapters), tenant_id, route, B};
+  return run_gated_backward(g, dY, gate, up, dX, gradients ? gradients->dA : nullptr, gradients ? gradients->dB : nullptr, workspace,
+                            (hipStream_t)stream);
 }
 
 extern "C" int milora_packed_workspace_status(const void* workspace, int* status, void* stream) {

@@ -177,6 +177,10 @@ int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, c
                           const void* W, const void* bias, const AdapterView& ad, int site,
                           const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y, hipStream_t stream);
 
+// The same without bias, from shrinks that are there already, in fp32.
+int launch_linear_f32(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req, const void* W, const AdapterView& ad,
+                      int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, float* Y, hipStream_t stream);
+
 // The same for up to kFewRows rows, with the glue of a layer's decode step in its store.
 constexpr int kFewRows = 16;
 constexpr int kFuseRank = 16;  // the largest rank that can be shrunk inside the launch
@@ -185,6 +189,7 @@ enum FewMode {
   kFewResid,   // h = x_res + linear (fp32); Y[0] = h rounded, if given
   kFewGateUp,  // Y[0] = silu(linear at site[0]) * linear at site[1]
   kFewDown,    // Y[0] = h + linear
+  kFewGated,   // the gated block: as kFewGateUp with both linears in fp32 up to the store; they go to gate_out and up_out, if given
 };
 struct FewArgs {
   const void* X;  // M rows of ldx elements
@@ -202,6 +207,8 @@ struct FewArgs {
   AdapterView ad;
   const void* x_res;
   float* h;
+  float* gate_out;  // [M][d2]
+  float* up_out;
   const float* t;  // filled in by the launch
   int col0;        // first column of the launch, the same
 };

@@ -1,0 +1,508 @@
+// The gated block of a layer with the LoRA terms of its two sites (paper Sec. 3.1, Eq. 1): g = X W_gate + [routed] (X A4) B4,
+// u = X W_up + [routed] (X A5) B5, Y = silu(g) u, g and u in fp32 up to the one rounding of Y.  And its backward pass against a frozen base:
+//   dg = dY u s (1 + g (1 - s)), du = dY g s, s = 1 / (1 + e^-g)
+//   dX = dg W_gate^T + du W_up^T + sum over the two sites of low A^T,  low = dz B^T (routed rows)
+//   dA = sum over the tenant's rows of x^T low,  dB = sum of (x A)^T dz
+//
+// Forward: bf16 takes the matrix-core tiles with gate and up columns side by side (tiles.hip, prefill.hip), 4-bit weights of few rows
+// mx4.hip, everything else the any-shape kernels of linear_generic.hip.
+#include "gated.h"
+#include "mx4.h"
+#include "tiles.h"
+
+namespace milora {
+
+// prefill.hip
+bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, const void* Y);
+int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
+                        const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream);
+
+namespace {
+
+constexpr int kGate = 4;  // site; the up projection's is the next
+constexpr int kThreads = 256;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// What of a workspace a call needs, in the order of its calls.
+struct Carver {
+  char* base;
+  size_t off = 0;
+  template <typename T>
+  T* take(size_t n) {
+    T* const p = (T*)(base + off);
+    off += align_up(n * sizeof(T), 256);
+    return p;
+  }
+};
+
+// ---- forward ---------------------------------------------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_glue_kernel(const float* __restrict__ g, const float* __restrict__ u, int64_t n, T* __restrict__ y) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) Elem<T>::store(y, i, silu(g[i]) * u[i]);
+}
+
+template <typename T>
+int launch_glue(const float* g, const float* u, int64_t n, void* y, hipStream_t st) {
+  const int64_t slice = (int64_t)1 << 31;  // a grid has to stay below 2^32 threads
+  int rc = MILORA_OK;
+  for (int64_t i = 0; i < n && !rc; i += slice) {
+    const int64_t c = n - i < slice ? n - i : slice;
+    hipLaunchKernelGGL(gated_glue_kernel<T>, dim3((unsigned)((c + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, g + i, u + i, c, (T*)y + i);
+    rc = check_launch();
+  }
+  return rc;
+}
+
+}  // namespace
+
+constexpr int64_t kMxGatedRows = 128;  // up to this many rows the few-row kernel reads the codes, beyond the weights are written out in bf16
+
+// The any-shape path holds g and u of so many rows at a time in fp32, 64 MB of both unless 64 rows are more.
+constexpr int64_t kAnyFloats = (int64_t)1 << 23;
+int64_t any_rows(int F) { return kAnyFloats / F > 64 ? kAnyFloats / F : 64; }
+
+size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
+  size_t most = 0;
+  if (dtype == MILORA_BF16) {  // control words, shrinks of both sites, look-ups, partial tiles, 4-bit weights in bf16
+    Carver c{nullptr};
+    c.take<char>(kStreamCtrlBytes);
+    c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
+    c.take<int2>((size_t)M * 2);
+    c.take<char>(partial_bytes_bound(M, d, 2 * F));
+    if (mx4 && M > kMxGatedRows) c.take<bf16_t>((size_t)d * F * 2);
+    most = c.off;
+  }
+  if (!mx4) {  // (bf16 too: whatever the alignment of its tensors)
+    Carver c{nullptr};
+    c.take<float>((size_t)M * r_max * 2);
+    const size_t held = (size_t)(kAnyFloats > (int64_t)64 * F ? kAnyFloats : (int64_t)64 * F), all = (size_t)M * F;
+    c.take<float>(2 * (all < held ? all : held));
+    most = c.off > most ? c.off : most;
+  }
+  return most;
+}
+
+int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void* workspace, hipStream_t st) {
+  const int64_t M = g.M;
+  int rc;
+  if (g.mx4 && M <= kMxGatedRows) {
+    Carver c{(char*)workspace};
+    const int parts = shrink_parts(M, g.d);
+    MxArgs a{};
+    a.ldx = g.d; a.d1 = g.d; a.d2 = g.F; a.W[0] = (const unsigned char*)g.Wg; a.W[1] = (const unsigned char*)g.Wu; a.ldy = g.F; a.ad = g.ad;
+    a.site[0] = kGate;
+    float* const t = c.take<float>((size_t)M * g.ad.r_max * parts * 2);
+    int2* const lora = c.take<int2>((size_t)M * 2);
+    a.t_part = (size_t)M * g.ad.r_max; a.t_site = a.t_part * parts; a.parts = parts; a.lora_site = (size_t)M;
+    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, lora, nullptr, st);
+    for (int64_t m0 = 0; m0 < M && !rc; m0 += kMxRows) {
+      a.M = (int)(M - m0 < kMxRows ? M - m0 : kMxRows);
+      a.X = (const bf16_t*)g.X + m0 * g.d;
+      a.Y[0] = (bf16_t*)Y + m0 * g.F;
+      a.gate_out = gate_out ? gate_out + m0 * g.F : nullptr;
+      a.up_out = up_out ? up_out + m0 * g.F : nullptr;
+      a.t = t + m0 * g.ad.r_max;
+      a.row_lora = lora + m0;
+      rc = launch_mx4_rows(a, 1, true, st);
+    }
+    return rc;
+  }
+  const bool packed = g.mx4 && g.d % 64 != 0;  // the layout 4-bit weights are written out in: the row-major tiles take whole 64 of a reduction
+  const void* const like = g.mx4 ? (const void*)(uintptr_t)256 : nullptr;  // (in the workspace: aligned)
+  const void *Wg = like ? like : g.Wg, *Wu = like ? like : g.Wu;
+  const bool small = g.dtype == MILORA_BF16 && g.F < 1 << 30 && tiles_supported(M, g.d, 2 * g.F, packed, g.X, Wg, Y) && aligned16(Wu) && g.F % 16 == 0;
+  const bool large = g.dtype == MILORA_BF16 && !packed && prefill_supported(M, g.d, g.F, g.X, Wg, Y) && aligned16(Wu);
+  if (small || large) {
+    Carver c{(char*)workspace};
+    char* const ctrl = c.take<char>(kStreamCtrlBytes);
+    const int parts = shrink_parts(M, g.d);
+    GatedTileArgs a{};
+    a.d = g.d; a.F = g.F; a.packed = packed; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
+    a.t_stride = (size_t)M * g.ad.r_max; a.t_site = a.t_stride * parts; a.parts = parts; a.lora_site = (size_t)M;
+    a.cnt = (int*)(ctrl + kTileCtrlOffset);
+    float* const t = c.take<float>(shrink_rows_bound(M, g.d) * g.ad.r_max * 2);
+    int2* const looked_up = c.take<int2>((size_t)M * 2);
+    a.partial = c.take<float>(partial_bytes_bound(M, g.d, 2 * g.F) / sizeof(float));
+    if (g.mx4) {
+      bf16_t* const w = c.take<bf16_t>((size_t)g.d * g.F * 2);
+      rc = mx4_dequantize(g.Wg, w, MILORA_BF16, g.d, g.F, packed, st);
+      if (!rc) rc = mx4_dequantize(g.Wu, w + (size_t)g.d * g.F, MILORA_BF16, g.d, g.F, packed, st);
+      if (rc) return rc;
+      Wg = w;
+      Wu = w + (size_t)g.d * g.F;
+    }
+    a.Wg = (const bf16_t*)Wg;
+    a.Wu = (const bf16_t*)Wu;
+    // slices of rows where the smaller tiles are the only ones and the call has more than a launch of them takes
+    const int64_t slice = large || M <= kTileMaxRows ? M : kTileMaxRows;
+    const TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large);
+    int2* const row_lora = large ? nullptr : looked_up;
+    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, row_lora,
+                             row_lora || first.S > 1 ? a.cnt : nullptr, st);
+    for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
+      a.M = M - m0 < slice ? M - m0 : slice;
+      a.row_base = m0;
+      a.X = (const bf16_t*)g.X + (size_t)m0 * g.d;
+      a.Y = (bf16_t*)Y + (size_t)m0 * g.F;
+      a.gate_out = gate_out ? gate_out + (size_t)m0 * g.F : nullptr;
+      a.up_out = up_out ? up_out + (size_t)m0 * g.F : nullptr;
+      a.row_to_req = g.row_to_req ? g.row_to_req + m0 : nullptr;
+      a.t = t + (size_t)m0 * g.ad.r_max;
+      a.row_lora = row_lora ? row_lora + m0 : nullptr;
+      const TilePlan pl = a.M == slice ? first : plan_tiles(a.M, g.d, 2 * g.F, small, large);
+      rc = pl.shape == kTiles256 ? gated_prefill(a, st) : gated_tiles(a, pl, st);
+    }
+    return rc;
+  }
+  // any shape and type
+  if (g.mx4) return MILORA_EUNSUPPORTED;
+  Carver c{(char*)workspace};
+  float* const t = c.take<float>((size_t)M * g.ad.r_max * 2);
+  if (M <= kFewRows) {
+    FewArgs a{};
+    a.X = g.X; a.ldx = g.d; a.M = (int)M; a.d1 = g.d; a.d2 = g.F;
+    a.W[0] = g.Wg; a.W[1] = g.Wu; a.Y[0] = Y; a.ldy = g.F; a.site[0] = kGate; a.site[1] = kGate + 1;
+    a.row_to_req = g.row_to_req; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B; a.ad = g.ad;
+    a.gate_out = gate_out; a.up_out = up_out;
+    return launch_few_rows(a, g.dtype, 2, kFewGated, t, st);
+  }
+  if (M > (int64_t)65535 * 64) return MILORA_ERANGE;
+  rc = launch_shrink(g.X, g.d, M, g.d, g.dtype, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, st);
+  const int64_t slice = any_rows(g.F);
+  const size_t es = dtype_size(g.dtype);
+  float* const held = c.take<float>(0);
+  for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
+    const int64_t rows = M - m0 < slice ? M - m0 : slice;
+    const char* const x = (const char*)g.X + (size_t)m0 * g.d * es;
+    char* const y = (char*)Y + (size_t)m0 * g.F * es;
+    const int32_t* const map = g.row_to_req ? g.row_to_req + m0 : nullptr;
+    const int64_t b0 = map ? 0 : m0;  // (unmapped rows: the slice's requests)
+    float* const gate = gate_out ? gate_out + (size_t)m0 * g.F : held;
+    float* const up = up_out ? up_out + (size_t)m0 * g.F : held + (size_t)rows * g.F;
+    for (int s = 0; s < 2 && !rc; ++s)
+      rc = launch_linear_f32(x, rows, g.d, g.F, g.dtype, map, s ? g.Wu : g.Wg, g.ad, kGate + s, g.tenant_id + b0, g.route + b0, (int)(g.B - b0),
+                             t + ((size_t)s * M + m0) * g.ad.r_max, s ? up : gate, st);
+    if (!rc) rc = g.dtype == MILORA_BF16 ? launch_glue<bf16_t>(gate, up, rows * g.F, y, st) : launch_glue<float>(gate, up, rows * g.F, y, st);
+  }
+  return rc;
+}
+
+// ---- backward --------------------------------------------------------------------------------------------------------------
+namespace {
+
+// dz = [dg | du], rows of 2 F: a workgroup takes kDzCols columns of a row.
+constexpr int kDzCols = 2048;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_dz_kernel(const T* __restrict__ dy, const float* __restrict__ g, const float* __restrict__ u,
+                                                            int F, int pieces, T* __restrict__ dz) {
+  const int64_t m = blockIdx.x / pieces;
+  const int j0 = blockIdx.x % pieces * kDzCols;
+  for (int j = j0 + threadIdx.x; j < F && j < j0 + kDzCols; j += kThreads) {
+    const int64_t i = m * F + j;
+    const float y = Elem<T>::load(dy, i), gv = g[i], uv = u[i], s = 1.f / (1.f + __expf(-gv));
+    T* const row = dz + m * 2 * F;
+    Elem<T>::store(row, j, y * uv * s * (1.f + gv * (1.f - s)));
+    Elem<T>::store(row, F + j, y * gv * s);
+  }
+}
+
+template <typename T>
+int launch_dz(const void* dY, const float* gate, const float* up, int64_t M, int F, void* dz, hipStream_t st) {
+  const int pieces = (F + kDzCols - 1) / kDzCols;
+  const int64_t slice = ((int64_t)1 << 23) / pieces;  // rows of a launch: a grid has to stay below 2^32 threads
+  if (slice < 1) return MILORA_ERANGE;
+  int rc = MILORA_OK;
+  for (int64_t m = 0; m < M && !rc; m += slice) {
+    const int64_t rows = M - m < slice ? M - m : slice;
+    hipLaunchKernelGGL(gated_dz_kernel<T>, dim3((unsigned)(rows * pieces)), dim3(kThreads), 0, st, (const T*)dY + m * F, gate + m * F, up + m * F, F,
+                       pieces, (T*)dz + m * 2 * F);
+    rc = check_launch();
+  }
+  return rc;
+}
+
+// Tenant and rank of every row at the two sites, [site][M], and the least and the largest tenant among 64 rows, [site][M / 64].
+__global__ void __launch_bounds__(kThreads) gated_rows_kernel(int64_t M, const int32_t* __restrict__ row_to_req, AdapterView ad,
+                                                              const int32_t* __restrict__ tenant_id, const uint8_t* __restrict__ route, int B,
+                                                              int2* __restrict__ row_lora, int2* __restrict__ among) {
+  const int64_t m = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t req = m < M ? (row_to_req ? (int64_t)row_to_req[m] : m) : -1;
+  for (int s = 0; s < 2; ++s) {
+    int tenant = -1;
+    const int r = req >= 0 && req < B ? routed_rank(ad, tenant_id, route, (int)req, B, kGate + s, &tenant) : 0;
+    if (m < M) row_lora[s * M + m] = int2{r ? tenant : -1, r};
+    int lo = r ? tenant : 0x7fffffff, hi = r ? tenant : -1;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int a = __shfl_xor(lo, off, 64), b = __shfl_xor(hi, off, 64);
+      lo = a < lo ? a : lo;
+      hi = b > hi ? b : hi;
+    }
+    if ((threadIdx.x & 63) == 0 && m < M) among[s * ((M + 63) / 64) + (m >> 6)] = int2{lo, hi};
+  }
+}
+
+// low[site][m][c] = sum_j dz[m][site F + j] B[c][j] for the routed rows: a workgroup for a row and site, a wave for a rank.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_low_kernel(const T* __restrict__ dz, int64_t M, int F, const int2* __restrict__ row_lora, AdapterView ad,
+                                                             float* __restrict__ low) {
+  const int64_t m = blockIdx.x;
+  const int s = blockIdx.y, lane = threadIdx.x & 63;
+  const int2 tr = row_lora[s * M + m];
+  if (tr.y == 0) return;
+  const T* const z = dz + m * 2 * F + (int64_t)s * F;
+  const T* const B = (const T*)ad.B[tr.x * MILORA_NUM_SITES + kGate + s];
+  for (int c = threadIdx.x >> 6; c < tr.y; c += kThreads / 64) {
+    float sum = 0.f;
+    for (int j = lane; j < F; j += 64) sum += Elem<T>::load(z, j) * Elem<T>::load(B, (size_t)c * F + j);
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_down(sum, off, 64);
+    if (lane == 0) low[((size_t)s * M + m) * ad.r_max + c] = sum;
+  }
+}
+
+// dX of any shape and type: 64 x 64 tiles, 32 of the reduction (2 F) at a time through LDS, fp32 matrix instructions; the LoRA part of a
+// row after them.
+constexpr int kNnK = 32;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_dx_kernel(const T* __restrict__ dz, int64_t M, int d, int F, const T* __restrict__ Wg,
+                                                            const T* __restrict__ Wu, const int2* __restrict__ row_lora, AdapterView ad,
+                                                            const float* __restrict__ low, T* __restrict__ dX) {
+  __shared__ float zs[64][kNnK + 1], ws[kNnK][64 + 4];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l32 = lane & 31, lh = lane >> 5;
+  const int64_t m0 = (int64_t)blockIdx.y * 64;
+  const int n0 = blockIdx.x * 64, wm = w & 1, wn = w >> 1;
+  f32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  for (int half = 0; half < 2; ++half) {
+    const T* const W = half ? Wu : Wg;
+    for (int k0 = 0; k0 < F; k0 += kNnK) {
+      __syncthreads();
+      for (int e = tid; e < 64 * kNnK; e += kThreads) {
+        const int row = e / kNnK, k = k0 + e % kNnK;
+        zs[row][e % kNnK] = m0 + row < M && k < F ? Elem<T>::load(dz, (m0 + row) * 2 * F + (int64_t)half * F + k) : 0.f;
+        const int col = n0 + e % 64, kw = k0 + e / 64;
+        ws[e / 64][e % 64] = col < d && kw < F ? Elem<T>::load(W, (size_t)kw * d + col) : 0.f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kNnK; k += 2)
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(ws[k + lh][wn * 32 + l32], zs[wm * 32 + l32][k + lh], acc, 0, 0, 0);
+    }
+  }
+  // (lane: row l % 32, registers 4 g .. + 3: columns 8 g + 4 (l / 32) ..)
+  const int64_t m = m0 + wm * 32 + l32;
+  if (m >= M) return;
+  for (int s = 0; s < 2; ++s) {
+    const int2 tr = row_lora[s * M + m];
+    if (tr.y == 0) continue;
+    const T* const A = (const T*)ad.A[tr.x * MILORA_NUM_SITES + kGate + s];
+    const float* const lw = low + ((size_t)s * M + m) * ad.r_max;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int n = n0 + wn * 32 + (e >> 2) * 8 + lh * 4 + (e & 3);
+      if (n >= d) continue;
+      float v = 0.f;
+      for (int c = 0; c < tr.y; ++c) v += lw[c] * Elem<T>::load(A, (size_t)n * tr.y + c);
+      acc[e] += v;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int n = n0 + wn * 32 + (e >> 2) * 8 + lh * 4 + (e & 3);
+    if (n < d) Elem<T>::store(dX, (size_t)m * d + n, acc[e]);
+  }
+}
+
+// Gradients of the tenants' matrices: out[col][c] = sum over the tenant's rows m of P[m][col] s[m][c], with (P, s) = (X, low) for dA and
+// (dz of the site, x A) for dB.  A workgroup takes 64 columns and 32 ranks of one of the tenant's four matrices; its rows, in order, 32 at a time.
+struct GradArgs {
+  const void *X, *dz;
+  int64_t M;
+  int d, F, T, tiles_a, tiles_b, chunks;  // 64-column tiles of dA and dB, chunks of 32 ranks
+  const int2 *row_lora, *among;
+  AdapterView ad;
+  const float *low, *t;  // [site][M][r_max]
+  size_t t_part;
+  size_t t_site;
+  int parts;
+  void* const* dA;
+  void* const* dB;
+};
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) {
+  __shared__ float ps[32][64 + 4], ss[32][32 + 4];
+  __shared__ int rows[64 + kThreads];
+  __shared__ int span[2];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l32 = lane & 31, lh = lane >> 5;
+  const int tile = blockIdx.x % (g.tiles_a + g.tiles_b), c0 = blockIdx.x / (g.tiles_a + g.tiles_b) * 32;
+  const int s = blockIdx.y & 1, ten = blockIdx.y >> 1;
+  const bool is_b = tile >= g.tiles_a;
+  void* const* const table = is_b ? g.dB : g.dA;
+  T* const out = table ? (T*)table[ten * MILORA_NUM_SITES + kGate + s] : nullptr;
+  const int r = g.ad.rank[ten];
+  if (!out || r < 1 || r > g.ad.r_max || c0 >= r) return;
+  const int cols = is_b ? g.F : g.d, n0 = (is_b ? tile - g.tiles_a : tile) * 64;
+  const T* const P = is_b ? (const T*)g.dz + (int64_t)s * g.F : (const T*)g.X;
+  const int64_t ldp = is_b ? 2 * (int64_t)g.F : g.d;
+  const float* const sc = is_b ? g.t + s * g.t_site : g.low + (size_t)s * g.M * g.ad.r_max;
+  const int parts = is_b ? g.parts : 1;
+  // the first and the last 64 rows that can hold one of the tenant's
+  const int blocks = (int)((g.M + 63) / 64);
+  if (tid == 0) { span[0] = blocks; span[1] = 0; }
+  __syncthreads();
+  {
+    int first = blocks, end = 0;
+    for (int i = tid; i < blocks; i += kThreads) {
+      const int2 a = g.among[(size_t)s * blocks + i];
+      if (ten < a.x || ten > a.y) continue;
+      first = first < i ? first : i;
+      end = i + 1;
+    }
+    if (first < end) {
+      atomicMin(&span[0], first);
+      atomicMax(&span[1], end);
+    }
+  }
+  __syncthreads();
+  const int64_t m_end = (int64_t)span[1] * 64 < g.M ? (int64_t)span[1] * 64 : g.M;
+  f32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  int have = 0;
+  for (int64_t m0 = (int64_t)span[0] * 64; m0 < m_end || have > 0;) {
+    // list the tenant's rows among the next ones, in their order
+    while (have < 32 && m0 < m_end) {
+      const int64_t m = m0 + tid;
+      const bool mine = m < m_end && g.row_lora[s * g.M + m].x == ten;
+      const unsigned long long votes = __ballot(mine);
+      __shared__ int counts[kThreads / 64];
+      if (lane == 0) counts[w] = __popcll(votes);
+      __syncthreads();
+      int at = have;
+      for (int i = 0; i < w; ++i) at += counts[i];
+      if (mine) rows[at + __popcll(votes & ((1ull << lane) - 1))] = (int)m;
+      for (int i = 0; i < kThreads / 64; ++i) have += counts[i];
+      m0 += kThreads;
+      __syncthreads();
+    }
+    if (have == 0) break;
+    const int n = have < 32 ? have : 32;
+    for (int e = tid; e < 32 * 64; e += kThreads) {
+      const int k = e >> 6, col = n0 + (e & 63);
+      ps[k][e & 63] = k < n && col < cols ? Elem<T>::load(P, (size_t)rows[k] * ldp + col) : 0.f;
+    }
+    for (int e = tid; e < 32 * 32; e += kThreads) {
+      const int k = e >> 5, c = c0 + (e & 31);
+      float v = 0.f;
+      if (k < n && c < r)
+        for (int p = 0; p < parts; ++p) v += sc[p * g.t_part + (size_t)rows[k] * g.ad.r_max + c];
+      ss[k][e & 31] = v;
+    }
+    __syncthreads();
+    if (w < 2)
+#pragma unroll
+      for (int k = 0; k < 32; k += 2) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(ss[k + lh][l32], ps[k + lh][w * 32 + l32], acc, 0, 0, 0);
+    // the rows that are left move to the front
+    int keep = 0;
+    if (tid < have - n) keep = rows[n + tid];
+    __syncthreads();
+    if (tid < have - n) rows[tid] = keep;
+    have -= n;
+    __syncthreads();
+  }
+  if (w >= 2) return;
+  const int col = n0 + w * 32 + l32;
+  if (col >= cols) return;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int c = c0 + (e >> 2) * 8 + lh * 4 + (e & 3);
+    if (c < r) Elem<T>::store(out, is_b ? (size_t)c * g.F + col : (size_t)col * r + c, acc[e]);
+  }
+}
+
+struct BackWs {
+  void* dz;        // [M][2 F] dtype
+  float* low;      // [2][M][r_max]
+  float* t;        // [2][part][M][r_max]
+  int2* row_lora;  // [2][M]
+  int2* among;     // [2][M / 64]
+  void* W;         // 4-bit weights in bf16
+  size_t bytes;
+};
+
+BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
+  Carver c{(char*)base};
+  BackWs w;
+  w.dz = c.take<char>((size_t)M * F * 2 * dtype_size(dtype));
+  w.low = c.take<float>((size_t)M * r_max * 2);
+  w.t = c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
+  w.row_lora = c.take<int2>((size_t)M * 2);
+  w.among = c.take<int2>((size_t)((M + 63) / 64) * 2);
+  w.W = c.take<bf16_t>(mx4 ? (size_t)d * F * 2 : 0);
+  w.bytes = c.off;
+  return w;
+}
+
+template <typename T>
+int backward_any(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB, const BackWs& w,
+                 hipStream_t st) {
+  const int64_t M = g.M;
+  const int tenants = g.ad.n_tenants;
+  if ((M + 63) / 64 > 65535 || tenants > 32767) return MILORA_ERANGE;
+  int rc = launch_dz<T>(dY, gate, up, M, g.F, w.dz, st);
+  if (rc) return rc;
+  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
+                     g.route, g.B, w.row_lora, w.among);
+  if ((rc = check_launch())) return rc;
+  hipLaunchKernelGGL(gated_low_kernel<T>, dim3((unsigned)M, 2), dim3(kThreads), 0, st, (const T*)w.dz, M, g.F, w.row_lora, g.ad, w.low);
+  if ((rc = check_launch())) return rc;
+  const T *Wg = (const T*)g.Wg, *Wu = (const T*)g.Wu;
+  if (g.mx4) {
+    Wg = (const T*)w.W;
+    Wu = Wg + (size_t)g.d * g.F;
+  }
+  if (dX) {
+    hipLaunchKernelGGL(gated_dx_kernel<T>, dim3((unsigned)((g.d + 63) / 64), (unsigned)((M + 63) / 64)), dim3(kThreads), 0, st, (const T*)w.dz, M, g.d,
+                       g.F, Wg, Wu, w.row_lora, g.ad, w.low, (T*)dX);
+    if ((rc = check_launch())) return rc;
+  }
+  if (dA || dB) {
+    GradArgs a{};
+    a.X = g.X; a.dz = w.dz; a.M = M; a.d = g.d; a.F = g.F; a.T = tenants;
+    a.tiles_a = dA ? (g.d + 63) / 64 : 0;
+    a.tiles_b = dB ? (g.F + 63) / 64 : 0;
+    a.chunks = (g.ad.r_max + 31) / 32;
+    a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = w.low; a.t = w.t;
+    a.parts = 1;
+    a.t_part = (size_t)M * g.ad.r_max; a.t_site = a.t_part;
+    a.dA = dA; a.dB = dB;
+    rc = launch_shrink(g.X, g.d, M, g.d, g.dtype, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, st);
+    if (rc) return rc;
+    hipLaunchKernelGGL(gated_grad_kernel<T>, dim3((unsigned)((a.tiles_a + a.tiles_b) * a.chunks), (unsigned)(2 * tenants)), dim3(kThreads), 0, st, a);
+    rc = check_launch();
+  }
+  return rc;
+}
+
+}  // namespace
+
+size_t gated_backward_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
+  return carve_back(nullptr, M, d, F, dtype, mx4, r_max).bytes;
+}
+
+int run_gated_backward(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB,
+                       void* workspace, hipStream_t st) {
+  const BackWs w = carve_back(workspace, g.M, g.d, g.F, g.dtype, g.mx4, g.ad.r_max);
+  if (g.mx4 && dX) {
+    int rc = mx4_dequantize(g.Wg, w.W, MILORA_BF16, g.d, g.F, false, st);
+    if (!rc) rc = mx4_dequantize(g.Wu, (bf16_t*)w.W + (size_t)g.d * g.F, MILORA_BF16, g.d, g.F, false, st);
+    if (rc) return rc;
+  }
+  return g.dtype == MILORA_BF16 ? backward_any<bf16_t>(g, dY, gate, up, dX, dA, dB, w, st) : backward_any<float>(g, dY, gate, up, dX, dA, dB, w, st);
+}
+
+}  // namespace milora

@@ -110,13 +110,14 @@ __device__ __forceinline__ float round_to(float v) {
 
 template <typename T, int MODE, int kFewW, bool FUSED>
 __global__ void __launch_bounds__(kFewW * 64, 4) few_rows_kernel(const FewArgs g) {
-  constexpr int NW = MODE == kFewGateUp ? 2 : 1;
+  constexpr bool kPair = MODE == kFewGateUp || MODE == kFewGated;
+  constexpr int NW = kPair ? 2 : 1;
   __shared__ float red[NW][kFewW][16][17];
   __shared__ float tpart[FUSED ? NW : 1][FUSED ? kFewW : 1][16][kFuseRank];
   __shared__ float ts[FUSED ? NW : 1][16][kFuseRank];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s0 = MODE == kFewGateUp ? 0 : blockIdx.y, n0 = g.col0 + blockIdx.x * 16;
+  const int s0 = kPair ? 0 : blockIdx.y, n0 = g.col0 + blockIdx.x * 16;
   const int d1 = g.d1;
 
   // rank and tenant of row li at the workgroup's site, of its two sites in lanes 0 .. 15 and 16 .. 31 (route byte and tenant id are
@@ -260,6 +261,11 @@ __global__ void __launch_bounds__(kFewW * 64, 4) few_rows_kernel(const FewArgs g
     if (g.Y[0]) Elem<T>::store((T*)g.Y[0], i, h);
   } else if constexpr (MODE == kFewGateUp) {
     Elem<T>::store((T*)g.Y[0], (size_t)m * g.ldy + n, silu(round_to<T>(val[0])) * round_to<T>(val[1]));
+  } else if constexpr (MODE == kFewGated) {
+    const size_t i = (size_t)m * g.d2 + n;
+    if (g.gate_out) g.gate_out[i] = val[0];
+    if (g.up_out) g.up_out[i] = val[1];
+    Elem<T>::store((T*)g.Y[0], (size_t)m * g.ldy + n, silu(val[0]) * val[1]);
   } else {
     const size_t i = (size_t)m * g.d2 + n;
     Elem<T>::store((T*)g.Y[0], i, g.h[i] + round_to<T>(val[0]));
@@ -294,13 +300,13 @@ typedef GenCfg<32, 32, 16> GenSmall;
 typedef GenCfg<64, 64, 32> GenLarge;
 constexpr int kGenLargeTiles = 128;
 
-template <typename T, class C, bool WIDE>
+template <typename T, class C, bool WIDE, typename TO>
 __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restrict__ X, int64_t M, int d1, int d2, int col0,
                                                            const int32_t* __restrict__ row_to_req, const T* __restrict__ W,
                                                            const T* __restrict__ bias, AdapterView ad, int site,
                                                            const int32_t* __restrict__ tenant_id,
                                                            const uint8_t* __restrict__ route, int B,
-                                                           const float* __restrict__ t, T* __restrict__ Y) {
+                                                           const float* __restrict__ t, TO* __restrict__ Y) {
   extern __shared__ __attribute__((aligned(16))) float buf[];
   __shared__ int s_rank[C::BM], s_ten[C::BM], s_most;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
@@ -448,11 +454,11 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
 #pragma unroll
   for (int i = 0; i < C::Outs; ++i) {
     const int64_t m = m0 + r0 + i * kStep;
-    if (m < M && n < d2) Elem<T>::store(Y, (size_t)m * d2 + n, val[i]);
+    if (m < M && n < d2) Elem<TO>::store(Y, (size_t)m * d2 + n, val[i]);
   }
 }
 
-template <typename T, class C, bool WIDE>
+template <typename T, class C, bool WIDE, typename TO>
 int launch_tile(const void* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const void* bias,
                 const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, void* Y,
                 hipStream_t stream) {
@@ -460,15 +466,15 @@ int launch_tile(const void* X, int64_t M, int d1, int d2, const int32_t* row_to_
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)linear_tile_kernel<T, C, WIDE>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
+    MILORA_HIP(hipFuncSetAttribute((const void*)linear_tile_kernel<T, C, WIDE, TO>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
     lds_set_for = dev;
   }
   int rc = MILORA_OK;
   for (int64_t col0 = 0; col0 < d2 && !rc; col0 += kLaunchCols) {
     const int cols = d2 - col0 < kLaunchCols ? (int)(d2 - col0) : kLaunchCols;
     dim3 grid((unsigned)((cols + C::BN - 1) / C::BN), (unsigned)((M + C::BM - 1) / C::BM));
-    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE>), grid, dim3(C::T), C::LdsBytes, stream, (const T*)X, M, d1, d2, (int)col0,
-                       row_to_req, (const T*)W, (const T*)bias, ad, site, tenant_id, route, B, t, (T*)Y);
+    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE, TO>), grid, dim3(C::T), C::LdsBytes, stream, (const T*)X, M, d1, d2, (int)col0,
+                       row_to_req, (const T*)W, (const T*)bias, ad, site, tenant_id, route, B, t, (TO*)Y);
     rc = check_launch();
   }
   return rc;
@@ -498,6 +504,7 @@ static int launch_few_rows_t(FewArgs& g, int sites, int mode, hipStream_t st) {
       case kFewPlain: hipLaunchKernelGGL((few_rows_kernel<T, kFewPlain, W, FUSED>), grid, dim3(W * 64), 0, st, g); break;
       case kFewResid: hipLaunchKernelGGL((few_rows_kernel<T, kFewResid, W, FUSED>), grid, dim3(W * 64), 0, st, g); break;
       case kFewGateUp: hipLaunchKernelGGL((few_rows_kernel<T, kFewGateUp, W, FUSED>), dim3(grid.x), dim3(W * 64), 0, st, g); break;
+      case kFewGated: hipLaunchKernelGGL((few_rows_kernel<T, kFewGated, W, FUSED>), dim3(grid.x), dim3(W * 64), 0, st, g); break;
       default: hipLaunchKernelGGL((few_rows_kernel<T, kFewDown, W, FUSED>), grid, dim3(W * 64), 0, st, g); break;
     }
     rc = check_launch();
@@ -551,6 +558,17 @@ int launch_few_rows(const FewArgs& args, int dtype, int sites, int mode, float* 
   return bf ? launch_few_rows_t<bf16_t, 8, true>(g, sites, mode, st) : launch_few_rows_t<float, 8, true>(g, sites, mode, st);
 }
 
+// Tiles of more than kFewRows rows; t: the shrinks.
+template <typename T, typename TO>
+static int launch_tiles_any(const void* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const void* bias,
+                            const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, void* Y,
+                            hipStream_t stream) {
+  const int64_t large = ((M + 63) / 64) * (int64_t)((d2 + 63) / 64);
+  if (d1 < 4) return launch_tile<T, GenLarge, false, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+  if (large >= kGenLargeTiles) return launch_tile<T, GenLarge, true, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+  return launch_tile<T, GenSmall, true, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+}
+
 int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req,
                           const void* W, const void* bias, const AdapterView& ad, int site,
                           const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y, hipStream_t stream) {
@@ -564,14 +582,17 @@ int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, c
   }
   const int rc = launch_shrink(X, d1, M, d1, dtype, row_to_req, ad, site, 1, tenant_id, route, B, t, stream);
   if (rc) return rc;
-  const int64_t large = ((M + 63) / 64) * (int64_t)((d2 + 63) / 64);
-#define MILORA_TILE(T, C, WIDE) \
-  launch_tile<T, C, WIDE>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream)
-  const bool bf = dtype == MILORA_BF16;
-  if (d1 < 4) return bf ? MILORA_TILE(bf16_t, GenLarge, false) : MILORA_TILE(float, GenLarge, false);
-  if (large >= kGenLargeTiles) return bf ? MILORA_TILE(bf16_t, GenLarge, true) : MILORA_TILE(float, GenLarge, true);
-  return bf ? MILORA_TILE(bf16_t, GenSmall, true) : MILORA_TILE(float, GenSmall, true);
-#undef MILORA_TILE
+  if (dtype == MILORA_BF16)
+    return launch_tiles_any<bf16_t, bf16_t>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+  return launch_tiles_any<float, float>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+}
+
+int launch_linear_f32(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req, const void* W, const AdapterView& ad,
+                      int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, float* Y, hipStream_t stream) {
+  if ((M + 63) / 64 > 65535) return MILORA_ERANGE;
+  if (dtype == MILORA_BF16)
+    return launch_tiles_any<bf16_t, float>(X, M, d1, d2, row_to_req, W, nullptr, ad, site, tenant_id, route, B, t, Y, stream);
+  return launch_tiles_any<float, float>(X, M, d1, d2, row_to_req, W, nullptr, ad, site, tenant_id, route, B, t, Y, stream);
 }
 
 }  // namespace milora

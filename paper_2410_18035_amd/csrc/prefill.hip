@@ -15,6 +15,7 @@
 // out of the stages and added to those rows at the end.
 // Bias is added and the result rounded once at the store.
 #include "shrink.h"
+#include "tiles.h"
 
 namespace milora {
 namespace {
@@ -24,6 +25,7 @@ typedef uint32_t u32x4_a8 __attribute__((ext_vector_type(4), aligned(8)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef __attribute__((address_space(1))) const u32x4_a2 gu32x4_a2;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kTM = 256, kTN = 256, kTK = 64;
 constexpr int kThreadsP = 256;
 constexpr int kBlocksM = kTM / 16, kBlocksN = kTN / 16;
@@ -44,8 +46,12 @@ constexpr int kGroupM = 4;  // consecutive workgroups of an XCD walk 4 row tiles
 struct PParams {
   const bf16_t* X;
   const bf16_t* W;
+  const bf16_t* W2;   // GATED: the up projection (W: the gate)
   const bf16_t* bias;
   bf16_t* Y;
+  float* gate_out;    // GATED: [M][d2] each, or null
+  float* up_out;
+  size_t t_site;      // GATED: floats to the shrinks of the next site
   const float* t;     // `parts` partial shrinks [part][rows of the whole call][r_max], to be added in part order
   size_t t_stride;    // floats from one part to the next
   int parts;
@@ -73,6 +79,9 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
 }
 
+// GATED: the tile's W side is 128 columns of the gate and the same of the up projection, 64 and 64 in each wave's part, so that a
+// lane ends up with both for its outputs: Y = silu(g) u, rounded once.
+template <bool GATED>
 __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -91,7 +100,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const int gsz = p.tilesM - first < kGroupM ? p.tilesM - first : kGroupM;
   const int in_group = id % gspan;
   const int64_t m0 = (int64_t)(first + in_group % gsz) * kTM;
-  const int n0 = in_group / gsz * kTN;
+  const int n0 = in_group / gsz * (GATED ? kTN / 2 : kTN);
 
   const int KT = p.d1 / kTK;
   const uint32_t lds0 = lds_addr(lds);
@@ -99,10 +108,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // copies.  A k step of 64 is brought in two halves: half 0 = X rows 0..127 and W rows 0..127 of the tile,
   // half 1 = the other rows; a half is 8 + 8 blocks of 16 rows, a block two copy instructions of 8 rows each
   // (8 lanes take the 128-byte line of a row, so every request is for whole cache lines).  Waves 0,1 bring
-  // the X blocks of a half (4 each), waves 2,3 the W blocks.  Which 16 bytes of the line a lane takes is
+  // the X blocks of a half (4 each), waves 2,3 the W blocks (GATED: wave 2 the gate's, wave 3 the up projection's).  Which 16 bytes of the line a lane takes is
   // permuted by the row so that the operand reads below spread over all LDS banks.
   const bool is_w = wave >= 2;
-  const unsigned char* src = is_w ? (const unsigned char*)p.W : (const unsigned char*)p.X;
+  const unsigned char* src = is_w ? (const unsigned char*)(GATED && wave == 3 ? p.W2 : p.W) : (const unsigned char*)p.X;
   const int64_t row0 = is_w ? (int64_t)n0 : m0;
   const int64_t rlim = is_w ? (int64_t)p.d2 : p.M;
   uint32_t voff[2][8];
@@ -111,7 +120,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int rr = lane >> 3;
-      int64_t r = row0 + (hh * 8 + (wave & 1) * 4 + (j >> 1)) * 16 + (j & 1) * 8 + rr;
+      const int block = GATED && is_w ? hh * 4 + (j >> 1) : hh * 8 + (wave & 1) * 4 + (j >> 1);
+      int64_t r = row0 + block * 16 + (j & 1) * 8 + rr;
       r = r < rlim ? r : rlim - 1;
       voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((j & 1) * 8 + rr)) * 16u);
     }
@@ -237,18 +247,28 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // t by way of LDS, one step at a time: a call of 777 rows on 4096 x 11008 with a tenant of rank 64 131 us, 120 so, 97 without).
   int* ctl = (int*)(lds + 4 * kHalfBytes);  // ring slots 0 .. 3 hold the operand blocks
   int* const row_ten = ctl + 16;            // tenant of each row of the tile, -1: no LoRA term
-  int my_ten = -1;
+  int my_ten = -1, my_ten2 = -1;  // (of the second site: GATED)
   {
     const int64_t m = m0 + tid;
     if (m < p.M) {
       const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : p.row_base + m;
+      const bool in = req >= 0 && req < p.B;
       int tenant = 0;
-      const int r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
+      int r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
       if (r) my_ten = tenant;
+      if (GATED) {
+        r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + 1, &tenant) : 0;
+        if (r) my_ten2 = tenant;
+      }
     }
   }
-  row_ten[tid] = my_ten;
   if (tid == 0) ctl[1] = 0;  // set: W^B of some tenant of the tile holds Inf or NaN
+#pragma unroll 1
+  for (int s = 0; s < (GATED ? 2 : 1); ++s) {
+  if (GATED && s) my_ten = my_ten2;
+  row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
+  const float* const t_of = p.t + (GATED ? s * p.t_site : 0);
+  const int site = p.site + (GATED ? s : 0);
   int last = -1;
   for (;;) {
     if (tid == 0) ctl[0] = 0x7fffffff;
@@ -264,7 +284,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     const int cur = ctl[0];
     if (cur == 0x7fffffff) break;
     const int r = p.ad.rank[cur];
-    gbf16* Bm = in_global(p.ad.B[cur * MILORA_NUM_SITES + p.site]);
+    gbf16* Bm = in_global(p.ad.B[cur * MILORA_NUM_SITES + site]);
     for (int c0 = 0; c0 < r; c0 += 64) {
       int tb = tid;  // opaque: addresses formed from it stay inside the loop instead of being spilled in front of it
       asm volatile("" : "+v"(tb));
@@ -275,8 +295,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       u32x4 a[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = u32x4{0u, 0u, 0u, 0u};
-      if (wput && n0 + pc * 8 < p.d2) {
-        gbf16* b = Bm + (size_t)cw * p.d2 + n0 + pc * 8;
+      // (GATED: of a wave's 128 columns the first 64 are the gate's; the other projection's stay zero)
+      const int n_piece = n0 + (GATED ? (pc >> 4) * 64 + (pc & 7) * 8 : pc * 8);
+      if (wput && n_piece < p.d2 && (!GATED || ((pc >> 3) & 1) == s)) {
+        gbf16* b = Bm + (size_t)cw * p.d2 + n_piece;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (cw + i < r) a[i] = *(gu32x4_a2*)(b + (size_t)i * p.d2);  // (whole pieces of 8 columns, d2 % 16 == 0, at any alignment)
@@ -294,7 +316,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           for (int i = 0; i < 4; ++i) {
             v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             const int64_t mr = m0 + (tb >> 3) + 32 * (i0 + i);
-            q[i] = p.t + (size_t)(mr < p.M ? mr : p.M - 1) * p.ad.r_max + cq;
+            q[i] = t_of + (size_t)(mr < p.M ? mr : p.M - 1) * p.ad.r_max + cq;
           }
           if (vec) {
             for (int k0 = 0; k0 < p.parts; k0 += 4) {  // four rows and four parts in flight
@@ -367,6 +389,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
     last = cur;
   }
+  }
 
   // ---- bias, one rounding, store: of a 32 x 32 tile a lane holds row l % 32 and, in registers 4 g .. 4 g + 3, the
   // columns 8 g + 4 (l / 32) .. + 3.  By way of the wave's own LDS, so that a store writes whole lines (256 bytes of four rows instead
@@ -378,6 +401,100 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const bool bad = ctl[1] != 0;
   __syncthreads();
   unsigned char* const mine = lds + wave * (128 * kOutPitch);
+  if constexpr (GATED) {
+    // What the stages could not take (products with the tenant's own Inf and NaN) has to be in g and u before the activation: formed
+    // row by row in the wave's LDS, 64 columns at a time, and added.
+    if (bad) {
+#pragma unroll 1
+      for (int s = 0; s < 2; ++s) {
+        for (int row = lane; row < 128; row += 64) {
+          float* const more = (float*)(mine + row * kOutPitch);
+          for (int n = 0; n < 64; ++n) more[n] = 0.f;
+          const int64_t m = m0 + wm * 128 + row;
+          if (m >= p.M) continue;
+          const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : p.row_base + m;
+          int tenant = 0;
+          const int r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + s, &tenant) : 0;
+          for (int c = 0; c < r; ++c) {
+            gbf16* b = in_global(p.ad.B[tenant * MILORA_NUM_SITES + p.site + s]) + (size_t)c * p.d2;
+            float t = 0.f;
+            for (int k = 0; k < p.parts; ++k) t += p.t[s * p.t_site + k * p.t_stride + (size_t)m * p.ad.r_max + c];
+            for (int q = 0; q < 64; ++q) {
+              const int n = n0 + wn * 64 + q;
+              if (n < p.d2 && (b[n] & 0x7f80u) == 0x7f80u) more[q] += t * bf16_to_f32(b[n]);
+            }
+          }
+        }
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if ((j >> 1) == s)
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const f32x4 v = *(const f32x4*)(mine + (i * 32 + (lane & 31)) * kOutPitch + ((j & 1) * 32 + g * 8 + (lane >> 5) * 4) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
+              }
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        asm volatile("" ::: "memory");
+      }
+    }
+    // g and u as they are, for a backward pass: whole lines of four rows a store
+    auto save = [&](int s, float* to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *(f32x4*)(mine + (i * 32 + (lane & 31)) * kOutPitch + (j * 32 + g * 8 + (lane >> 5) * 4) * 4) =
+                f32x4{acc[i][2 * s + j][4 * g], acc[i][2 * s + j][4 * g + 1], acc[i][2 * s + j][4 * g + 2], acc[i][2 * s + j][4 * g + 3]};
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      asm volatile("" ::: "memory");
+      const int n = n0 + wn * 64 + (lane & 15) * 4;
+      const int64_t mw = m0 + wm * 128 + (lane >> 4);
+      const unsigned char* q = mine + (lane >> 4) * kOutPitch + (lane & 15) * 16;
+      if (n < p.d2)
+#pragma unroll 4
+        for (int it = 0; it < 32; ++it)
+          if (mw + it * 4 < p.M)
+            __builtin_nontemporal_store(*(const f32x4*)(q + it * 4 * kOutPitch), (f32x4_a4*)(to + (size_t)(mw + it * 4) * p.d2 + n));
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      asm volatile("" ::: "memory");
+    };
+    if (p.gate_out) save(0, p.gate_out);
+    if (p.up_out) save(1, p.up_out);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x2 v;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            v[h] = pack_bf16x2(silu(acc[i][j][4 * g + 2 * h]) * acc[i][j + 2][4 * g + 2 * h],
+                               silu(acc[i][j][4 * g + 2 * h + 1]) * acc[i][j + 2][4 * g + 2 * h + 1]);
+          *(u32x2*)(mine + (i * 32 + (lane & 31)) * kOutPitch + (j * 32 + g * 8 + (lane >> 5) * 4) * 2) = v;
+        }
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+    const int n = n0 + wn * 64 + (lane & 7) * 8;
+    const int64_t mw = m0 + wm * 128 + (lane >> 3);
+    bf16_t* y = p.Y + (size_t)mw * p.d2 + n;
+    const unsigned char* q = mine + (lane >> 3) * kOutPitch + (lane & 7) * 16;
+    if (n < p.d2)
+#pragma unroll 4
+      for (int it = 0; it < 16; ++it)
+        if (mw + it * 8 < p.M) {
+          const u32x4_a8 v = *(const u32x4*)(q + it * 8 * kOutPitch);
+          __builtin_nontemporal_store(v, (u32x4_a8*)(y + (size_t)(it * 8) * p.d2));
+        }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -480,50 +597,61 @@ bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, 
   return (uint64_t)d2 * (uint64_t)d1 * 2u < (1ull << 32);  // 32-bit byte offsets inside W (X is cut into row slices)
 }
 
-int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const bf16_t* W,
-                          const bf16_t* bias, const AdapterView& ad, int site, const int32_t* tenant_id,
-                          const uint8_t* route, int B, const float* t, bf16_t* Y, hipStream_t stream) {
+template <bool GATED>
+static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t stream) {
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
+    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel<GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
     lds_set_for = dev;
   }
   // rows are independent: slices whose byte offsets inside X fit 32 bits and whose tile count fits a launch
-  int64_t slice = (int64_t)(((1ull << 32) - 1) / ((uint64_t)d1 * 2u)) / kTM * kTM;
-  const int tilesN = (d2 + kTN - 1) / kTN;
+  const PParams all = p;
+  int64_t slice = (int64_t)(((1ull << 32) - 1) / ((uint64_t)p.d1 * 2u)) / kTM * kTM;
+  const int tilesN = (p.d2 + kTN / (GATED ? 2 : 1) - 1) / (kTN / (GATED ? 2 : 1));
   const int64_t by_grid = (int64_t)((1 << 24) / tilesN) * kTM;
   if (slice > by_grid) slice = by_grid;
   if (slice < kTM) return MILORA_EUNSUPPORTED;
   for (int64_t r0 = 0; r0 < M; r0 += slice) {
-    PParams p;
     p.M = M - r0 < slice ? M - r0 : slice;
-    p.X = X + (size_t)r0 * d1;
-    p.W = W;
-    p.bias = bias;
-    p.Y = Y + (size_t)r0 * d2;
-    p.t = t + (size_t)r0 * ad.r_max;
-    p.t_stride = (size_t)M * ad.r_max;
-    p.parts = shrink_parts(M, d1);
-    p.row_to_req = row_to_req ? row_to_req + r0 : nullptr;
-    p.row_base = r0;
-    p.tenant_id = tenant_id;
-    p.route = route;
-    p.ad = ad;
-    p.d1 = d1;
-    p.d2 = d2;
-    p.site = site;
-    p.B = B;
+    p.X = all.X + (size_t)r0 * p.d1;
+    p.Y = all.Y + (size_t)r0 * p.d2;
+    if (GATED && all.gate_out) p.gate_out = all.gate_out + (size_t)r0 * p.d2;
+    if (GATED && all.up_out) p.up_out = all.up_out + (size_t)r0 * p.d2;
+    p.t = all.t + (size_t)r0 * p.ad.r_max;
+    p.row_to_req = all.row_to_req ? all.row_to_req + r0 : nullptr;
+    p.row_base = row_base + r0;
     p.tilesM = (int)((p.M + kTM - 1) / kTM);
     p.tilesN = tilesN;
     const int total = p.tilesM * p.tilesN;
     const int per = (total + 7) / 8;
-    hipLaunchKernelGGL(prefill_kernel, dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
+    hipLaunchKernelGGL(prefill_kernel<GATED>, dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
     const int rc = check_launch();
     if (rc) return rc;
   }
   return MILORA_OK;
+}
+
+int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const bf16_t* W,
+                          const bf16_t* bias, const AdapterView& ad, int site, const int32_t* tenant_id,
+                          const uint8_t* route, int B, const float* t, bf16_t* Y, hipStream_t stream) {
+  PParams p{};
+  p.X = X; p.W = W; p.bias = bias; p.Y = Y; p.t = t;
+  p.t_stride = (size_t)M * ad.r_max;
+  p.parts = shrink_parts(M, d1);
+  p.row_to_req = row_to_req; p.tenant_id = tenant_id; p.route = route; p.ad = ad;
+  p.d1 = d1; p.d2 = d2; p.site = site; p.B = B;
+  return launch_prefill<false>(p, M, 0, stream);
+}
+
+int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
+  PParams p{};
+  p.X = g.X; p.W = g.Wg; p.W2 = g.Wu; p.Y = g.Y; p.gate_out = g.gate_out; p.up_out = g.up_out;
+  p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
+  p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
+  p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
+  return launch_prefill<true>(p, g.M, g.row_base, stream);
 }
 
 // LoRA shrink of the rows the tile kernel serves (same conditions as prefill_supported) at `sites` consecutive sites: t receives

@@ -35,4 +35,30 @@ int routed_linear_tiles(const bf16_t* X, int64_t M, int d1, int d2, const int32_
                         const int2* row_lora, const bf16_t* bias, const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route,
                         int B, const float* t, size_t t_stride, int parts, const TilePlan& pl, int* cnt, float* partial, bf16_t* Y, hipStream_t st);
 
+// The gated block Y = silu(X Wg + its term) * (X Wu + its term): gate and up columns side by side in a tile (plan_tiles and
+// tiles_supported with 2 F columns).  kTiles256: gated_prefill.
+struct GatedTileArgs {
+  const bf16_t* X;
+  int64_t M, row_base;  // rows of the launch, index of the first in the caller's matrix (requests of unmapped rows)
+  int d, F;
+  const int32_t* row_to_req;
+  const bf16_t *Wg, *Wu;
+  bool packed;
+  const int2* row_lora;  // [2][lora_site], or null: the terms by the matrix cores
+  size_t lora_site;
+  AdapterView ad;
+  const int32_t* tenant_id;
+  const uint8_t* route;
+  int B;
+  const float* t;  // [2][part][t_stride]
+  size_t t_stride, t_site;
+  int parts;
+  int* cnt;
+  float* partial;
+  bf16_t* Y;
+  float *gate_out, *up_out;
+};
+int gated_tiles(const GatedTileArgs& g, const TilePlan& pl, hipStream_t st);
+int gated_prefill(const GatedTileArgs& g, hipStream_t st);
+
 }  // namespace milora

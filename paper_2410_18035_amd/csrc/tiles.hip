@@ -34,6 +34,7 @@ typedef uint32_t u32x4_a8 __attribute__((ext_vector_type(4), aligned(8)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef __attribute__((address_space(1))) const u32x4_a2 gu32x4_a2;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kT = 512;        // threads: eight waves
 constexpr int kCtlBytes = 4096;
@@ -64,10 +65,14 @@ typedef TileCfg<128, 128, 2, 2, 2, 4, 1> CfgMid;
 struct TParams {
   const bf16_t* X;
   const bf16_t* W;
+  const bf16_t* W2;  // GATED: the up projection (W: the gate)
   const bf16_t* bias;
   bf16_t* Y;
+  float* gate_out;  // GATED: [M][d2] each, or null
+  float* up_out;
   const float* t;  // partial shrinks [part][M][r_max], to be added in part order
   size_t t_stride;
+  size_t t_site, lora_site;  // GATED: elements to those of the next site
   int parts;
   const int32_t* row_to_req;
   const int32_t* tenant_id;
@@ -92,16 +97,19 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
 }
 
-template <class C, bool PK, bool ROWS>
+template <class C, bool PK, bool ROWS, bool GATED>
 __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  constexpr int kSites = GATED ? 2 : 1;
+  constexpr int kOutN = C::BN / kSites;  // outputs of a row: GATED tiles hold as many columns of the gate and then of the up projection
   int* const row_ten = reinterpret_cast<int*>(lds);   // [BM] tenant of each row of the tile, -1: no LoRA term
   int* const row_rank = row_ten + C::BM;              // [BM]
   int* const row_group = row_rank + C::BM;            // [BM] first rank group of the row's run
   int2* const groups = reinterpret_cast<int2*>(row_group + C::BM);  // [kMaxGroups] tenant, first rank
   int* const ctl = reinterpret_cast<int*>(groups + kMaxGroups);     // 0: arrivals before this one, 1, 2: rows with a LoRA term, kCtlBad
-  int* const row_c0 = row_rank;    // (ROWS) [BM] first rank of the row in this part
-  int* const row_cnt = row_group;  // (ROWS) [BM] ranks of the row in this part
+  // (ROWS) [3][BM] tenant, first rank and ranks of the row in this part; the second site's in place of the groups
+  auto rows_of = [&](int s) __attribute__((always_inline)) { return s == 0 ? row_ten : reinterpret_cast<int*>(groups); };
+  static_assert(C::BM * 12 <= kMaxGroups * 8, "rows of the second site");
   unsigned char* const ring = lds + kCtlBytes;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -118,7 +126,7 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   const int gsz = p.tilesM - first < kGroupM ? p.tilesM - first : kGroupM;
   const int in_group = tile % (kGroupM * p.tilesN);
   const int64_t m0 = (int64_t)(first + in_group % gsz) * C::BM;
-  const int n0 = in_group / gsz * C::BN;
+  const int n0 = in_group / gsz * kOutN;
 
   const int KT = (p.d1 + 63) >> 6;
   const int kt0 = part * p.steps, n_steps = KT - kt0 < p.steps ? KT - kt0 : p.steps;
@@ -126,16 +134,20 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   // ---- copies: instruction i of a stage brings lines 8 i .. 8 i + 7 (X rows first, then W columns) ----
   const size_t row_bytes = (size_t)p.d1 * 2;
   const unsigned char* const xb = (const unsigned char*)p.X + (size_t)m0 * row_bytes;
-  const unsigned char* const wb = (const unsigned char*)p.W + (PK ? (size_t)(n0 >> 4) * (p.d1 >> 5) * 1024 : (size_t)n0 * row_bytes);
+  const size_t w_off = PK ? (size_t)(n0 >> 4) * (p.d1 >> 5) * 1024 : (size_t)n0 * row_bytes;
+  const unsigned char* const wb = (const unsigned char*)p.W + w_off;
+  const unsigned char* const wb2 = GATED ? (const unsigned char*)p.W2 + w_off : wb;
   const int rows = p.M - m0 < C::BM ? (int)(p.M - m0) : C::BM;
-  const int cols = p.d2 - n0 < C::BN ? p.d2 - n0 : C::BN;
+  const int cols = p.d2 - n0 < kOutN ? p.d2 - n0 : kOutN;
   uint32_t voff[C::CPW];
-  bool isw[C::CPW];
+  bool isw[C::CPW], isw2[C::CPW];
 #pragma unroll
   for (int j = 0; j < C::CPW; ++j) {
     const int i = w * C::CPW + j;
     isw[j] = i >= C::BM / 8;
-    const int line = isw[j] ? i - C::BM / 8 : i;
+    int line = isw[j] ? i - C::BM / 8 : i;
+    isw2[j] = GATED && isw[j] && line >= kOutN / 8;
+    if (isw2[j]) line -= kOutN / 8;
     const int rr = lane >> 3;
     if (PK && isw[j]) {
       int blk = line >> 1;
@@ -155,7 +167,7 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
 #pragma unroll
     for (int j = 0; j < C::CPW; ++j) {
       const uint32_t dst = ring0 + slot * C::StageBytes + (w * C::CPW + j) * 1024;
-      const unsigned char* b = isw[j] ? wb + (size_t)kt * (PK ? 2048 : 128) : xb + (size_t)kt * 128;
+      const unsigned char* b = isw[j] ? (isw2[j] ? wb2 : wb) + (size_t)kt * (PK ? 2048 : 128) : xb + (size_t)kt * 128;
       uint32_t v = voff[j];
       if (half) {  // the k past the end are not multiplied: read valid memory in their place
         const int line = isw[j] ? w * C::CPW + j - C::BM / 8 : w * C::CPW + j;
@@ -203,27 +215,34 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   for (int s = 0; s < C::NS - 1; ++s) issue(s, s);
   // which rows carry a LoRA term (looked up while the first stages are on their way)
   const bool with_lora = part == p.S - 1;
+  int ten2 = -1, rank2 = 0;  // (GATED, not ROWS) the second site's, until its turn
   if ((ROWS || with_lora) && tid < C::BM) {
     if constexpr (ROWS) {
-      const int2 ten_rank = tid < rows ? p.row_lora[m0 + tid] : int2{-1, 0};
-      const int r = ten_rank.y;
-      const int ng = (r + 7) >> 3, c0 = part * ng / p.S * 8, c1 = (part + 1) * ng / p.S * 8, cnt = (c1 < r ? c1 : r) - c0;
-      row_ten[tid] = ten_rank.x;
-      row_c0[tid] = c0;
-      row_cnt[tid] = cnt > 0 ? cnt : 0;
-      int most = cnt;
 #pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_xor(most, off, 64);
-        most = o > most ? o : most;
+      for (int s = 0; s < kSites; ++s) {
+        const int2 ten_rank = tid < rows ? p.row_lora[s * p.lora_site + m0 + tid] : int2{-1, 0};
+        const int r = ten_rank.y;
+        const int ng = (r + 7) >> 3, c0 = part * ng / p.S * 8, c1 = (part + 1) * ng / p.S * 8, cnt = (c1 < r ? c1 : r) - c0;
+        int* const rs = rows_of(s);
+        rs[tid] = ten_rank.x;
+        rs[C::BM + tid] = c0;
+        rs[2 * C::BM + tid] = cnt > 0 ? cnt : 0;
+        int most = cnt;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const int o = __shfl_xor(most, off, 64);
+          most = o > most ? o : most;
+        }
+        if (lane == 0) ctl[1 + 2 * s + w] = most;
       }
-      if (lane == 0) ctl[1 + w] = most;
     } else {
       int tenant = -1, r = 0;
       if (tid < rows) {
         const int64_t m = m0 + tid;
         const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : m;
-        r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
+        const bool in = req >= 0 && req < p.B;
+        r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
+        if (GATED && in) rank2 = routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + 1, &ten2);
       }
       row_ten[tid] = r ? tenant : -1;
       row_rank[tid] = r;
@@ -258,10 +277,29 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   // Consecutive rows of one tenant are a run; a run's ranks get groups of their own, in which the other rows of the tile are
   // zero, so tenants share stages.
   bool lora = false;
-  if (!ROWS && with_lora)
+  if constexpr (!ROWS)
+#pragma unroll 1
+  for (int s = 0; s < kSites; ++s) {
+    if (!with_lora) break;
+    if (s > 0) {  // (the first site's rows are no longer read)
+      if (tid < C::BM) {
+        row_ten[tid] = rank2 ? ten2 : -1;
+        row_rank[tid] = rank2;
+        const unsigned long long any = __ballot(rank2 > 0);
+        if (lane == 0) ctl[1 + w] = any != 0;
+      }
+      __syncthreads();
+    }
+    bool any = false;
 #pragma unroll
-    for (int i = 0; i < C::BM / 64; ++i) lora = lora || ctl[1 + i];
-  if (lora) {
+    for (int i = 0; i < C::BM / 64; ++i) any = any || ctl[1 + i];
+    lora = lora || any;
+    if (!any) {
+      if (GATED) __syncthreads();
+      continue;
+    }
+    const float* const t_of = p.t + (GATED ? s * p.t_site : 0);
+    const int site = p.site + (GATED ? s : 0);
     int n_groups = 0;
     for (int g0 = 0;; g0 += kMaxGroups) {
       if (w == 0) {  // list groups g0 .. g0 + kMaxGroups - 1
@@ -305,7 +343,7 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
         const bool tvec = (p.ad.r_max & 3) == 0;
         constexpr int kFly = C::OCC == 1 ? 4 : 2;  // parts in flight: registers of half a compute unit allow two
         auto ask_t = [&](int c0, int k0, f32x4 (&v)[2][kFly]) __attribute__((always_inline)) {  // parts k0 .. of ranks c0 .. c0 + 7 of row xr
-          const float* tp = p.t + (size_t)(m0 + xr) * p.ad.r_max + c0;
+          const float* tp = t_of + (size_t)(m0 + xr) * p.ad.r_max + c0;
 #pragma unroll
           for (int k = 0; k < kFly; ++k)
 #pragma unroll
@@ -327,7 +365,7 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
               add_t(k0, v, tv);
             }
           } else {
-            const float* tp = p.t + (size_t)(m0 + xr) * p.ad.r_max + c0;
+            const float* tp = t_of + (size_t)(m0 + xr) * p.ad.r_max + c0;
             for (int e = 0; e < 8; ++e)
               if (c0 + e < my_rank)
                 for (int k = 0; k < p.parts; ++k) tv[e] += tp[k * p.t_stride + e];
@@ -379,10 +417,11 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
         };
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = u32x4{0u, 0u, 0u, 0u};
-        if (wput && s0 + wg < g1 && wc < cols) {
+        // (GATED: columns of the other projection stay zero)
+        if (wput && s0 + wg < g1 && wc % kOutN < cols && (!GATED || wc / kOutN == s)) {
           const int2 gr = groups[s0 + wg - g0];
           const int r = p.ad.rank[gr.x];
-          gbf16* b = in_global(p.ad.B[gr.x * MILORA_NUM_SITES + p.site]) + n0 + wc;
+          gbf16* b = in_global(p.ad.B[gr.x * MILORA_NUM_SITES + site]) + n0 + wc % kOutN;
           // (whole pieces of 8 columns, d2 % 16 == 0, at whatever alignment the adapter has: one load each)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -469,9 +508,17 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   // its own: 64 packed rows, rank 64, 4096 x 4096: 143 us a call with the term as matrix stages, 56 us so (37 since the shrink in
   // front has more workgroups).  A tile of one tenant reads its W^B again for each row: 300 rows of 4 tenants, rank 64, 4096 x
   // 11008: 77 -> 90 us.
+  const int my_site = GATED ? cg / (kGroups / 2) : 0;              // of this thread's columns
+  const int my_col = GATED ? cg % (kGroups / 2) * 8 : cg * 8;      // first of them, from n0 on
   if constexpr (ROWS) {
-    int most = ctl[1];
-    if (C::BM > 64) most = ctl[2] > most ? ctl[2] : most;
+#pragma unroll 1
+   for (int s = 0; s < kSites; ++s) {
+    int most = ctl[1 + 2 * s];
+    if (C::BM > 64) most = ctl[2 + 2 * s] > most ? ctl[2 + 2 * s] : most;
+    const int* const rs_ten = rows_of(s);
+    const int *const row_c0 = rs_ten + C::BM, *const row_cnt = rs_ten + 2 * C::BM;
+    const float* const t_of = p.t + (GATED ? s * p.t_site : 0);
+    const int site = p.site + (GATED ? s : 0);
     if (most > 0) {
       constexpr int kU = C::Items == 1 ? 16 : 8;
       float* const ts = reinterpret_cast<float*>(ring);  // [BM][kTs]: rows 16 bytes past a multiple of all banks
@@ -479,10 +526,10 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
       int cnt[C::Items], ranks = 0;
 #pragma unroll
       for (int it = 0; it < C::Items; ++it) {
-        cnt[it] = cg * 8 < cols ? row_cnt[r0 + it * kRowStep] : 0;
+        cnt[it] = my_col < cols && (!GATED || my_site == s) ? row_cnt[r0 + it * kRowStep] : 0;
         const int row = r0 + it * kRowStep;
         bp[it] = in_global(p.W);  // (no rank: any valid 16 bytes)
-        if (cnt[it] > 0) bp[it] = in_global(p.ad.B[row_ten[row] * MILORA_NUM_SITES + p.site]) + (size_t)row_c0[row] * p.d2 + n0 + cg * 8;
+        if (cnt[it] > 0) bp[it] = in_global(p.ad.B[rs_ten[row] * MILORA_NUM_SITES + site]) + (size_t)row_c0[row] * p.d2 + n0 + my_col;
         ranks = cnt[it] > ranks ? cnt[it] : ranks;
       }
       __syncthreads();  // the sums are read
@@ -491,7 +538,7 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
         const int row = e / pieces, c = (e - row * pieces) * 4, left = row_cnt[row] - c;
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
         if (left > 0) {
-          const float* const tp = p.t + (size_t)(m0 + row) * p.ad.r_max + row_c0[row] + c;
+          const float* const tp = t_of + (size_t)(m0 + row) * p.ad.r_max + row_c0[row] + c;
           if ((p.ad.r_max & 3) == 0) {
             for (int k0 = 0; k0 < p.parts; k0 += 4) {
               f32x4 x[4];
@@ -536,18 +583,25 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
           }
       }
     }
+   }
   }
 
   // ---- what the stages could not take: products with the tenant's own Inf and NaN ----
-  if (!ROWS && lora && ctl[kCtlBad] && cg * 8 < cols) {
+  if (!ROWS && lora && ctl[kCtlBad] && my_col < cols) {
 #pragma unroll
     for (int it = 0; it < C::Items; ++it) {
-      const int row = r0 + it * kRowStep, ten = row_ten[row], r = ten >= 0 ? row_rank[row] : 0;
+      const int row = r0 + it * kRowStep;
+      int ten = row_ten[row], r = ten >= 0 ? row_rank[row] : 0;
+      if (GATED && my_site == 0) {  // (the rows in LDS are the second site's)
+        const int64_t m = m0 + row, req = m < p.M ? (p.row_to_req ? (int64_t)p.row_to_req[m] : m) : -1;
+        r = req >= 0 && req < p.B ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &ten) : 0;
+      }
+      const float* const t_of = p.t + (GATED ? my_site * p.t_site : 0);
       for (int c = 0; c < r; ++c) {
-        const u32x4 b = *(gu32x4_a2*)(in_global(p.ad.B[ten * MILORA_NUM_SITES + p.site]) + (size_t)c * p.d2 + n0 + cg * 8);
+        const u32x4 b = *(gu32x4_a2*)(in_global(p.ad.B[ten * MILORA_NUM_SITES + p.site + my_site]) + (size_t)c * p.d2 + n0 + my_col);
         if (!(nonfinite2(b[0]) | nonfinite2(b[1]) | nonfinite2(b[2]) | nonfinite2(b[3]))) continue;
         float t = 0.f;
-        for (int k = 0; k < p.parts; ++k) t += p.t[k * p.t_stride + (size_t)(m0 + row) * p.ad.r_max + c];
+        for (int k = 0; k < p.parts; ++k) t += t_of[k * p.t_stride + (size_t)(m0 + row) * p.ad.r_max + c];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t bad = nonfinite2(b[e]);
@@ -601,6 +655,37 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
     }
   }
 
+  // ---- GATED: a thread of the gate takes its partner's columns of the up projection; g and u stay in fp32 ----
+  if constexpr (GATED) {
+#pragma unroll
+    for (int it = 0; it < C::Items; ++it) {
+      const int r = r0 + it * kRowStep;
+      f32x4 up[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) up[h][e] = __shfl_xor(val[it][h][e], kGroups / 2, 64);
+      if (my_col >= cols || r >= rows) continue;
+      const size_t at = (size_t)(m0 + r) * p.d2 + n0 + my_col;
+      float* const save = my_site ? p.up_out : p.gate_out;
+      if (save) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4_a4*>(save + at + h * 4) = val[it][h];
+      }
+      if (my_site == 0) {
+        u32x4_a8 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 g = val[it][e >> 1], u = up[e >> 1];
+          const int k = 2 * (e & 1);
+          o[e] = pack_bf16x2(silu(g[k]) * u[k], silu(g[k + 1]) * u[k + 1]);
+        }
+        *reinterpret_cast<u32x4_a8*>(p.Y + at) = o;
+      }
+    }
+    return;
+  }
+
   // ---- bias, one rounding, stores ----
   if (cg * 8 >= cols) return;
   const int n = n0 + cg * 8;
@@ -619,17 +704,17 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
   }
 }
 
-template <class C, bool PK, bool ROWS>
+template <class C, bool PK, bool ROWS, bool GATED>
 int launch_tiles(const TParams& p, hipStream_t st) {
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)tile_kernel<C, PK, ROWS>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
+    MILORA_HIP(hipFuncSetAttribute((const void*)tile_kernel<C, PK, ROWS, GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
     lds_set_for = dev;
   }
   const int total = p.tilesM * p.tilesN * p.S;
-  hipLaunchKernelGGL((tile_kernel<C, PK, ROWS>), dim3(8 * ((total + 7) / 8)), dim3(kT), C::LdsBytes, st, p);
+  hipLaunchKernelGGL((tile_kernel<C, PK, ROWS, GATED>), dim3(8 * ((total + 7) / 8)), dim3(kT), C::LdsBytes, st, p);
   return check_launch();
 }
 
@@ -697,19 +782,40 @@ bool tiles_supported(int64_t M, int d1, int d2, bool packed, const void* X, cons
   return (uint64_t)d1 * 128u * 2u < (1ull << 31);  // byte offsets inside a tile's lines
 }
 
+static void fill_plan(TParams* p, const TilePlan& pl) {
+  p->tilesM = pl.tilesM; p->tilesN = pl.tilesN; p->S = pl.S; p->steps = pl.steps;
+}
+
+template <bool GATED>
+static int launch_any_tiles(const TParams& p, int shape, bool packed, hipStream_t st) {
+  const bool mid = shape == kTiles128;
+  static_assert(kMaxSplitUnits <= kShrinkClear, "counters the shrink zeroes");
+  if (packed) return mid ? launch_tiles<CfgMid, true, true, GATED>(p, st) : launch_tiles<CfgSmall, true, true, GATED>(p, st);
+  if (p.row_lora) return mid ? launch_tiles<CfgMid, false, true, GATED>(p, st) : launch_tiles<CfgSmall, false, true, GATED>(p, st);
+  return mid ? launch_tiles<CfgMid, false, false, GATED>(p, st) : launch_tiles<CfgSmall, false, false, GATED>(p, st);
+}
+
 int routed_linear_tiles(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const bf16_t* W, bool packed,
                         const int2* row_lora, const bf16_t* bias, const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route,
                         int B, const float* t, size_t t_stride, int parts, const TilePlan& pl, int* cnt, float* partial, bf16_t* Y, hipStream_t st) {
-  TParams p;
+  TParams p{};
   p.X = X; p.W = W; p.bias = bias; p.Y = Y; p.t = t; p.t_stride = t_stride; p.parts = parts;
   p.row_to_req = row_to_req; p.tenant_id = tenant_id; p.route = route; p.ad = ad; p.M = M; p.row_lora = row_lora; p.d1 = d1; p.d2 = d2;
-  p.site = site; p.B = B; p.tilesM = pl.tilesM; p.tilesN = pl.tilesN; p.S = pl.S; p.steps = pl.steps;
+  p.site = site; p.B = B;
   p.partial = partial; p.cnt = cnt;
-  const bool mid = pl.shape == kTiles128;
-  static_assert(kMaxSplitUnits <= kShrinkClear, "counters the shrink zeroes");
-  if (packed) return mid ? launch_tiles<CfgMid, true, true>(p, st) : launch_tiles<CfgSmall, true, true>(p, st);
-  if (row_lora) return mid ? launch_tiles<CfgMid, false, true>(p, st) : launch_tiles<CfgSmall, false, true>(p, st);
-  return mid ? launch_tiles<CfgMid, false, false>(p, st) : launch_tiles<CfgSmall, false, false>(p, st);
+  fill_plan(&p, pl);
+  return launch_any_tiles<false>(p, pl.shape, packed, st);
+}
+
+int gated_tiles(const GatedTileArgs& g, const TilePlan& pl, hipStream_t st) {
+  TParams p{};
+  p.X = g.X; p.W = g.Wg; p.W2 = g.Wu; p.Y = g.Y; p.gate_out = g.gate_out; p.up_out = g.up_out;
+  p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.lora_site = g.lora_site; p.parts = g.parts;
+  p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad; p.M = g.M; p.row_lora = g.row_lora;
+  p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
+  p.partial = g.partial; p.cnt = g.cnt;
+  fill_plan(&p, pl);
+  return launch_any_tiles<true>(p, pl.shape, g.packed, st);
 }
 
 }  // namespace milora
