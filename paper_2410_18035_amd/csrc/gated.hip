@@ -16,12 +16,18 @@ namespace milora {
 bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, const void* Y);
 int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
                         const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream);
+int launch_low_sites(const bf16_t* dz, int64_t M, int F, const int32_t* row_to_req, const AdapterView& ad, const int32_t* tenant_id,
+                     const uint8_t* route, int B, float* low, hipStream_t stream);
 
 namespace {
 
 constexpr int kGate = 4;  // site; the up projection's is the next
 constexpr int kThreads = 256;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+static_assert(kThreads * 8 == 2048, "columns of gated_dz8_kernel");
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -209,6 +215,39 @@ __global__ void __launch_bounds__(kThreads) gated_dz_kernel(const T* __restrict_
   }
 }
 
+// The same eight columns a thread (bf16, F % 8 == 0, 16-byte aligned): bound by HBM, 14 bytes an element.
+__global__ void __launch_bounds__(kThreads) gated_dz8_kernel(const bf16_t* __restrict__ dy, const float* __restrict__ g, const float* __restrict__ u,
+                                                             int F, int pieces, bf16_t* __restrict__ dz) {
+  const int64_t m = blockIdx.x / pieces;
+  const int j = blockIdx.x % pieces * kDzCols + threadIdx.x * 8;
+  if (j >= F) return;
+  const int64_t i = m * F + j;
+  const u32x4 y = *(const u32x4*)(dy + i);
+  f32x4 gv[2], uv[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    gv[h] = __builtin_nontemporal_load((const f32x4*)(g + i) + h);
+    uv[h] = __builtin_nontemporal_load((const f32x4*)(u + i) + h);
+  }
+  u32x4 dg, du;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float a[2], b[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float yv = __uint_as_float(k ? y[e] & 0xffff0000u : y[e] << 16), x = gv[e >> 1][2 * (e & 1) + k], v = uv[e >> 1][2 * (e & 1) + k];
+      const float s = 1.f / (1.f + __expf(-x));
+      a[k] = yv * v * s * (1.f + x * (1.f - s));
+      b[k] = yv * x * s;
+    }
+    dg[e] = pack_bf16x2(a[0], a[1]);
+    du[e] = pack_bf16x2(b[0], b[1]);
+  }
+  bf16_t* const row = dz + m * 2 * F;
+  *(u32x4*)(row + j) = dg;
+  *(u32x4*)(row + F + j) = du;
+}
+
 template <typename T>
 int launch_dz(const void* dY, const float* gate, const float* up, int64_t M, int F, void* dz, hipStream_t st) {
   const int pieces = (F + kDzCols - 1) / kDzCols;
@@ -217,7 +256,11 @@ int launch_dz(const void* dY, const float* gate, const float* up, int64_t M, int
   int rc = MILORA_OK;
   for (int64_t m = 0; m < M && !rc; m += slice) {
     const int64_t rows = M - m < slice ? M - m : slice;
-    hipLaunchKernelGGL(gated_dz_kernel<T>, dim3((unsigned)(rows * pieces)), dim3(kThreads), 0, st, (const T*)dY + m * F, gate + m * F, up + m * F, F,
+    if (sizeof(T) == 2 && F % 8 == 0 && aligned16(dY) && aligned16(gate) && aligned16(up))
+      hipLaunchKernelGGL(gated_dz8_kernel, dim3((unsigned)(rows * pieces)), dim3(kThreads), 0, st, (const bf16_t*)dY + m * F, gate + m * F, up + m * F, F,
+                         pieces, (bf16_t*)dz + m * 2 * F);
+    else
+      hipLaunchKernelGGL(gated_dz_kernel<T>, dim3((unsigned)(rows * pieces)), dim3(kThreads), 0, st, (const T*)dY + m * F, gate + m * F, up + m * F, F,
                        pieces, (T*)dz + m * 2 * F);
     rc = check_launch();
   }
@@ -424,6 +467,183 @@ __global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) 
   }
 }
 
+// ---- the same on the bf16 matrix cores -------------------------------------------------------------------------------------
+// The scales of a rank (low, x A: fp32) as two bf16 halves, about 17 of their bits: line [chunk of 32 ranks][m] of 64 values, 32 high and 32 low
+// halves, zero past the rank and for rows without a term.
+__global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __restrict__ v, size_t part, int parts, int64_t M, int r_max,
+                                                                const int2* __restrict__ row_lora, bf16_t* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);  // a row
+  if (i >= M) return;
+  const int c = blockIdx.y * 32 + (threadIdx.x & 31);
+  const int r = row_lora[i].y;
+  float x = 0.f;
+  if (c < r)
+    for (int p = 0; p < parts; ++p) x += v[p * part + (size_t)i * r_max + c];
+  const bf16_t hi = f32_to_bf16(x);
+  bf16_t* const line = out + ((size_t)blockIdx.y * M + i) * 64 + (threadIdx.x & 31);
+  line[0] = hi;
+  line[32] = f32_to_bf16(x - bf16_to_f32(hi));
+}
+
+// out[col][c] = sum over the tenant's rows of P[m][col] s[m][c]: a workgroup of eight waves takes 64 columns and 32 ranks of one of a
+// tenant's matrices, a wave every eighth 64 rows of the call.  A wave lists the tenant's rows among its own and takes 32 of them at a time: their 128 bytes
+// of P and of s go through registers (the next 32 rows' are on their way while these are multiplied) into the wave's LDS, and the
+// transposing read makes operands of both.  The waves' sums meet in LDS at the end.  Bound: the reads of P (HBM) and s (L2).
+constexpr int kGradW = 8;
+struct GradTileArgs {
+  const bf16_t *X, *dz;
+  int64_t M;
+  int d, F, tiles_a, tiles_b;  // tiles of 64 columns
+  const int2 *row_lora, *among;
+  AdapterView ad;
+  const bf16_t *low, *t;  // halves, [site][chunk][M][64]
+  size_t half_site;
+  void* const* dA;
+  void* const* dB;
+};
+// 16-column pieces (32 bytes) of a 128-byte row k: permuted so that four rows of two pieces, which half a wave reads at once, hit all banks
+__device__ __forceinline__ int grad_swz(int k) { return ((k >> 1) & 1) * 2; }
+
+__global__ void __launch_bounds__(kGradW * 64, 4) gated_grad_tile_kernel(const GradTileArgs g) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kGradW * 8192];
+  __shared__ int lists[kGradW][128];
+  __shared__ int span[2];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = g.tiles_a + g.tiles_b, tile = blockIdx.x % tiles, chunk = blockIdx.x / tiles, c0 = chunk * 32;
+  const int s = blockIdx.y & 1, ten = blockIdx.y >> 1;
+  const bool is_b = tile >= g.tiles_a;
+  void* const* const table = is_b ? g.dB : g.dA;
+  bf16_t* const out = table ? (bf16_t*)table[ten * MILORA_NUM_SITES + kGate + s] : nullptr;
+  const int r = g.ad.rank[ten];
+  if (!out || r < 1 || r > g.ad.r_max || c0 >= r) return;
+  const int cols = is_b ? g.F : g.d, n0 = (is_b ? tile - g.tiles_a : tile) * 64;
+  const bf16_t* const P = is_b ? g.dz + (int64_t)s * g.F : g.X;
+  const int64_t ldp = is_b ? 2 * (int64_t)g.F : g.d;
+  const bf16_t* const sc = (is_b ? g.t : g.low) + s * g.half_site + (size_t)chunk * g.M * 64;
+  const int blocks = (int)((g.M + 63) / 64);
+  if (tid == 0) { span[0] = blocks; span[1] = 0; }
+  __syncthreads();
+  {
+    int first = blocks, end = 0;
+    for (int i = tid; i < blocks; i += kGradW * 64) {
+      const int2 a = g.among[(size_t)s * blocks + i];
+      if (ten < a.x || ten > a.y) continue;
+      first = first < i ? first : i;
+      end = i + 1;
+    }
+    if (first < end) {
+      atomicMin(&span[0], first);
+      atomicMax(&span[1], end);
+    }
+  }
+  __syncthreads();
+  const int b_end = span[1];
+  int blk = span[0] + w;
+  int* const list = lists[w];
+  unsigned char* const mine = lds + w * 8192;
+  const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)mine;
+  f32x16 acc[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+
+  // rows 8 it + lane / 8 of 32, piece lane % 8 of 16 bytes
+  const int piece = lane & 7;
+  const bool p_in = n0 + piece * 8 < cols;  // (cols % 16 == 0)
+  u32x4 pv[4], sv[4];
+  auto ask = [&](int n) __attribute__((always_inline)) {  // the first n of the list
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int k = it * 8 + (lane >> 3);
+      pv[it] = sv[it] = u32x4{0u, 0u, 0u, 0u};
+      if (k < n) {
+        const int64_t m = list[k];
+        if (p_in) pv[it] = *(const u32x4*)(P + m * ldp + n0 + piece * 8);
+        sv[it] = *(const u32x4*)(sc + m * 64 + piece * 8);
+      }
+    }
+  };
+  int have = 0;
+  // fills the list up to 32 rows or the end; the rows asked for before leave it
+  auto next = [&](int drop) __attribute__((always_inline)) {
+    if (drop) {
+      const int keep = drop + lane < have ? list[drop + lane] : 0;
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      asm volatile("" ::: "memory");
+      if (drop + lane < have) list[lane] = keep;
+      have -= drop;
+    }
+    while (have < 32 && blk < b_end) {
+      const int64_t m = (int64_t)blk * 64 + lane;
+      const bool ours = m < g.M && g.row_lora[s * g.M + m].x == ten;
+      const unsigned long long votes = __ballot(ours);
+      if (ours) list[have + __popcll(votes & ((1ull << lane) - 1))] = (int)m;
+      have += __popcll(votes);
+      blk += kGradW;
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+    return have < 32 ? have : 32;
+  };
+  const int k_of = (lane >> 5) * 8 + ((lane & 15) >> 2), col_half = (lane >> 4) & 1;
+  auto read_tr = [&](uint32_t base, int ks, int pair) __attribute__((always_inline)) {  // rows 16 ks + 8 (l / 32) .., pieces 2 pair, 2 pair + 1
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    s16x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = ks * 16 + k_of + 4 * h;
+      v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(base + k * 128 + ((2 * pair + col_half) ^ grad_swz(k)) * 32 + (lane & 3) * 8));
+    }
+    return __builtin_bit_cast(bf16x8, v);
+  };
+  int n = next(0);
+  if (n) ask(n);
+  while (n) {
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int k = it * 8 + (lane >> 3);
+      unsigned char* const at = mine + k * 128 + ((piece >> 1) ^ grad_swz(k)) * 32 + (piece & 1) * 16;
+      *(u32x4*)at = pv[it];
+      *(u32x4*)(at + 4096) = sv[it];
+    }
+    const int left = next(n);
+    if (left) ask(left);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // the wave's own LDS writes
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 hi = read_tr(mine_at + 4096, ks, 0), lo = read_tr(mine_at + 4096, ks, 1);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const bf16x8 p = read_tr(mine_at, ks, j);
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, p, acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, p, acc[j], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+    n = left;
+  }
+  // (lane: column l % 32, registers 4 q .. + 3: ranks 8 q + 4 (l / 32) ..)
+  __syncthreads();
+  float* const sums = (float*)lds;  // [wave][rank][64 columns]
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[(w * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3)) * 64 + j * 32 + (lane & 31)] = acc[j][e];
+  __syncthreads();
+  for (int e = tid; e < 32 * 64; e += kGradW * 64) {
+    // dB: columns next to one another are next to one another in memory; dA: ranks
+    const int c = is_b ? e >> 6 : e & 31, col = is_b ? e & 63 : e >> 5;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGradW; ++k) v += sums[(k * 32 + c) * 64 + col];
+    if (c0 + c < r && n0 + col < cols) out[is_b ? (size_t)(c0 + c) * g.F + n0 + col : (size_t)(n0 + col) * r + c0 + c] = f32_to_bf16(v);
+  }
+}
+
 struct BackWs {
   void* dz;        // [M][2 F] dtype
   float* low;      // [2][M][r_max]
@@ -431,18 +651,24 @@ struct BackWs {
   int2* row_lora;  // [2][M]
   int2* among;     // [2][M / 64]
   void* W;         // 4-bit weights in bf16
+  bf16_t* halves;  // bf16 shapes of the matrix cores: [low, t][site][chunk][M][64]
+  float* partial;
   size_t bytes;
 };
+
 
 BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
   Carver c{(char*)base};
   BackWs w;
   w.dz = c.take<char>((size_t)M * F * 2 * dtype_size(dtype));
-  w.low = c.take<float>((size_t)M * r_max * 2);
+  w.low = c.take<float>(shrink_rows_bound(M, F) * r_max * 2);
   w.t = c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
   w.row_lora = c.take<int2>((size_t)M * 2);
   w.among = c.take<int2>((size_t)((M + 63) / 64) * 2);
   w.W = c.take<bf16_t>(mx4 ? (size_t)d * F * 2 : 0);
+  const bool tiles = dtype == MILORA_BF16;  // (whatever the other sizes: none may go down when one goes up)
+  w.halves = c.take<bf16_t>(tiles ? (size_t)((r_max + 31) / 32) * M * 64 * 4 : 0);
+  w.partial = c.take<float>(tiles ? back_partial_floats(M, d, F) : 0);
   w.bytes = c.off;
   return w;
 }
@@ -488,6 +714,55 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   return rc;
 }
 
+// bf16 of whole 64 of F and 32 of d, 16-byte aligned: everything on the bf16 matrix cores.
+int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB, const BackWs& w,
+                   hipStream_t st) {
+  const int64_t M = g.M;
+  const int tenants = g.ad.n_tenants, r_max = g.ad.r_max;
+  const bf16_t* const dz = (const bf16_t*)w.dz;
+  int rc = launch_dz<bf16_t>(dY, gate, up, M, g.F, w.dz, st);
+  if (!rc) rc = launch_low_sites(dz, M, g.F, g.row_to_req, g.ad, g.tenant_id, g.route, g.B, w.low, st);
+  if (rc) return rc;
+  const int low_parts = shrink_parts(M, g.F);
+  const size_t row_floats = (size_t)M * r_max;
+  if (dX) {
+    GatedBackArgs a{};
+    a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
+    a.Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
+    a.Wu = g.mx4 ? (const bf16_t*)w.W + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
+    a.low = w.low; a.low_stride = row_floats; a.low_site = row_floats * low_parts; a.parts = low_parts;
+    a.partial = w.partial; a.dX = (bf16_t*)dX;
+    if ((rc = gated_dx_tiles(a, st))) return rc;
+  }
+  if (!dA && !dB) return rc;
+  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
+                     g.route, g.B, w.row_lora, w.among);
+  if ((rc = check_launch())) return rc;
+  const int chunks = (r_max + 31) / 32;
+  const size_t half_site = (size_t)chunks * M * 64;
+  bf16_t* const halves[2] = {w.halves, w.halves + 2 * half_site};  // of low, of t
+  const int t_parts = shrink_parts(M, g.d);
+  if (dB && (rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st)))
+    return rc;
+  for (int k = 0; k < 2; ++k) {
+    if (!(k ? dB : dA)) continue;
+    const int parts = k ? t_parts : low_parts;
+    for (int s = 0; s < 2 && !rc; ++s) {
+      hipLaunchKernelGGL(gated_halves_kernel, dim3((unsigned)((M + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)chunks), dim3(kThreads), 0, st,
+                         (k ? w.t : w.low) + s * row_floats * parts, row_floats, parts, M, r_max, w.row_lora + s * M, halves[k] + s * half_site);
+      rc = check_launch();
+    }
+    if (rc) return rc;
+  }
+  GradTileArgs a{};
+  a.X = (const bf16_t*)g.X; a.dz = dz; a.M = M; a.d = g.d; a.F = g.F;
+  a.tiles_a = dA ? (g.d + 63) / 64 : 0;
+  a.tiles_b = dB ? (g.F + 63) / 64 : 0;
+  a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = halves[0]; a.t = halves[1]; a.half_site = half_site; a.dA = dA; a.dB = dB;
+  hipLaunchKernelGGL(gated_grad_tile_kernel, dim3((unsigned)((a.tiles_a + a.tiles_b) * chunks), (unsigned)(2 * tenants)), dim3(kGradW * 64), 0, st, a);
+  return check_launch();
+}
+
 }  // namespace
 
 size_t gated_backward_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
@@ -502,6 +777,11 @@ int run_gated_backward(const GatedCall& g, const void* dY, const float* gate, co
     if (!rc) rc = mx4_dequantize(g.Wu, (bf16_t*)w.W + (size_t)g.d * g.F, MILORA_BF16, g.d, g.F, false, st);
     if (rc) return rc;
   }
+  const bf16_t* const Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
+  const bf16_t* const Wu = g.mx4 ? Wg + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
+  if (g.dtype == MILORA_BF16 && g.d % 32 == 0 && aligned16(g.X) && g.M <= (int64_t)65535 * 64 && g.ad.n_tenants <= 32767 &&
+      back_supported(g.M, g.d, g.F, w.dz, Wg, Wu, dX))
+    return backward_tiles(g, dY, gate, up, dX, dA, dB, w, st);
   return g.dtype == MILORA_BF16 ? backward_any<bf16_t>(g, dY, gate, up, dX, dA, dB, w, st) : backward_any<float>(g, dY, gate, up, dX, dA, dB, w, st);
 }
 

@@ -14,6 +14,8 @@
 // (hi + lo, about 17 of its 24 bits) against W^B of the tenant, masked to that tenant's rows; Inf and NaN of W^B are kept
 // out of the stages and added to those rows at the end.
 // Bias is added and the result rounded once at the store.
+#include <type_traits>
+
 #include "shrink.h"
 #include "tiles.h"
 
@@ -43,15 +45,19 @@ constexpr int kCopyAStride = 2, kCopyB0 = 16, kCopyBStride = 3;
 static_assert(kCopyB0 >= 16 && 7 * kCopyAStride < kCopyB0 && kCopyB0 + 7 * kCopyBStride < 64, "copy positions");
 constexpr int kGroupM = 4;  // consecutive workgroups of an XCD walk 4 row tiles of one column tile
 
+enum PMode { kPlain, kGated, kBack };
 struct PParams {
   const bf16_t* X;
   const bf16_t* W;
-  const bf16_t* W2;   // GATED: the up projection (W: the gate)
+  const bf16_t* W2;   // kGated, kBack: the up projection (W: the gate)
   const bf16_t* bias;
   bf16_t* Y;
-  float* gate_out;    // GATED: [M][d2] each, or null
+  float* gate_out;    // kGated: [M][d2] each, or null
   float* up_out;
-  size_t t_site;      // GATED: floats to the shrinks of the next site
+  size_t t_site;      // kGated, kBack: floats to the shrinks of the next site
+  float* partial;     // kBack, S > 1: [part][M][d2] sums of the parts of the reduction
+  size_t partial_stride;
+  int S, steps;       // kBack: parts, and k steps of a part
   const float* t;     // `parts` partial shrinks [part][rows of the whole call][r_max], to be added in part order
   size_t t_stride;    // floats from one part to the next
   int parts;
@@ -79,10 +85,28 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
 }
 
-// GATED: the tile's W side is 128 columns of the gate and the same of the up projection, 64 and 64 in each wave's part, so that a
+// kGated: the tile's W side is 128 columns of the gate and the same of the up projection, 64 and 64 in each wave's part, so that a
 // lane ends up with both for its outputs: Y = silu(g) u, rounded once.
-template <bool GATED>
+//
+// kBack: Y = X [W; W2], the reduction (d1) running over the rows of both row-major weights (each [d1 / 2][d2]): the gradient behind the two
+// projections, X = [dg | du].  A k step's W side is 64 rows of 256 columns, copied as they lie, 256 bytes of a row to a half; the transposing
+// LDS read (ds_read_b64_tr_b16: four rows x sixteen columns by sixteen lanes) makes operands of them.  A row's sixteen-column pieces are permuted
+// so that the four rows of two pieces that half a wave reads at once lie on all banks.  The LoRA steps take t = dz W^B^T against the rows of
+// W^A, which are contiguous along the ranks.  Few tiles: the reduction in S parts, their fp32 sums added in part order by a launch behind this one.
+__device__ __forceinline__ int swz_tr(int k) { return ((k & 3) << 1) | ((k >> 3) & 1); }  // of a row's eight pieces
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bf16x8 read_tr(uint32_t at) {  // rows k .. k + 3 and, 1024 bytes on, k + 4 .. k + 7
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  s16x4 v[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + h * 1024));
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+template <int MODE>
 __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
+  constexpr bool GATED = MODE == kGated, BACK = MODE == kBack;
+  constexpr int kSites = MODE == kPlain ? 1 : 2;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -91,10 +115,12 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // workgroup -> tile: workgroup ids go round-robin over the 8 XCDs; each XCD takes a contiguous run of the
   // tile order, which walks kGroupM row tiles per column tile so that the XCD's L2 serves the re-reads
   // (the 32 workgroups resident on an XCD then cover 4 row tiles x 8 column tiles)
-  const int total = p.tilesM * p.tilesN;
+  const int total = p.tilesM * p.tilesN * (BACK ? p.S : 1);
   const int per = (total + 7) / 8;
-  const int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
   if (id >= total) return;
+  const int part = BACK ? id / (p.tilesM * p.tilesN) : 0;
+  if (BACK) id %= p.tilesM * p.tilesN;
   const int gspan = kGroupM * p.tilesN;
   const int first = id / gspan * kGroupM;
   const int gsz = p.tilesM - first < kGroupM ? p.tilesM - first : kGroupM;
@@ -102,7 +128,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const int64_t m0 = (int64_t)(first + in_group % gsz) * kTM;
   const int n0 = in_group / gsz * (GATED ? kTN / 2 : kTN);
 
-  const int KT = p.d1 / kTK;
+  const int kt0 = BACK ? part * p.steps : 0;
+  const int KT = BACK ? (p.d1 / kTK - kt0 < p.steps ? p.d1 / kTK - kt0 : p.steps) : p.d1 / kTK;
   const uint32_t lds0 = lds_addr(lds);
 
   // copies.  A k step of 64 is brought in two halves: half 0 = X rows 0..127 and W rows 0..127 of the tile,
@@ -124,14 +151,25 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       int64_t r = row0 + block * 16 + (j & 1) * 8 + rr;
       r = r < rlim ? r : rlim - 1;
       voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((j & 1) * 8 + rr)) * 16u);
+      if (BACK && is_w) {  // four rows of 128 columns
+        const int k = ((wave & 1) * 8 + j) * 4 + (lane >> 4);
+        int n = n0 + hh * 128 + (((lane & 15) >> 1) ^ swz_tr(k)) * 16 + (lane & 1) * 8;
+        n = n < p.d2 ? n : p.d2 - 8;  // past the edge: results dropped
+        voff[hh][j] = (uint32_t)k * (uint32_t)p.d2 * 2u + (uint32_t)n * 2u;
+      }
     }
+  // (BACK: the second half of the reduction is the second weight's)
+  const int half_steps = p.d1 / kTK / 2, back_by = BACK && is_w ? half_steps : 0;
+  const unsigned char* const src2 = BACK && is_w ? (const unsigned char*)p.W2 : src;
+  const size_t k_bytes = BACK && is_w ? (size_t)kTK * p.d2 * 2 : kTK * 2;
   const uint32_t dst_in_half = (uint32_t)((is_w ? 8 : 0) + (wave & 1) * 4) * kBlockBytes;
   // half H = 2 * (k step) + hh lives in ring slot H % kHalves
   // copy j (0..7) of a half; a wave's eight copies of a half are spread between its matrix instructions: issued
   // back to back they would hold the wave at the issue of the memory instructions while the matrix cores idle
   auto issue_one = [&](int kt, int hh, int slot, int j) __attribute__((always_inline)) {
-    const int kk = kt < KT ? kt : KT - 1;  // past the end: re-read the last step into a slot nobody reads
-    const unsigned char* b = src + (size_t)kk * (kTK * 2);
+    const int kk = kt0 + (kt < KT ? kt : KT - 1);  // past the end: re-read the last step into a slot nobody reads
+    const bool second = BACK && kk >= half_steps;
+    const unsigned char* b = (second ? src2 : src) + (size_t)(second ? kk - back_by : kk) * (BACK ? k_bytes : kTK * 2);
     const uint32_t dst = lds0 + slot * kHalfBytes + dst_in_half;
     copy_to_lds16(b, voff[hh][j], dst + j * 1024);
   };
@@ -157,27 +195,38 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   for (int ks = 0; ks < 4; ++ks)
     rd[ks] = (rrow >> 4) * kBlockBytes + (rrow & 15) * 128 + (((2 * ks + (lane >> 5)) ^ swz(rrow & 15)) << 4);
   const unsigned char* wbase = lds + (kBlocksM / 2) * kBlockBytes;
+  uint32_t rd_tr[4];  // (BACK) of the columns 32 j .., rows 8 (l / 32) .. of a sub-step
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int k = (lane >> 5) * 8 + ((lane & 15) >> 2);
+    rd_tr[j] = lds0 + (kBlocksM / 2) * kBlockBytes + k * 256 + (((2 * j + ((lane >> 4) & 1)) ^ swz_tr(k)) & 7) * 32 + (lane & 3) * 8;
+  }
   // One k step of 64 for the wave's 128 x 128 part: 64 matrix instructions, number q = 16 ks + 4 i + j.  The
   // operand reads come early: the sixteen of the first two sub-steps, then the other sixteen between the matrix
   // instructions of the first sub-step.  `mid` runs after instruction 15, once every wave of the workgroup has
   // its operands in registers: the step's two ring slots are free from there on.  copy(q) runs after instruction q.
-  auto mma64 = [&](int slot_x, int slot_w, auto mid, auto copy) __attribute__((always_inline)) {
+  auto mma64 = [&](auto tr, int slot_x, int slot_w, auto mid, auto copy) __attribute__((always_inline)) {
     const unsigned char* sa = lds + slot_x * kHalfBytes;
     const unsigned char* sb = wbase + slot_w * kHalfBytes;
+    const uint32_t tb = slot_w * kHalfBytes;
     bf16x8 a[4][4], b[4][4];
+    auto read_w = [&](int ks, int j) __attribute__((always_inline)) {
+      if constexpr (decltype(tr)::value) return read_tr(rd_tr[j] + tb + ks * 4096);
+      else return *(const bf16x8*)(sb + rd[ks] + j * 2 * kBlockBytes);
+    };
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[ks][i] = *(const bf16x8*)(sa + rd[ks] + i * 2 * kBlockBytes);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[ks][j] = *(const bf16x8*)(sb + rd[ks] + j * 2 * kBlockBytes);
+      for (int j = 0; j < 4; ++j) b[ks][j] = read_w(ks, j);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
       acc[q >> 2][q & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[0][q & 3], a[0][q >> 2], acc[q >> 2][q & 3], 0, 0, 0);
       const int ks = 2 + (q >> 3), e = q & 3;
-      if (q & 4) b[ks][e] = *(const bf16x8*)(sb + rd[ks] + e * 2 * kBlockBytes);
+      if (q & 4) b[ks][e] = read_w(ks, e);
       else a[ks][e] = *(const bf16x8*)(sa + rd[ks] + e * 2 * kBlockBytes);
       copy(q);
       __builtin_amdgcn_sched_barrier(0);
@@ -219,7 +268,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     __builtin_amdgcn_s_barrier();   // for every wave
     asm volatile("" ::: "memory");
     mma64(
-        wm ? h1 : h0, wn ? h1 : h0,
+        std::integral_constant<bool, BACK>{}, wm ? h1 : h0, wn ? h1 : h0,
         [&]() __attribute__((always_inline)) {
           __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's operand reads have returned
           __builtin_amdgcn_s_barrier();        // and every other wave's
@@ -247,16 +296,16 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // t by way of LDS, one step at a time: a call of 777 rows on 4096 x 11008 with a tenant of rank 64 131 us, 120 so, 97 without).
   int* ctl = (int*)(lds + 4 * kHalfBytes);  // ring slots 0 .. 3 hold the operand blocks
   int* const row_ten = ctl + 16;            // tenant of each row of the tile, -1: no LoRA term
-  int my_ten = -1, my_ten2 = -1;  // (of the second site: GATED)
+  int my_ten = -1, my_ten2 = -1;  // (of the second site)
   {
     const int64_t m = m0 + tid;
-    if (m < p.M) {
+    if (m < p.M && (!BACK || part == p.S - 1)) {
       const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : p.row_base + m;
       const bool in = req >= 0 && req < p.B;
       int tenant = 0;
       int r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
       if (r) my_ten = tenant;
-      if (GATED) {
+      if (kSites > 1) {
         r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + 1, &tenant) : 0;
         if (r) my_ten2 = tenant;
       }
@@ -264,11 +313,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   }
   if (tid == 0) ctl[1] = 0;  // set: W^B of some tenant of the tile holds Inf or NaN
 #pragma unroll 1
-  for (int s = 0; s < (GATED ? 2 : 1); ++s) {
-  if (GATED && s) my_ten = my_ten2;
+  for (int s = 0; s < kSites; ++s) {
+  if (s) my_ten = my_ten2;
   row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
-  const float* const t_of = p.t + (GATED ? s * p.t_site : 0);
-  const int site = p.site + (GATED ? s : 0);
+  const float* const t_of = p.t + (kSites > 1 ? s * p.t_site : 0);
+  const int site = p.site + (kSites > 1 ? s : 0);
   int last = -1;
   for (;;) {
     if (tid == 0) ctl[0] = 0x7fffffff;
@@ -284,7 +333,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     const int cur = ctl[0];
     if (cur == 0x7fffffff) break;
     const int r = p.ad.rank[cur];
-    gbf16* Bm = in_global(p.ad.B[cur * MILORA_NUM_SITES + site]);
+    gbf16* Bm = in_global((BACK ? p.ad.A : p.ad.B)[cur * MILORA_NUM_SITES + site]);
+    const bool vec_a = BACK && (r & 7) == 0 && ((uintptr_t)Bm & 15) == 0;
     for (int c0 = 0; c0 < r; c0 += 64) {
       int tb = tid;  // opaque: addresses formed from it stay inside the loop instead of being spilled in front of it
       asm volatile("" : "+v"(tb));
@@ -298,10 +348,12 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       // (GATED: of a wave's 128 columns the first 64 are the gate's; the other projection's stay zero)
       const int n_piece = n0 + (GATED ? (pc >> 4) * 64 + (pc & 7) * 8 : pc * 8);
       if (wput && n_piece < p.d2 && (!GATED || ((pc >> 3) & 1) == s)) {
-        gbf16* b = Bm + (size_t)cw * p.d2 + n_piece;
+        gbf16* b = BACK ? Bm + (size_t)n_piece * r + cw : Bm + (size_t)cw * p.d2 + n_piece;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (cw + i < r) a[i] = *(gu32x4_a2*)(b + (size_t)i * p.d2);  // (whole pieces of 8 columns, d2 % 16 == 0, at any alignment)
+          if (BACK) {  // column n_piece + i, eight ranks of it (zero past the last)
+            if (cw < r) a[i] = load8(b + (size_t)i * r, r - cw, vec_a);
+          } else if (cw + i < r) a[i] = *(gu32x4_a2*)(b + (size_t)i * p.d2);  // (whole pieces of 8 columns, d2 % 16 == 0, at any alignment)
       }
       // X side: eight lanes take 32 ranks of a row, the shrink's parts added in part order
       const int rq = tb & 7;
@@ -373,7 +425,12 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           ctl[1] = 1;
         }
         u32x4 at[8];
-        transpose8(a, at);
+        if constexpr (BACK) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) at[i] = a[i];
+        } else {
+          transpose8(a, at);
+        }
         // (columns 8 pc .. + 7: one half of a block of 16)
         unsigned char* const wst = lds + (2 * (gq >> 2) + (pc >> 4)) * kHalfBytes + (kBlocksM / 2 + ((pc >> 1) & 7)) * kBlockBytes;
 #pragma unroll
@@ -384,7 +441,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         }
       }
       __syncthreads();
-      for (int st = 0; st < steps; ++st) mma64(2 * st + wm, 2 * st + wn, []() {}, [](int) {});
+      for (int st = 0; st < steps; ++st) mma64(std::false_type{}, 2 * st + wm, 2 * st + wn, []() {}, [](int) {});
       __syncthreads();
     }
     last = cur;
@@ -442,8 +499,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         asm volatile("" ::: "memory");
       }
     }
-    // g and u as they are, for a backward pass: whole lines of four rows a store
-    auto save = [&](int s, float* to) __attribute__((always_inline)) {
+  }
+  if constexpr (MODE != kPlain) {
+    // 64 columns of the wave's sums in fp32, whole lines of four rows a store
+    auto save = [&](int s, float* to, int col0) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -454,7 +513,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
                 f32x4{acc[i][2 * s + j][4 * g], acc[i][2 * s + j][4 * g + 1], acc[i][2 * s + j][4 * g + 2], acc[i][2 * s + j][4 * g + 3]};
       __builtin_amdgcn_s_waitcnt(0xc07f);
       asm volatile("" ::: "memory");
-      const int n = n0 + wn * 64 + (lane & 15) * 4;
+      const int n = col0 + (lane & 15) * 4;
       const int64_t mw = m0 + wm * 128 + (lane >> 4);
       const unsigned char* q = mine + (lane >> 4) * kOutPitch + (lane & 15) * 16;
       if (n < p.d2)
@@ -465,8 +524,18 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       __builtin_amdgcn_s_waitcnt(0xc07f);
       asm volatile("" ::: "memory");
     };
-    if (p.gate_out) save(0, p.gate_out);
-    if (p.up_out) save(1, p.up_out);
+    if constexpr (BACK) {
+      if (p.S > 1) {
+        float* const mine_out = p.partial + part * p.partial_stride;
+        save(0, mine_out, n0 + wn * 128);
+        save(1, mine_out, n0 + wn * 128 + 64);
+      }
+    } else {
+      if (p.gate_out) save(0, p.gate_out, n0 + wn * 64);  // g and u as they are, for a backward pass
+      if (p.up_out) save(1, p.up_out, n0 + wn * 64);
+    }
+  }
+  if constexpr (GATED) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -495,6 +564,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         }
     return;
   }
+  const bool whole = !BACK || p.S == 1;  // the sums are the result
+  if (whole) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -530,6 +601,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         }
       }
   }
+  }
 
   // ---- what the stages could not take: products with the tenant's own Inf and NaN, onto the stored results (no finite part of
   // them matters any more)
@@ -540,25 +612,33 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       const int64_t m = m0 + wm * 128 + i * 32 + (lane & 31);
       if (m >= p.M) continue;
       const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : p.row_base + m;
+      for (int s = 0; s < kSites; ++s) {
       int tenant = 0;
-      const int r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
+      const int r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + s, &tenant) : 0;
       for (int c = 0; c < r; ++c) {
-        gbf16* b = in_global(p.ad.B[tenant * MILORA_NUM_SITES + p.site]) + (size_t)c * p.d2;
+        gbf16* b = in_global((BACK ? p.ad.A : p.ad.B)[tenant * MILORA_NUM_SITES + p.site + s]) + (BACK ? (size_t)c : (size_t)c * p.d2);
         float t = 0.f;
-        for (int k = 0; k < p.parts; ++k) t += p.t[k * p.t_stride + (size_t)m * p.ad.r_max + c];
+        for (int k = 0; k < p.parts; ++k) t += p.t[(kSites > 1 ? s * p.t_site : 0) + k * p.t_stride + (size_t)m * p.ad.r_max + c];
         for (int q = 0; q < 64; ++q) {  // this lane's columns
           const int n = n0 + wn * 128 + (q >> 4) * 32 + ((q >> 2) & 3) * 8 + (lane >> 5) * 4 + (q & 3);
-          if (n >= p.d2 || (b[n] & 0x7f80u) != 0x7f80u) continue;
-          bf16_t* const y = p.Y + (size_t)m * p.d2 + n;
-          *y = f32_to_bf16(bf16_to_f32(*y) + t * bf16_to_f32(b[n]));
+          if (n >= p.d2) continue;
+          const bf16_t bv = b[BACK ? (size_t)n * r : (size_t)n];
+          if ((bv & 0x7f80u) != 0x7f80u) continue;
+          if (whole) {
+            bf16_t* const y = p.Y + (size_t)m * p.d2 + n;
+            *y = f32_to_bf16(bf16_to_f32(*y) + t * bf16_to_f32(bv));
+          } else {
+            p.partial[part * p.partial_stride + (size_t)m * p.d2 + n] += t * bf16_to_f32(bv);
+          }
         }
+      }
       }
     }
   }
 }
 
 // SITES: several sites in one launch, blockIdx.z = site x shares + share.
-template <int RT, bool INFO, bool SITES>
+template <int RT, bool INFO, bool SITES, bool TRANS>
 __global__ void __launch_bounds__(512, 4) shrink_tiles_kernel(const ShrinkArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char smem[8 * kShrinkWaveBytes];
   __shared__ int row_ten[RT * 16 * (INFO ? 2 : 1)];
@@ -567,25 +647,29 @@ __global__ void __launch_bounds__(512, 4) shrink_tiles_kernel(const ShrinkArgs g
     const int shares = gridDim.z / g.sites, s = blockIdx.z / shares;
     ShrinkArgs one = g;
     one.site += s;
+    one.X += s * g.x_site;
     one.t += s * g.t_site;
     if (one.row_lora) one.row_lora += s * g.lora_site;
-    shrink_block<RT, 8, INFO>(one, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z % shares, shares, smem, row_ten, store);
+    shrink_block<RT, 8, INFO, TRANS>(one, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z % shares, shares, smem, row_ten, store);
   } else {
-    shrink_block<RT, 8, INFO>(g, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z, gridDim.z, smem, row_ten, store);
+    shrink_block<RT, 8, INFO, TRANS>(g, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z, gridDim.z, smem, row_ten, store);
   }
   static_assert(kShrinkClear == 512, "one word per thread");
   if (INFO && g.clear && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) g.clear[threadIdx.x] = 0;
 }
 
 template <int RT>
-void launch_shrink_block(const ShrinkArgs& g, dim3 grid, hipStream_t st) {
+void launch_shrink_block(const ShrinkArgs& g, dim3 grid, bool trans, hipStream_t st) {
   const bool info = g.row_lora || g.clear;
-  if (g.sites > 1) {
-    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, true>), grid, dim3(512), 0, st, g);
-    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, true>), grid, dim3(512), 0, st, g);
+  if (!trans) {
+    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, true, false>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, true, false>), grid, dim3(512), 0, st, g);
+  } else if (g.sites > 1) {
+    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, true, true>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, true, true>), grid, dim3(512), 0, st, g);
   } else {
-    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, false>), grid, dim3(512), 0, st, g);
-    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, false>), grid, dim3(512), 0, st, g);
+    if (info) hipLaunchKernelGGL((shrink_tiles_kernel<RT, true, false, true>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((shrink_tiles_kernel<RT, false, false, true>), grid, dim3(512), 0, st, g);
   }
 }
 
@@ -597,19 +681,20 @@ bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, 
   return (uint64_t)d2 * (uint64_t)d1 * 2u < (1ull << 32);  // 32-bit byte offsets inside W (X is cut into row slices)
 }
 
-template <bool GATED>
+template <int MODE>
 static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t stream) {
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel<GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
+    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel<MODE>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
     lds_set_for = dev;
   }
   // rows are independent: slices whose byte offsets inside X fit 32 bits and whose tile count fits a launch
   const PParams all = p;
   int64_t slice = (int64_t)(((1ull << 32) - 1) / ((uint64_t)p.d1 * 2u)) / kTM * kTM;
-  const int tilesN = (p.d2 + kTN / (GATED ? 2 : 1) - 1) / (kTN / (GATED ? 2 : 1));
+  constexpr int kCols = MODE == kGated ? kTN / 2 : kTN;
+  const int tilesN = (p.d2 + kCols - 1) / kCols;
   const int64_t by_grid = (int64_t)((1 << 24) / tilesN) * kTM;
   if (slice > by_grid) slice = by_grid;
   if (slice < kTM) return MILORA_EUNSUPPORTED;
@@ -617,16 +702,17 @@ static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t st
     p.M = M - r0 < slice ? M - r0 : slice;
     p.X = all.X + (size_t)r0 * p.d1;
     p.Y = all.Y + (size_t)r0 * p.d2;
-    if (GATED && all.gate_out) p.gate_out = all.gate_out + (size_t)r0 * p.d2;
-    if (GATED && all.up_out) p.up_out = all.up_out + (size_t)r0 * p.d2;
+    if (all.gate_out) p.gate_out = all.gate_out + (size_t)r0 * p.d2;
+    if (all.up_out) p.up_out = all.up_out + (size_t)r0 * p.d2;
+    if (all.partial) p.partial = all.partial + (size_t)r0 * p.d2;
     p.t = all.t + (size_t)r0 * p.ad.r_max;
     p.row_to_req = all.row_to_req ? all.row_to_req + r0 : nullptr;
     p.row_base = row_base + r0;
     p.tilesM = (int)((p.M + kTM - 1) / kTM);
     p.tilesN = tilesN;
-    const int total = p.tilesM * p.tilesN;
+    const int total = p.tilesM * p.tilesN * (MODE == kBack ? p.S : 1);
     const int per = (total + 7) / 8;
-    hipLaunchKernelGGL(prefill_kernel<GATED>, dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
+    hipLaunchKernelGGL(prefill_kernel<MODE>, dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
     const int rc = check_launch();
     if (rc) return rc;
   }
@@ -642,7 +728,7 @@ int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int3
   p.parts = shrink_parts(M, d1);
   p.row_to_req = row_to_req; p.tenant_id = tenant_id; p.route = route; p.ad = ad;
   p.d1 = d1; p.d2 = d2; p.site = site; p.B = B;
-  return launch_prefill<false>(p, M, 0, stream);
+  return launch_prefill<kPlain>(p, M, 0, stream);
 }
 
 int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
@@ -651,7 +737,97 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
   p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
   p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
-  return launch_prefill<true>(p, g.M, g.row_base, stream);
+  return launch_prefill<kGated>(p, g.M, g.row_base, stream);
+}
+
+// Parts of the reduction: as many as make the tiles fill the compute units once, whole k steps each, eight at least.
+static int back_parts(int64_t M, int d, int F, int* steps) {
+  const int64_t tiles = ((M + kTM - 1) / kTM) * ((d + kTN - 1) / kTN);
+  const int KT = 2 * F / kTK;
+  int64_t S = 256 / tiles;
+  if (S > KT / 8) S = KT / 8;
+  if (S < 1) S = 1;
+  *steps = (int)((KT + S - 1) / S);
+  return (KT + *steps - 1) / *steps;
+}
+
+// What the sums of a call with several parts take, at most: 256 workgroups share its reduction, eight k steps at least each.  Never
+// less for a larger call, so that a workspace for the largest serves all.
+size_t back_partial_floats(int64_t M, int d, int F) {
+  const size_t by_grid = (size_t)256 * kTM * kTN, by_steps = (size_t)(F / 256 + 1) * (size_t)M * d;
+  return by_steps < by_grid ? by_steps : by_grid;
+}
+
+bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX) {
+  if (F % kTK != 0 || d % 16 != 0 || M < 1) return false;
+  if ((((uintptr_t)dz | (uintptr_t)Wg | (uintptr_t)Wu) & 15) != 0 || ((uintptr_t)dX & 7) != 0) return false;
+  return (uint64_t)d * kTK * 2u < (1ull << 31) && (uint64_t)F * 4u * kTM < (1ull << 32) && (int64_t)((d + kTN - 1) / kTN) <= 1 << 16;
+}
+
+static __global__ void __launch_bounds__(256) add_parts_kernel(const float* __restrict__ partial, int S, size_t stride, int64_t fours, bf16_t* __restrict__ y) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= fours) return;
+  const float* const q = partial + i * 4;
+  f32x4 v = *(const f32x4*)q;
+  int s = 1;
+  for (; s + 4 <= S; s += 4) {
+    f32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = *(const f32x4*)(q + (s + u) * stride);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v += x[u];
+  }
+  for (; s < S; ++s) v += *(const f32x4*)(q + s * stride);
+  u32x2 o;
+  o[0] = pack_bf16x2(v[0], v[1]);
+  o[1] = pack_bf16x2(v[2], v[3]);
+  *(u32x2*)(y + i * 4) = o;
+}
+
+int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
+  PParams p{};
+  p.X = g.dz; p.W = g.Wg; p.W2 = g.Wu; p.Y = g.dX; p.t = g.low; p.t_stride = g.low_stride; p.t_site = g.low_site; p.parts = g.parts;
+  p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
+  p.d1 = 2 * g.F; p.d2 = g.d; p.site = 4; p.B = g.B;
+  p.S = back_parts(g.M, g.d, g.F, &p.steps);
+  p.partial = p.S > 1 ? g.partial : nullptr;
+  p.partial_stride = (size_t)g.M * g.d;
+  const int rc = launch_prefill<kBack>(p, g.M, 0, stream);
+  if (rc || p.S == 1) return rc;
+  const int64_t fours = g.M * g.d / 4;
+  hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, stream, g.partial, p.S, p.partial_stride, fours, g.dX);
+  return check_launch();
+}
+
+static int launch_shrinks(ShrinkArgs g, bool trans, hipStream_t stream) {
+  const ShrinkArgs all = g;
+  const int64_t M = g.M;
+  const int parts = shrink_parts(M, g.d1);
+  const int64_t slice = (int64_t)1 << 28;  // rows per launch: 512 threads for 64 rows, a grid has to stay below 2^32 threads
+  for (int64_t r0 = 0; r0 < M; r0 += slice) {
+    g.X = all.X + (size_t)r0 * g.ldx;
+    g.M = M - r0 < slice ? M - r0 : slice;
+    g.row_base = r0;
+    g.row_to_req = all.row_to_req ? all.row_to_req + r0 : nullptr;
+    g.t = all.t + (size_t)r0 * g.ad.r_max;
+    g.row_lora = all.row_lora ? all.row_lora + r0 : nullptr;
+    if (M <= kTileMaxRows) {
+      // Workgroups share the units of a block (32 ranks of a tenant each) while there can be units for them and all are resident
+      // at once, two per compute unit.  64 packed rows of 64 tenants, rank 256, 4096 x 4096, a call: 189 us with four at
+      // most, 87 so; 45 rows of one request have one unit a block, and no workgroup comes for nothing.
+      const int64_t blocks = (g.M + 15) / 16;
+      const int tenants = g.B < g.ad.n_tenants ? g.B : g.ad.n_tenants;
+      const int units = (tenants < 16 ? tenants : 16) * ((g.ad.r_max + kShrinkC - 1) / kShrinkC);
+      int shares = 1;
+      while (shares < units && blocks * parts * g.sites * shares * 2 <= 512) shares *= 2;
+      launch_shrink_block<1>(g, dim3((unsigned)blocks, parts, shares * g.sites), trans, stream);
+    }
+    else
+      launch_shrink_block<4>(g, dim3((unsigned)((g.M + 63) / 64), parts, g.sites), trans, stream);
+    const int rc = check_launch();
+    if (rc) return rc;
+  }
+  return MILORA_OK;
 }
 
 // LoRA shrink of the rows the tile kernel serves (same conditions as prefill_supported) at `sites` consecutive sites: t receives
@@ -659,30 +835,18 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
 // look-ups found of each row; `clear` (or null) is zeroed.
 int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
                         const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream) {
-  const int parts = shrink_parts(M, d1);
-  const int64_t slice = (int64_t)1 << 28;  // rows per launch: 512 threads for 64 rows, a grid has to stay below 2^32 threads
   const size_t t_stride = (size_t)M * ad.r_max;
-  for (int64_t r0 = 0; r0 < M; r0 += slice) {
-    ShrinkArgs g{X + (size_t)r0 * ldx, ldx, M - r0 < slice ? M - r0 : slice, r0, d1, site, B, row_to_req ? row_to_req + r0 : nullptr,
-                 tenant_id, route, ad, t + (size_t)r0 * ad.r_max, t_stride, row_lora ? row_lora + r0 : nullptr, clear,
-                 sites, t_stride * parts, (size_t)M};
-    if (M <= kTileMaxRows) {
-      // Workgroups share the units of a block (32 ranks of a tenant each) while there can be units for them and all are resident
-      // at once, two per compute unit.  64 packed rows of 64 tenants, rank 256, 4096 x 4096, a call: 189 us with four at
-      // most, 87 so; 45 rows of one request have one unit a block, and no workgroup comes for nothing.
-      const int64_t blocks = (g.M + 15) / 16;
-      const int tenants = B < ad.n_tenants ? B : ad.n_tenants;
-      const int units = (tenants < 16 ? tenants : 16) * ((ad.r_max + kShrinkC - 1) / kShrinkC);
-      int shares = 1;
-      while (shares < units && blocks * parts * sites * shares * 2 <= 512) shares *= 2;
-      launch_shrink_block<1>(g, dim3((unsigned)blocks, parts, shares * sites), stream);
-    }
-    else
-      launch_shrink_block<4>(g, dim3((unsigned)((g.M + 63) / 64), parts, sites), stream);
-    const int rc = check_launch();
-    if (rc) return rc;
-  }
-  return MILORA_OK;
+  return launch_shrinks(ShrinkArgs{X, ldx, M, 0, d1, site, B, row_to_req, tenant_id, route, ad, t, t_stride, row_lora, clear, sites,
+                                   t_stride * shrink_parts(M, d1), (size_t)M, 0}, true, stream);
+}
+
+// low[site][part][m][0..r) = dz[m] (of the site) . (W^B)^T for the rows routed to the gate (site 4) and the up projection; dz [M][2 F],
+// F % 32 == 0, shrink_parts(M, F) parts.
+int launch_low_sites(const bf16_t* dz, int64_t M, int F, const int32_t* row_to_req, const AdapterView& ad, const int32_t* tenant_id,
+                     const uint8_t* route, int B, float* low, hipStream_t stream) {
+  const size_t stride = (size_t)M * ad.r_max;
+  return launch_shrinks(ShrinkArgs{dz, 2 * (int64_t)F, M, 0, F, 4, B, row_to_req, tenant_id, route, ad, low, stride, nullptr, nullptr, 2,
+                                   stride * shrink_parts(M, F), (size_t)M, F}, false, stream);
 }
 
 int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site,

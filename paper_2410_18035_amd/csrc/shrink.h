@@ -41,7 +41,10 @@ struct ShrinkArgs {
   int* clear;      // INFO: [kShrinkClear] words of the launch behind this one that have to start from zero, or null
   int sites;       // consecutive sites of the launch, from `site` on; each has its own t and row_lora
   size_t t_site, lora_site;  // elements from one site's to the next's
+  int64_t x_site;            // elements from one site's X to the next's
 };
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef __attribute__((address_space(1))) const u32x4_any gu32x4_any;
 
 // Two by two bf16 of two words a (k) and b (k + 1): the pair of low halves, the pair of high halves.
 __device__ __forceinline__ uint32_t lo_pair(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
@@ -88,8 +91,9 @@ __device__ __forceinline__ u32x4 load8(gbf16* p, int left, bool vec) {
   return v;
 }
 
+// TRANS false: t = X . (W^B)^T instead, W^B [r][d1] row by row: its rows are operands as they lie.
 // STORE(float* p, float v) stores one element of t.  `smem`: NW * kShrinkWaveBytes, `row_ten`: 16 * RT ints (INFO: twice that).
-template <int RT, int NW, bool INFO, class STORE>
+template <int RT, int NW, bool INFO, bool TRANS, class STORE>
 __device__ __forceinline__ void shrink_block(const ShrinkArgs& g, int row_block, int part, int parts, int share, int shares,
                                              unsigned char* smem, int* row_ten, STORE store) {
   constexpr int kRows = RT * 16;
@@ -132,7 +136,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& g, int row_block,
     if (cur == 0x7fffffff) break;
     const unsigned long long mine = __ballot(my_ten == cur);
     const int r = g.ad.rank[cur];
-    gbf16* A = in_global(g.ad.A[cur * MILORA_NUM_SITES + g.site]);
+    gbf16* A = in_global((TRANS ? g.ad.A : g.ad.B)[cur * MILORA_NUM_SITES + g.site]);
     const bool vec = (r & 7) == 0 && ((uintptr_t)A & 15) == 0;
     for (int cb = 0; cb < r; cb += kShrinkC) {
       const bool ours = unit == share;
@@ -150,7 +154,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& g, int row_block,
       for (int ch = part * NW + wave; ch < chunks; ch += parts * NW) {
         const int k0 = ch * kShrinkChunkK;
         const int steps = g.d1 - k0 < kShrinkChunkK ? (g.d1 - k0) / 32 : kShrinkChunkK / 32;
-        if (oct < kShrinkChunkK / 8) {
+        if (TRANS && oct < kShrinkChunkK / 8) {
           u32x4 a[8], at[8];
           const int k = k0 + oct * 8 < g.d1 ? k0 + oct * 8 : g.d1 - 8;  // past the end: valid rows, not multiplied
 #pragma unroll
@@ -172,7 +176,12 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& g, int row_block,
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
               if (nt < ntile) {
-                const bf16x8 w = *reinterpret_cast<const bf16x8*>(At + (nt * 16 + (lane & 15)) * kShrinkLd + ks * 32 + (lane >> 4) * 8);
+                bf16x8 w;
+                if constexpr (TRANS) w = *reinterpret_cast<const bf16x8*>(At + (nt * 16 + (lane & 15)) * kShrinkLd + ks * 32 + (lane >> 4) * 8);
+                else {
+                  const int c = nt * 16 + (lane & 15);
+                  w = __builtin_bit_cast(bf16x8, *(gu32x4_any*)(A + (size_t)(cb + (c < rc ? c : 0)) * g.d1 + k0 + ks * 32 + (lane >> 4) * 8));
+                }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
                   if (RT == 1 || ((mine >> (16 * rt)) & 0xffff))

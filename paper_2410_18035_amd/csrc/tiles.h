@@ -61,4 +61,25 @@ struct GatedTileArgs {
 int gated_tiles(const GatedTileArgs& g, const TilePlan& pl, hipStream_t st);
 int gated_prefill(const GatedTileArgs& g, hipStream_t st);
 
+// dX = [dg | du] [W_gate; W_up] + sum over the two sites of low A^T on 256 x 256 tiles (prefill.hip).
+struct GatedBackArgs {
+  const bf16_t* dz;  // [M][2 F]
+  int64_t M;
+  int d, F;
+  const int32_t* row_to_req;
+  const bf16_t *Wg, *Wu;  // row-major [F][d]
+  AdapterView ad;
+  const int32_t* tenant_id;
+  const uint8_t* route;
+  int B;
+  const float* low;  // [2][part][M][r_max] = dz W^B^T, to be added in part order
+  size_t low_stride, low_site;
+  int parts;
+  float* partial;  // back_partial_floats(M, d, F)
+  bf16_t* dX;
+};
+bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX);
+size_t back_partial_floats(int64_t M, int d, int F);
+int gated_dx_tiles(const GatedBackArgs& g, hipStream_t st);
+
 }  // namespace milora
