@@ -234,21 +234,15 @@ int layer_decode_generic(const void* x, int B, int d, int F, int dtype, const mi
   return check_launch();
 }
 
-// ---- a decode step on 4-bit weights: the linears of a level in one launch, the glue in their stores ----
+// ---- a decode step on 4-bit weights: two launches a level, the glue in the second ----
 struct MxLayerWs {
-  float* h;      // [B][d]
-  bf16_t* xn;    // [B][d]
-  bf16_t* qkv;   // [B][3 d]
-  bf16_t* hn;    // [B][d]
-  bf16_t* mm;    // [B][F]
-  char* shrink;  // of up to three sites
+  float* h;     // [B][d]
+  bf16_t* qkv;  // [B][3 d]
+  bf16_t* hn;   // [B][d]: h rounded
+  bf16_t* mm;   // [B][F]
+  char* level;  // workspace of a level
   size_t bytes;
 };
-
-size_t mx4_few_workspace(int64_t M, int d1, int r_max, int sites);
-int mx4_shrink(MxArgs* g, const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, int sites, const int32_t* tenant_id,
-               const uint8_t* route, int B, void* workspace, hipStream_t st);
-int mx4_few(MxArgs g, int64_t M, int sites, bool gated, hipStream_t st);
 
 MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
   size_t off = 0;
@@ -256,11 +250,16 @@ MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
   char* b = (char*)base;
   MxLayerWs w;
   w.h = (float*)(b + take((size_t)B * d * 4));
-  w.xn = (bf16_t*)(b + take((size_t)B * d * 2));
   w.qkv = (bf16_t*)(b + take((size_t)B * d * 6));
   w.hn = (bf16_t*)(b + take((size_t)B * d * 2));
   w.mm = (bf16_t*)(b + take((size_t)B * F * 2));
-  w.shrink = b + take(mx4_few_workspace(B, d > F ? d : F, r_max, 3));
+  size_t level = 0;
+  const struct { int d1, d2, sites; } levels[4] = {{d, d, 3}, {d, d, 1}, {d, F, 2}, {F, d, 1}};
+  for (const auto& l : levels) {
+    const size_t n = mx4_rows_workspace_bytes(B, l.d1, l.d2, r_max, l.sites);
+    level = n > level ? n : level;
+  }
+  w.level = b + take(level);
   w.bytes = off;
   return w;
 }
@@ -269,43 +268,33 @@ int layer_decode_mx4(const bf16_t* x, int B, int d, int F, const milora_layer_we
                      const uint8_t* route, uint32_t flags, const bf16_t* attn_out, bf16_t* y, bf16_t* qkv_out, void* workspace, hipStream_t st) {
   const MxLayerWs w = carve_mx4(workspace, B, d, F, ad.r_max);
   const bool norm = (flags & MILORA_LAYER_RMSNORM) != 0;
-  int rc = MILORA_OK;
   MxArgs g{};
+  g.M = g.B = B; g.ad = ad; g.tenant_id = tenant_id; g.route = route;
   // level of `sites` linears from site0 on
   auto level = [&](int site0, int sites, const bf16_t* in, int64_t ldx, bool gated, int64_t ldy) {
-    if (rc) return;
-    int d1, d2;
-    site_dims(site0, d, F, &d1, &d2);
-    g.X = in; g.ldx = ldx; g.d1 = d1; g.d2 = d2; g.ldy = ldy; g.ad = ad;
+    site_dims(site0, d, F, &g.d1, &g.d2);
+    g.X = in; g.ldx = ldx; g.ldy = ldy;
     for (int s = 0; s < sites; ++s) { g.site[s] = site0 + s; g.W[s] = (const unsigned char*)wts->W[site0 + s]; }
-    rc = mx4_shrink(&g, in, ldx, B, d1, nullptr, sites, tenant_id, route, B, w.shrink, st);
-    if (!rc) rc = mx4_few(g, B, sites, gated, st);
+    return launch_mx4_rows(g, sites, gated, w.level, st);
   };
-  if (norm) {
-    hipLaunchKernelGGL((rmsnorm_rows_kernel<bf16_t, bf16_t>), dim3(B), dim3(kThreads), 0, st, x, d, w.xn);
-    if ((rc = check_launch())) return rc;
-  }
   bf16_t* const qkv = qkv_out ? qkv_out : w.qkv;
   for (int s = 0; s < 3; ++s) g.Y[s] = qkv + (size_t)s * d;
-  level(0, 3, norm ? w.xn : x, d, false, 3 * (int64_t)d);
-  g.Y[1] = g.Y[2] = nullptr;
-  g.Y[0] = norm ? nullptr : w.hn;
+  g.norm_x = norm ? x : nullptr;
+  int rc = level(0, 3, x, d, false, 3 * (int64_t)d);
+  if (rc) return rc;
+  g.norm_x = nullptr;
+  g.Y[0] = w.hn;
   g.res = x;
   g.h_out = w.h;
-  if (attn_out) level(3, 1, attn_out, d, false, d);
-  else level(3, 1, qkv + 2 * (size_t)d, 3 * (int64_t)d, false, d);
+  if ((rc = attn_out ? level(3, 1, attn_out, d, false, d) : level(3, 1, qkv + 2 * (size_t)d, 3 * (int64_t)d, false, d))) return rc;
   g.res = nullptr;
-  if (rc) return rc;
-  if (norm) {
-    hipLaunchKernelGGL((rmsnorm_rows_kernel<float, bf16_t>), dim3(B), dim3(kThreads), 0, st, w.h, d, w.hn);
-    if ((rc = check_launch())) return rc;
-  }
   g.Y[0] = w.mm;
-  level(4, 2, w.hn, d, true, F);
+  g.norm_h = norm ? w.h : nullptr;
+  if ((rc = level(4, 2, w.hn, d, true, F))) return rc;
+  g.norm_h = nullptr;
   g.Y[0] = y;
   g.h_in = w.h;
-  level(6, 1, w.mm, F, false, d);
-  return rc;
+  return level(6, 1, w.mm, F, false, d);
 }
 
 bool valid_dtype(int dt) { return dt == MILORA_BF16 || dt == MILORA_F32; }
@@ -393,48 +382,8 @@ int run_linear(const void* X, int64_t M, int d1, int d2, int dtype, const int32_
 }
 
 // ---- 4-bit weights ----
-// Up to kMxFewRows rows the few-row kernel reads the codes again for every kMxRows rows (from the L2 and the cache behind it);
-// beyond, the weight is written out in bf16 once per call, row-major or, where the row-major tiles do not take its reduction, packed.
+// Up to kMxFewRows rows the kernels of mx4.hip multiply the codes; beyond, the weight is written out in bf16 once per call, row-major or, where the row-major tiles do not take its reduction, packed.
 constexpr int64_t kMxFewRows = 128;
-
-size_t mx4_few_workspace(int64_t M, int d1, int r_max, int sites) {
-  return align_up(shrink_rows_bound(M, d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256);
-}
-
-// Shrinks of the rows at `sites` consecutive sites from g.site[0] on, into the workspace, and what the few-row kernel reads of them.
-int mx4_shrink(MxArgs* g, const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, int sites, const int32_t* tenant_id,
-               const uint8_t* route, int B, void* workspace, hipStream_t st) {
-  const int parts = shrink_parts(M, d1);
-  float* const t = (float*)workspace;
-  int2* const lora = (int2*)((char*)t + align_up((size_t)M * g->ad.r_max * parts * sites * sizeof(float), 256));
-  g->t = t;
-  g->t_part = (size_t)M * g->ad.r_max;
-  g->t_site = g->t_part * parts;
-  g->parts = parts;
-  g->row_lora = lora;
-  g->lora_site = (size_t)M;
-  return launch_shrink_sites(X, ldx, M, d1, row_to_req, g->ad, g->site[0], sites, tenant_id, route, B, t, lora, nullptr, st);
-}
-
-// The rows of a call in slices of what a launch takes.
-int mx4_few(MxArgs g, int64_t M, int sites, bool gated, hipStream_t st) {
-  for (int64_t m0 = 0; m0 < M; m0 += kMxRows) {
-    MxArgs s = g;
-    s.M = (int)(M - m0 < kMxRows ? M - m0 : kMxRows);
-    s.X += m0 * g.ldx;
-    for (int i = 0; i < 3; ++i)
-      if (s.Y[i]) s.Y[i] += m0 * g.ldy;
-    if (s.gate_out) s.gate_out += m0 * g.d2;
-    if (s.up_out) s.up_out += m0 * g.d2;
-    if (s.res) { s.res += m0 * g.d2; s.h_out += m0 * g.d2; }
-    if (s.h_in) s.h_in += m0 * g.d2;
-    s.t += m0 * g.ad.r_max;
-    s.row_lora += m0;
-    const int rc = launch_mx4_rows(s, sites, gated, st);
-    if (rc) return rc;
-  }
-  return MILORA_OK;
-}
 
 bool mx4_rowmajor(int d1) { return d1 % 64 == 0; }  // the layout a weight is written out in
 
@@ -443,9 +392,9 @@ int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* ro
                    hipStream_t st) {
   if (M <= kMxFewRows) {
     MxArgs g{};
-    g.X = X; g.ldx = d1; g.d1 = d1; g.d2 = d2; g.W[0] = (const unsigned char*)W; g.bias = bias; g.Y[0] = Y; g.ldy = d2; g.ad = ad; g.site[0] = site;
-    const int rc = mx4_shrink(&g, X, d1, M, d1, row_to_req, 1, tenant_id, route, B, workspace, st);
-    return rc ? rc : mx4_few(g, M, 1, false, st);
+    g.X = X; g.ldx = d1; g.M = (int)M; g.d1 = d1; g.d2 = d2; g.W[0] = (const unsigned char*)W; g.bias = bias; g.Y[0] = Y; g.ldy = d2;
+    g.ad = ad; g.site[0] = site; g.row_to_req = row_to_req; g.tenant_id = tenant_id; g.route = route; g.B = B;
+    return launch_mx4_rows(g, 1, false, workspace, st);
   }
   const bool packed = !mx4_rowmajor(d1);
   const int rc = mx4_dequantize(W, workspace, MILORA_BF16, d1, d2, packed, st);
@@ -487,7 +436,7 @@ extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2
 
 extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
   if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
-  const size_t few = mx4_few_workspace(M < kMxFewRows ? M : kMxFewRows, d1, r_max, 1);
+  const size_t few = mx4_rows_workspace_bytes(M < kMxFewRows ? M : kMxFewRows, d1, d2, r_max, 1);
   if (M <= kMxFewRows) return few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
   return many > few ? many : few;

@@ -80,6 +80,11 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
     c.take<char>(partial_bytes_bound(M, d, 2 * F));
     if (mx4 && M > kMxGatedRows) c.take<bf16_t>((size_t)d * F * 2);
     most = c.off;
+    if (mx4) {
+      const size_t few = mx4_rows_workspace_bytes(M < kMxGatedRows ? M : kMxGatedRows, d, F, r_max, 2);
+      if (M <= kMxGatedRows) return few;
+      most = few > most ? few : most;
+    }
   }
   if (!mx4) {  // (bf16 too: whatever the alignment of its tensors)
     Carver c{nullptr};
@@ -95,26 +100,12 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
   const int64_t M = g.M;
   int rc;
   if (g.mx4 && M <= kMxGatedRows) {
-    Carver c{(char*)workspace};
-    const int parts = shrink_parts(M, g.d);
     MxArgs a{};
-    a.ldx = g.d; a.d1 = g.d; a.d2 = g.F; a.W[0] = (const unsigned char*)g.Wg; a.W[1] = (const unsigned char*)g.Wu; a.ldy = g.F; a.ad = g.ad;
-    a.site[0] = kGate;
-    float* const t = c.take<float>((size_t)M * g.ad.r_max * parts * 2);
-    int2* const lora = c.take<int2>((size_t)M * 2);
-    a.t_part = (size_t)M * g.ad.r_max; a.t_site = a.t_part * parts; a.parts = parts; a.lora_site = (size_t)M;
-    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, lora, nullptr, st);
-    for (int64_t m0 = 0; m0 < M && !rc; m0 += kMxRows) {
-      a.M = (int)(M - m0 < kMxRows ? M - m0 : kMxRows);
-      a.X = (const bf16_t*)g.X + m0 * g.d;
-      a.Y[0] = (bf16_t*)Y + m0 * g.F;
-      a.gate_out = gate_out ? gate_out + m0 * g.F : nullptr;
-      a.up_out = up_out ? up_out + m0 * g.F : nullptr;
-      a.t = t + m0 * g.ad.r_max;
-      a.row_lora = lora + m0;
-      rc = launch_mx4_rows(a, 1, true, st);
-    }
-    return rc;
+    a.X = (const bf16_t*)g.X; a.ldx = g.d; a.M = (int)M; a.d1 = g.d; a.d2 = g.F;
+    a.W[0] = (const unsigned char*)g.Wg; a.W[1] = (const unsigned char*)g.Wu; a.Y[0] = (bf16_t*)Y; a.ldy = g.F;
+    a.gate_out = gate_out; a.up_out = up_out;
+    a.ad = g.ad; a.site[0] = kGate; a.row_to_req = g.row_to_req; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
+    return launch_mx4_rows(a, 2, true, workspace, st);
   }
   const bool packed = g.mx4 && g.d % 64 != 0;  // the layout 4-bit weights are written out in: the row-major tiles take whole 64 of a reduction
   const void* const like = g.mx4 ? (const void*)(uintptr_t)256 : nullptr;  // (in the workspace: aligned)

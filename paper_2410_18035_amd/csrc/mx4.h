@@ -15,29 +15,31 @@ int mx4_quantize(const void* src, int dtype, void* dst, int d1, int d2, hipStrea
 // To [d2][d1] of `dtype`, or (bf16, d2 % 16 == 0) to the packed layout.
 int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool packed, hipStream_t st);
 
-// Few rows: up to kMxRows in one launch.
-constexpr int kMxRows = 32;
+// Few rows: the linears of up to three consecutive sites on the same X, or the gated block.
 struct MxArgs {
   const bf16_t* X;  // M rows of ldx elements
   int64_t ldx;
   int M, d1, d2;
-  const unsigned char* W[3];  // of the sites of the launch; gated: W[0] gate, W[1] up
+  const unsigned char* W[3];  // of the sites; gated: W[0] gate, W[1] up
   const bf16_t* bias;
-  bf16_t* Y[3];     // rows of ldy elements, or null (with res)
+  bf16_t* Y[3];     // rows of ldy elements
   int64_t ldy;
   float* gate_out;  // gated: [M][d2] or null
   float* up_out;
-  const bf16_t* res;   // [M][d2] or null: h_out = res + linear, in fp32 (Y gets it rounded)
+  const bf16_t* res;   // [M][d2] or null: h_out = res + linear, in fp32, and Y that rounded
   float* h_out;
   const float* h_in;   // [M][d2] or null: Y = h_in + linear
-  const float* t;   // [site][part][t_rows][r_max] partial shrinks, to be added in part order
-  size_t t_part, t_site;  // floats from a part, a site to the next
-  int parts;
-  const int2* row_lora;   // [site][lora_rows] tenant and rank of each row
-  size_t lora_site;
+  const bf16_t* norm_x;  // [M][d1] or null: the products are of the rows divided by the root of their mean square (plus 1e-5)
+  const float* norm_h;   // the same, rows in fp32
   AdapterView ad;
   int site[3];
+  const int32_t* row_to_req;
+  const int32_t* tenant_id;
+  const uint8_t* route;
+  int B;
 };
-int launch_mx4_rows(const MxArgs& g, int sites, bool gated, hipStream_t st);
+size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites);
+// gated: sites = 2
+int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st);
 
 }  // namespace milora

@@ -7,13 +7,13 @@
 // s = 255, its weights are NaN.
 #include "mx4.h"
 
+#include "shrink.h"
+
 namespace milora {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(1))) const bf16_t gbf16;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // ---- conversion ---------------------------------------------------------------------------------------------------------
 // Four lanes share a group of 32, eight values each.  Bound: HBM.
@@ -133,263 +133,579 @@ __global__ void __launch_bounds__(kQuantT) mx4_dequantize_kernel(const uint32_t*
   }
 }
 
-// ---- few rows -------------------------------------------------------------------------------------------------------------
-// A workgroup of eight waves takes NT tiles of 16 columns (GATED: half of them of the gate, half of the up projection, for the
-// same outputs) and up to 16 MT rows.  The reduction is dealt to the waves in steps of 128 inputs: a lane loads the 32 codes of
-// one group of one column (16 bytes), its scale and the same 32 inputs of a row of X, and multiplies them in four matrix
-// instructions of 8 inputs a lane (which inputs stand at which place of an instruction does not matter as long as both
-// operands agree).  The codes of a chunk of steps are on their way before the first is used: the whole of a weight of 4096 x 4096
-// is then in flight at once.  The waves' sums meet in LDS.
-// The LoRA term: t = X W^A comes from a launch of its own; the first ranks of W^B are asked for in front of the reduction.
+// ---- few rows: two launches a level -----------------------------------------------------------------------------------------
+// First launch: the base products and the LoRA shrinks, which do not depend on each other.  A workgroup of eight waves takes 256 columns (32 a wave),
+// 32 RT rows and one part of the reduction, in stages of 256 inputs.  A lane holds one group of 32 inputs of one column: 16
+// bytes of codes straight from global memory, two stages on their way; the rows of X go through LDS, shared by the waves, two buffers.  Four
+// matrix instructions of 8 inputs a lane multiply 64 inputs (which inputs stand at which place does not matter as long as both operands agree).
+// The sums of a part go to memory in fp32.  The workgroups in front of those are the shrink's (shrink.h).
+// Second launch: adds the parts in part order, the LoRA term t W^B, bias and glue, and rounds once.
+// Bound: the stream of the codes; many workgroups with short reductions keep it in flight, at the price of their sums' way through memory.
 constexpr int kMxW = 8;
 constexpr int kMxT = kMxW * 64;
+constexpr int kMxCols = kMxW * 32;
+constexpr int kMxK = 256;    // inputs of a stage
+constexpr int kMxAhead = 2;  // stages of codes on their way, and buffers of X
 
-template <int MT, int NT, bool GATED>
-struct MxCfg {
-  static constexpr int U = MT * NT > 2 ? 2 : 4;  // steps of a chunk
-  static constexpr int Ld = 16 * NT + 4;      // fp32 row of the sums in LDS
-  static constexpr int Sites = GATED ? 2 : 1;
-  static constexpr int Outs = MT * NT;        // outputs of a thread (two threads share each)
-  static constexpr int Pre = Outs == 1 ? 16 : 16 / Outs;      // ranks of each asked for ahead
-  static constexpr int RedBytes = kMxW * 16 * MT * Ld * 4;
+struct MxBase {
+  const bf16_t* X;
+  int64_t ldx;
+  int M, d1, d2;
+  const unsigned char* W[3];
+  int sites, col_groups, row_groups, parts, stages;  // stages of a part
+  float* partial;  // [site][part][M][d2]
+  int shrink_blocks, shrink_parts, shrink_z;         // workgroups of the shrink: row blocks x parts x (sites x shares)
+  ShrinkArgs shrink;
 };
 
-template <int MT, int NT, bool GATED>
-__global__ void __launch_bounds__(kMxT, 4) mx4_rows_kernel(const MxArgs g) {
-  typedef MxCfg<MT, NT, GATED> C;
+template <int RT>
+__global__ void __launch_bounds__(kMxT, RT > 2 ? 2 : 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  __shared__ int2 s_lora[C::Sites][16 * MT];
-  float* const red = reinterpret_cast<float*>(lds);                 // [wave][row][Ld]
-  float* const ts = reinterpret_cast<float*>(lds + C::RedBytes);    // [site][row][r_max]
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lq = lane >> 4;
+  const int tid = threadIdx.x;
+  int id = blockIdx.x;
+  const int shrinks = g.shrink_blocks * g.shrink_parts * g.shrink_z;
+  if (id < shrinks) {
+    __shared__ int row_ten[32];
+    const int block = id % g.shrink_blocks, part = id / g.shrink_blocks % g.shrink_parts, z = id / (g.shrink_blocks * g.shrink_parts);
+    const int shares = g.shrink_z / g.shrink.sites, s = z / shares;
+    ShrinkArgs one = g.shrink;
+    one.site += s;
+    one.t += s * one.t_site;
+    one.row_lora += s * one.lora_site;
+    shrink_block<1, kMxW, true, true>(one, block, part, g.shrink_parts, z % shares, shares, lds, row_ten, [](float* p, float v) { *p = v; });
+    return;
+  }
+  id -= shrinks;
+  const int lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s0 = GATED ? 0 : blockIdx.y;
-  constexpr int kCols = GATED ? NT * 8 : NT * 16;  // outputs of the workgroup
-  const int n0 = blockIdx.x * kCols;
-  const int d1 = g.d1, r_max = g.ad.r_max;
+  const int rg = id % g.row_groups, part = id / g.row_groups % g.parts, cg = id / (g.row_groups * g.parts) % g.col_groups,
+            site = id / (g.row_groups * g.parts * g.col_groups);
+  const int m0 = rg * 32 * RT, rows = g.M - m0 < 32 * RT ? g.M - m0 : 32 * RT;
+  const int n0 = cg * kMxCols + w * 32, d1 = g.d1;
+  const bool active = n0 < g.d2;  // (a wave without columns helps with X)
+  const int all = (d1 + kMxK - 1) / kMxK, st0 = part * g.stages, n_st = all - st0 < g.stages ? all - st0 : g.stages;
 
-  // ---- operands of this lane ----
-  const unsigned char* wp[NT];
-  const uint8_t* sp[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    int col = n0 + (GATED ? j / 2 : j) * 16 + li;
+  const unsigned char* wp;
+  const uint8_t* sp;
+  {
+    int col = n0 + l32;
     col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
-    const unsigned char* const base = g.W[GATED ? j & 1 : s0];
-    wp[j] = base + (size_t)col * (d1 >> 1) + lq * 16;
-    sp[j] = base + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5) + lq;
+    wp = g.W[site] + (size_t)col * (d1 >> 1) + lh * 16;
+    sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5);
   }
-  const bf16_t* xp[MT];
+  typedef uint64_t u64_a1 __attribute__((aligned(1)));
+  u32x4 c[kMxAhead][4];
+  uint64_t sc[kMxAhead];
+  auto ask_w = [&](int i, u32x4 (&cv)[4], uint64_t& sv) __attribute__((always_inline)) {
+    const int st = st0 + (i < n_st ? i : n_st - 1);
+    if (!active) return;
+    if ((st + 1) * kMxK <= d1) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int row = i * 16 + li < g.M ? i * 16 + li : g.M - 1;
-    xp[i] = g.X + (size_t)row * g.ldx + lq * 32;
-  }
-  f32x4 acc[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int full = d1 >> 7;  // whole steps
-  u32x4 c[C::U][NT];
-  uint32_t sc[C::U][NT];
-  auto load = [&](int b0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < C::U; ++u) {
-      const int b = b0 + u * kMxW < full ? b0 + u * kMxW : full - 1;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        c[u][j] = *reinterpret_cast<const u32x4*>(wp[j] + (size_t)b * 64);
-        sc[u][j] = sp[j][b * 4];
-      }
-    }
-  };
-  auto load_x = [&](int b, u32x4 (&x)[MT][4]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[i][k] = *reinterpret_cast<const u32x4*>(xp[i] + (size_t)b * 128 + k * 8);
-  };
-  auto step = [&](const u32x4 (&cc)[NT], const uint32_t (&ss)[NT], const u32x4 (&xx)[MT][4]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const float scale = mx4_scale(ss[j]);
+      for (int k = 0; k < 4; ++k) cv[k] = *reinterpret_cast<const u32x4*>(wp + (size_t)st * (kMxK / 2) + k * 32);
+      sv = *reinterpret_cast<const u64_a1*>(sp + st * (kMxK / 32)) >> (8 * lh);
+    } else {  // the last stage: zeros past the end of the reduction
+      sv = 0x007f007f007f007full;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_bf16(cc[j][k], scale));
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, xx[i][k]), acc[i][j], 0, 0, 0);
+        const int at = st * kMxK + k * 64 + lh * 32;
+        cv[k] = u32x4{0u, 0u, 0u, 0u};
+        if (at < d1) {
+          cv[k] = *reinterpret_cast<const u32x4*>(wp + (size_t)st * (kMxK / 2) + k * 32);
+          sv = (sv & ~(0xffffull << (16 * k))) | ((uint64_t)sp[at >> 5] << (16 * k));
+        }
       }
     }
   };
-  if (w < full) load(w);
-
-  // ---- LoRA: tenants and ranks of the rows, t into LDS, the first ranks of W^B ----
-  if (tid < 16 * MT)
+  // X: thread -> 16-byte piece tid % 32 of rows tid / 32 + 16 i of a stage's 512 bytes a row; pieces permuted by the row so that an
+  // operand read of neighbouring rows at one piece hits different banks
+  constexpr int kXRows = 2 * RT;
+  constexpr int kXBytes = 32 * RT * kMxK * 2;
+  const int piece = tid & 31, xr0 = tid >> 5;
+  const bf16_t* const xb = g.X + (size_t)m0 * g.ldx + piece * 8;
+  u32x4 x[kXRows];
+  auto ask_x = [&](int i) __attribute__((always_inline)) {
+    const int st = st0 + (i < n_st ? i : n_st - 1);
+    const bool in = st * kMxK + piece * 8 < d1;
 #pragma unroll
-    for (int s = 0; s < C::Sites; ++s)
-      s_lora[s][tid] = tid < g.M ? g.row_lora[(s0 + s) * g.lora_site + tid] : int2{-1, 0};
-  __syncthreads();
-  const int n_out = tid & 15, m_out = (tid >> 4) & 15, half = tid >> 8;
-  const bf16_t* bp[MT][NT];
-  int rank[MT][NT];
-  uint32_t pre[MT][NT][C::Pre];
+    for (int k = 0; k < kXRows; ++k) {
+      const int r = xr0 + 16 * k;
+      x[k] = u32x4{0u, 0u, 0u, 0u};
+      if (in && r < rows) x[k] = *reinterpret_cast<const u32x4*>(xb + (size_t)r * g.ldx + st * kMxK);
+    }
+  };
+  auto put_x = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+    for (int k = 0; k < kXRows; ++k) {
+      const int r = xr0 + 16 * k;
+      if (r < rows) *reinterpret_cast<u32x4*>(lds + buf * kXBytes + r * (kMxK * 2) + ((piece ^ (r & 31)) << 4)) = x[k];
+    }
+  };
+  f32x16 acc[RT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int2 tr = s_lora[GATED ? j & 1 : 0][i * 16 + m_out];
-      const int n = n0 + (GATED ? j / 2 : j) * 16 + n_out;
-      rank[i][j] = n < g.d2 ? tr.y : 0;
-      bp[i][j] = nullptr;
-      if (rank[i][j] > 0) {
-        bp[i][j] = (const bf16_t*)g.ad.B[tr.x * MILORA_NUM_SITES + g.site[s0] + (GATED ? j & 1 : 0)] + n;
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int u = 0; u < C::Pre; ++u) {  // this half's ranks: half, half + 2, ...
-          const int r = 2 * u + half;
-          pre[i][j][u] = ((gbf16*)bp[i][j])[(size_t)(r < rank[i][j] ? r : 0) * g.d2];
+    for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+  auto barrier = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS reads and writes done; what is on its way from memory stays so
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto stage = [&](const u32x4 (&cv)[4], uint64_t sv, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float scale = mx4_scale((uint32_t)(sv >> (16 * k)) & 255u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_bf16(cv[k][e], scale));
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const int at = (k * 8 + lh * 4 + e) ^ l32;
+          const bf16x8 xv = *reinterpret_cast<const bf16x8*>(lds + buf * kXBytes + (i * 32 + l32) * (kMxK * 2) + (at << 4));
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv, acc[i], 0, 0, 0);
         }
       }
     }
-  for (int e = tid; e < C::Sites * 16 * MT * r_max; e += kMxT) {
-    const int s = e / (16 * MT * r_max), row = e / r_max % (16 * MT), r = e % r_max;
-    float v = 0.f;
-    if (r < s_lora[s][row].y) {
-      const float* const tp = g.t + (s0 + s) * g.t_site + (size_t)row * r_max + r;
-      for (int k = 0; k < g.parts; ++k) v += tp[k * g.t_part];
+  };
+  ask_x(0);
+#pragma unroll
+  for (int i = 0; i < kMxAhead; ++i) ask_w(i, c[i], sc[i]);
+  put_x(0);
+  ask_x(1);
+  barrier();
+  for (int i0 = 0; i0 < n_st; i0 += kMxAhead) {
+#pragma unroll
+    for (int u = 0; u < kMxAhead; ++u) {
+      if (i0 + u >= n_st) break;
+      if (active) stage(c[u], sc[u], u);
+      ask_w(i0 + u + kMxAhead, c[u], sc[u]);
+      put_x(u ^ 1);
+      ask_x(i0 + u + 2);
+      barrier();
     }
-    ts[e] = v;
   }
-
-  // ---- base linear ----
-  for (int b0 = w; b0 < full; b0 += kMxW * C::U) {
-    if (b0 != w) load(b0);
+  if (!active) return;
+  // (lane: row l % 32, registers 4 q .. + 3: columns 8 q + 4 (l / 32) ..)
+  float* const out = g.partial + ((size_t)(site * g.parts + part) * g.M + m0) * g.d2 + n0;
 #pragma unroll
-    for (int u = 0; u < C::U; ++u)
-      if (b0 + u * kMxW < full) {
-        u32x4 x[MT][4];
-        load_x(b0 + u * kMxW, x);
-        step(c[u], sc[u], x);
-      }
-  }
-  if ((d1 & 127) && w == full % kMxW) {  // the last groups: lanes past the end multiply zeros
-    const bool in = full * 128 + lq * 32 < d1;
-    u32x4 c1[NT], x1[MT][4];
-    uint32_t s1[NT];
+  for (int i = 0; i < RT; ++i) {
+    const int r = i * 32 + l32;
+    if (r >= rows) continue;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      c1[j] = u32x4{0u, 0u, 0u, 0u};
-      s1[j] = 127;
-      if (in) {
-        c1[j] = *reinterpret_cast<const u32x4*>(wp[j] + (size_t)full * 64);
-        s1[j] = sp[j][full * 4];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x1[i][k] = u32x4{0u, 0u, 0u, 0u};
-        if (in) x1[i][k] = *reinterpret_cast<const u32x4*>(xp[i] + (size_t)full * 128 + k * 8);
-      }
-    step(c1, s1, x1);
-  }
-  // (lane: row li, columns 4 lq .. + 3 of the 16)
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-      *reinterpret_cast<f32x4*>(red + ((size_t)w * 16 * MT + i * 16 + li) * C::Ld + j * 16 + lq * 4) = acc[i][j];
-  __syncthreads();
-
-  // ---- sums: two threads an output, four waves' parts and every other rank each ----
-  float val[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      float v = 0.f;
-#pragma unroll
-      for (int k = 0; k < kMxW / 2; ++k) v += red[((size_t)(half * (kMxW / 2) + k) * 16 * MT + i * 16 + m_out) * C::Ld + j * 16 + n_out];
-      if (rank[i][j] > 0) {
-        const float* const tr = ts + ((GATED ? j & 1 : 0) * 16 * MT + i * 16 + m_out) * r_max;
-#pragma unroll
-        for (int u = 0; u < C::Pre; ++u) {
-          const int r = 2 * u + half;
-          if (r < rank[i][j]) v += tr[r] * bf16_to_f32((bf16_t)pre[i][j][u]);
-        }
-        for (int r0 = 2 * C::Pre + half; r0 < rank[i][j]; r0 += 16) {
-          bf16_t b[8];
-#pragma unroll
-          for (int u = 0; u < 8; ++u) b[u] = ((gbf16*)bp[i][j])[(size_t)(r0 + 2 * u < rank[i][j] ? r0 + 2 * u : 0) * g.d2];
-#pragma unroll
-          for (int u = 0; u < 8; ++u)
-            if (r0 + 2 * u < rank[i][j]) v += tr[r0 + 2 * u] * bf16_to_f32(b[u]);
-        }
-      }
-      val[i][j] = v;
-    }
-  __syncthreads();
-  if (half == 1)
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) red[(i * 16 + m_out) * C::Ld + j * 16 + n_out] = val[i][j];
-  __syncthreads();
-  if (half == 1) return;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = i * 16 + m_out;
-    if (m >= g.M) continue;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) val[i][j] += red[m * C::Ld + j * 16 + n_out];
-    if constexpr (GATED) {
-#pragma unroll
-      for (int j = 0; j < NT; j += 2) {
-        const int n = n0 + j * 8 + n_out;
-        if (n >= g.d2) continue;
-        const float gate = val[i][j], up = val[i][j + 1];
-        const size_t at = (size_t)m * g.d2 + n;
-        if (g.gate_out) g.gate_out[at] = gate;
-        if (g.up_out) g.up_out[at] = up;
-        g.Y[0][(size_t)m * g.ldy + n] = f32_to_bf16(silu(gate) * up);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int n = n0 + j * 16 + n_out;
-        if (n >= g.d2) continue;
-        float v = val[i][j];
-        if (g.bias) v += bf16_to_f32(g.bias[n]);
-        const size_t at = (size_t)m * g.d2 + n;
-        if (g.res) {
-          v += bf16_to_f32(g.res[at]);
-          g.h_out[at] = v;
-        }
-        if (g.h_in) v += g.h_in[at];
-        if (g.Y[s0]) g.Y[s0][(size_t)m * g.ldy + n] = f32_to_bf16(v);
-      }
+    for (int q = 0; q < 4; ++q) {
+      const int n = q * 8 + lh * 4;
+      if (n0 + n < g.d2) *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
     }
   }
 }
 
-template <int MT, int NT, bool GATED>
-int launch_rows(const MxArgs& g, int sites, hipStream_t st) {
-  typedef MxCfg<MT, NT, GATED> C;
-  const int bytes = C::RedBytes + C::Sites * 16 * MT * g.ad.r_max * (int)sizeof(float);
+// ---- the first launch of up to 32 rows -------------------------------------------------------------------------------------
+// All of a workgroup's reduction at once: a wave takes 32 columns and NL steps of 64 inputs, every load of it and of its X on its way together;
+// KW waves share the columns and split a reduction of KW x NL x 64 inputs, so that few rows, whose X is small, need few parts or none.
+// Their sums meet in LDS.  The shrink's workgroups are of one row, site and 1024 inputs each; most rows have no term and end at once.
+constexpr int kShotShrinkK = 1024;
+
+template <int KW, int NL>
+__global__ void __launch_bounds__(kMxT, 4) mx4_shot_kernel(const MxBase g) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int d1 = g.d1;
+  int id = blockIdx.x;
+  const int shrinks = g.M * g.sites * g.shrink_parts;
+  if (id < shrinks) {
+    const ShrinkArgs& sh = g.shrink;
+    const int part = id % g.shrink_parts, m = id / g.shrink_parts % g.M, s = id / (g.shrink_parts * g.M), site = sh.site + s;
+    const int64_t req = sh.row_to_req ? (int64_t)sh.row_to_req[m] : m;
+    int ten = -1;
+    const int r = req >= 0 && req < sh.B ? routed_rank(sh.ad, sh.tenant_id, sh.route, (int)req, sh.B, site, &ten) : 0;
+    if (part == 0 && tid == 0) sh.row_lora[s * sh.lora_site + m] = int2{r ? ten : -1, r};
+    if (r == 0) return;
+    gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
+    const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
+    // lane: eight ranks (piece) of every kpl-th input of the wave's 128
+    const int pieces = (r + 7) >> 3;
+    int p2 = 1;
+    while (p2 < pieces) p2 <<= 1;
+    const int piece = lane & (p2 - 1), kpl = 64 / p2, left = r - piece * 8;
+    const int k0 = part * kShotShrinkK + w * (kShotShrinkK / kMxW), k1 = k0 + kShotShrinkK / kMxW < d1 ? k0 + kShotShrinkK / kMxW : d1;
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+    if (left > 0)
+      for (int k = k0 + lane / p2; k < k1; k += 8 * kpl) {
+        u32x4 a[8];
+        float xv[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int kk = k + u * kpl < k1 ? k + u * kpl : k;
+          gbf16* const q = A + (size_t)kk * r + piece * 8;
+          if (left >= 8) a[u] = *(gu32x4_any*)q;
+          else a[u] = load8(q, left, false);
+          xv[u] = bf16_to_f32(x[kk]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (k + u * kpl < k1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              sum[2 * e] += xv[u] * __uint_as_float(a[u][e] << 16);
+              sum[2 * e + 1] += xv[u] * __uint_as_float(a[u][e] & 0xffff0000u);
+            }
+      }
+    float* const red = reinterpret_cast<float*>(lds);  // [wave][256]
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      for (int off = p2; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
+      if (lane < p2) red[w * 256 + lane * 8 + e] = sum[e];
+    }
+    __syncthreads();
+    if (tid < r) {
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < kMxW; ++k) v += red[k * 256 + tid];
+      sh.t[s * sh.t_site + part * sh.t_stride + (size_t)m * sh.ad.r_max + tid] = v;
+    }
+    return;
+  }
+  id -= shrinks;
+  constexpr int kCols = kMxCols / KW, kPart = KW * NL * 64;  // columns and inputs of the workgroup
+  const int l32 = lane & 31, lh = lane >> 5, kw = w % KW, cw = w / KW;
+  const int part = id % g.parts, cg = id / g.parts % g.col_groups, site = id / (g.parts * g.col_groups);
+  const int n0 = cg * kCols + cw * 32, k_part = part * kPart, k0 = k_part + kw * NL * 64;
+  const int rows = g.M;
+
+  // ---- codes and scales: NL steps ----
+  u32x4 c[NL];
+  uint64_t sc[NL / 4];
+  {
+    typedef uint64_t u64_a1 __attribute__((aligned(1)));
+    int col = n0 + l32;
+    col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
+    const unsigned char* const wp = g.W[site] + (size_t)col * (d1 >> 1) + lh * 16 + (k0 >> 1);
+    const uint8_t* const sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5) + (k0 >> 5);
+    if (k0 + NL * 64 <= d1) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) c[i] = *reinterpret_cast<const u32x4*>(wp + i * 32);
+#pragma unroll
+      for (int i = 0; i < NL / 4; ++i) sc[i] = *reinterpret_cast<const u64_a1*>(sp + i * 8) >> (8 * lh);
+    } else {  // zeros past the end of the reduction
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        if (i % 4 == 0) sc[i / 4] = 0x007f007f007f007full;
+        const int at = k0 + i * 64 + lh * 32;
+        c[i] = u32x4{0u, 0u, 0u, 0u};
+        if (at < d1) {
+          c[i] = *reinterpret_cast<const u32x4*>(wp + i * 32);
+          sc[i / 4] = (sc[i / 4] & ~(0xffffull << (16 * (i & 3)))) | ((uint64_t)sp[i * 2 + lh] << (16 * (i & 3)));
+        }
+      }
+    }
+  }
+  // ---- X: [row][kPart], 16-byte pieces permuted by the row inside 512 bytes ----
+  constexpr int kPieces = kPart / 8;
+  for (int e0 = tid; e0 < rows * kPieces; e0 += kMxT * 4) {
+    u32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int e = e0 + u * kMxT, r = e / kPieces, p = e % kPieces;
+      x[u] = u32x4{0u, 0u, 0u, 0u};
+      if (r < rows && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(g.X + (size_t)r * g.ldx + k_part + p * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int e = e0 + u * kMxT, r = e / kPieces, p = e % kPieces;
+      if (r < rows) *reinterpret_cast<u32x4*>(lds + r * (kPart * 2) + ((p ^ (r & 31)) << 4)) = x[u];
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  f32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  if (n0 < g.d2 && k0 < d1) {
+    const int row = l32 < rows ? l32 : rows - 1;  // (rows past the end: results dropped)
+    const unsigned char* const xr = lds + row * (kPart * 2);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const float scale = mx4_scale((uint32_t)(sc[i / 4] >> (16 * (i & 3))) & 255u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int p = ((kw * NL + i) * 8 + lh * 4 + e) ^ (row & 31);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mx4_bf16(c[i][e], scale)),
+                                                      *reinterpret_cast<const bf16x8*>(xr + (p << 4)), acc, 0, 0, 0);
+      }
+    }
+  }
+  // ---- the waves' sums ----
+  __syncthreads();
+  constexpr int Ld = kMxCols + 4;  // a row of all waves' columns: [row][wave][32]
+  float* const red = reinterpret_cast<float*>(lds);
+  if (l32 < rows)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(red + l32 * Ld + w * 32 + q * 8 + lh * 4) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+  __syncthreads();
+  float* const out = g.partial + (size_t)(site * g.parts + part) * g.M * g.d2 + cg * kCols;
+  for (int e = tid; e < rows * (kCols / 4); e += kMxT) {
+    const int r = e / (kCols / 4), n = e % (kCols / 4) * 4;
+    if (cg * kCols + n >= g.d2) continue;
+    const float* const q = red + r * Ld + (n / 32) * KW * 32 + n % 32;
+    f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+    for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4*>(q + k * 32);
+    *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = v;
+  }
+}
+
+// ---- second launch: a workgroup takes 256 columns of a row (GATED: of both projections), its four waves a quarter of the parts and of the
+// ranks each, so that everything a row needs is on its way together ----
+constexpr int kFinT = 256, kFinCols = 256;
+struct MxFinish {
+  MxArgs a;
+  int parts;
+  const float* partial;
+  const float* t;  // [site][t_parts][M][r_max]
+  size_t t_part, t_site;
+  int t_parts;
+  const int2* row_lora;  // [site][M]
+};
+typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x2_a8 __attribute__((ext_vector_type(2)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+template <bool GATED>
+__global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) {
+  constexpr int kSites = GATED ? 2 : 1;
+  __shared__ float ts[kSites][MILORA_MAX_RANK];
+  __shared__ float ss[kFinT / 64];
+  __shared__ f32x4 red[kFinT / 64][kSites][64];
+  const MxArgs& g = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m = blockIdx.y, s0 = GATED ? 0 : blockIdx.z;
+  const int n = blockIdx.x * kFinCols + lane * 4;
+  const bool in = n < g.d2;
+  int2 tr[kSites];
+#pragma unroll
+  for (int s = 0; s < kSites; ++s) tr[s] = f.row_lora[(size_t)(s0 + s) * g.M + m];
+  // ---- this wave's parts ----
+  f32x4 v[kSites];
+#pragma unroll
+  for (int s = 0; s < kSites; ++s) {
+    v[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const size_t stride = (size_t)g.M * g.d2;
+    const float* const q = f.partial + ((size_t)(s0 + s) * f.parts * g.M + m) * g.d2 + (in ? n : 0);
+    for (int p = w; p < f.parts; p += 16) {
+      f32x4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const f32x4*>(q + (p + 4 * u < f.parts ? p + 4 * u : p) * stride);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (p + 4 * u < f.parts) v[s] += x[u];
+    }
+  }
+  // ---- normalisation of the level's input: a factor of the row, applied to its products ----
+  const bool norm = g.norm_x || g.norm_h;
+  if (norm) {
+    float sum = 0.f;
+    if (g.norm_x) {
+      const bf16_t* const x = g.norm_x + (size_t)m * g.d1;
+      for (int i = tid * 8; i < g.d1; i += kFinT * 8) {
+        const u32x4 q = *reinterpret_cast<const u32x4*>(x + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float a = __uint_as_float(q[e] << 16), b = __uint_as_float(q[e] & 0xffff0000u);
+          sum += a * a + b * b;
+        }
+      }
+    } else {
+      const float* const h = g.norm_h + (size_t)m * g.d1;
+      for (int i = tid * 4; i < g.d1; i += kFinT * 4) {
+        const f32x4 q = *reinterpret_cast<const f32x4*>(h + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += q[e] * q[e];
+      }
+    }
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (lane == 0) ss[w] = sum;
+  }
+  // ---- LoRA: t of the row, this wave's ranks of W^B ----
+  const bool lora = tr[0].y || tr[kSites - 1].y;
+  if (lora) {
+    gbf16* b[kSites];
+#pragma unroll
+    for (int s = 0; s < kSites; ++s)
+      b[s] = tr[s].y ? in_global(g.ad.B[tr[s].x * MILORA_NUM_SITES + g.site[s0] + s]) + (in ? n : 0) : nullptr;
+#pragma unroll
+    for (int s = 0; s < kSites; ++s)
+      if (tid < tr[s].y) {
+        const float* const tp = f.t + (s0 + s) * f.t_site + (size_t)m * g.ad.r_max + tid;
+        float x = 0.f;
+        for (int p = 0; p < f.t_parts; p += 4) {
+          float q[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) q[u] = tp[(p + u < f.t_parts ? p + u : p) * f.t_part];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (p + u < f.t_parts) x += q[u];
+        }
+        ts[s][tid] = x;
+      }
+    constexpr int kU = 8;
+    u32x2_a2 first[kSites][kU];
+#pragma unroll
+    for (int s = 0; s < kSites; ++s)
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int c = w + 4 * u;
+        if (tr[s].y) first[s][u] = *(__attribute__((address_space(1))) const u32x2_a2*)(b[s] + (size_t)(c < tr[s].y ? c : 0) * g.d2);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kSites; ++s) {
+      const int r = tr[s].y;
+      auto add = [&](int c, u32x2_a2 x) __attribute__((always_inline)) {
+        if (c >= r) return;
+        const float t = ts[s][c];
+        v[s][0] += t * __uint_as_float(x[0] << 16);
+        v[s][1] += t * __uint_as_float(x[0] & 0xffff0000u);
+        v[s][2] += t * __uint_as_float(x[1] << 16);
+        v[s][3] += t * __uint_as_float(x[1] & 0xffff0000u);
+      };
+      if (r)
+#pragma unroll
+        for (int u = 0; u < kU; ++u) add(w + 4 * u, first[s][u]);
+      for (int c0 = w + 4 * kU; c0 < r; c0 += 4 * kU) {
+        u32x2_a2 x[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) x[u] = *(__attribute__((address_space(1))) const u32x2_a2*)(b[s] + (size_t)(c0 + 4 * u < r ? c0 + 4 * u : 0) * g.d2);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) add(c0 + 4 * u, x[u]);
+      }
+    }
+  }
+  // ---- glue, by the first wave ----
+#pragma unroll
+  for (int s = 0; s < kSites; ++s) red[w][s][lane] = v[s];
+  __syncthreads();
+  if (w || !in) return;
+#pragma unroll
+  for (int s = 0; s < kSites; ++s) v[s] = (red[0][s][lane] + red[1][s][lane]) + (red[2][s][lane] + red[3][s][lane]);
+  if (norm) {
+    const float inv = rsqrtf((ss[0] + ss[1] + ss[2] + ss[3]) / (float)g.d1 + 1e-5f);
+#pragma unroll
+    for (int s = 0; s < kSites; ++s) v[s] *= inv;
+  }
+  const size_t at = (size_t)m * g.d2 + n;
+  f32x4 y;
+  if constexpr (GATED) {
+    if (g.gate_out) *reinterpret_cast<f32x4_a4*>(g.gate_out + at) = v[0];
+    if (g.up_out) *reinterpret_cast<f32x4_a4*>(g.up_out + at) = v[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = silu(v[0][e]) * v[1][e];
+  } else {
+    y = v[0];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (g.bias) y[e] += bf16_to_f32(g.bias[n + e]);
+      if (g.res) y[e] += bf16_to_f32(g.res[at + e]);
+    }
+    if (g.res) *reinterpret_cast<f32x4*>(g.h_out + at) = y;
+    if (g.h_in) y += *reinterpret_cast<const f32x4*>(g.h_in + at);
+  }
+  u32x2_a8 o;
+  o[0] = pack_bf16x2(y[0], y[1]);
+  o[1] = pack_bf16x2(y[2], y[3]);
+  *reinterpret_cast<u32x2_a8*>(g.Y[s0] + (size_t)m * g.ldy + n) = o;
+}
+
+template <int KW, int NL>
+int launch_shot(const MxBase& b, hipStream_t st) {
+  constexpr int kPart = KW * NL * 64, kRed = 32 * (kMxCols + 4) * 4;
+  const int x = b.M * kPart * 2, red = b.M * (kMxCols + 4) * 4;
+  int bytes = x > red ? x : red;
+  if (bytes < kMxW * 256 * 4) bytes = kMxW * 256 * 4;  // (the shrink's sums)
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    const int most = C::RedBytes + C::Sites * 16 * MT * MILORA_MAX_RANK * (int)sizeof(float);
-    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_rows_kernel<MT, NT, GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, most));
+    const int most = 32 * kPart * 2 > kRed ? 32 * kPart * 2 : kRed;
+    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_shot_kernel<KW, NL>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
     lds_set_for = dev;
   }
-  constexpr int kCols = GATED ? NT * 8 : NT * 16;
-  hipLaunchKernelGGL((mx4_rows_kernel<MT, NT, GATED>), dim3((unsigned)((g.d2 + kCols - 1) / kCols), GATED ? 1 : sites), dim3(kMxT), bytes, st, g);
+  const int64_t grid = (int64_t)b.M * b.sites * b.shrink_parts + (int64_t)b.sites * b.col_groups * b.parts;
+  if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
+  hipLaunchKernelGGL((mx4_shot_kernel<KW, NL>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
   return check_launch();
+}
+
+template <int RT>
+int launch_base(const MxBase& b, hipStream_t st) {
+  constexpr int kX = kMxAhead * 32 * RT * kMxK * 2, kShrink = kMxW * kShrinkWaveBytes;
+  constexpr int kBytes = kX > kShrink ? kX : kShrink;
+  static thread_local int lds_set_for = -1;
+  int dev = 0;
+  MILORA_HIP(hipGetDevice(&dev));
+  if (lds_set_for != dev) {
+    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<RT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes));
+    lds_set_for = dev;
+  }
+  const int64_t grid = (int64_t)b.shrink_blocks * b.shrink_parts * b.shrink_z + (int64_t)b.sites * b.col_groups * b.row_groups * b.parts;
+  if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
+  hipLaunchKernelGGL(mx4_base_kernel<RT>, dim3((unsigned)grid), dim3(kMxT), kBytes, st, b);
+  return check_launch();
+}
+
+// How the first launch cuts a call; a function of the sizes alone, shared by the launch and the workspace's sizing.
+// Up to 32 rows (kw > 0): waves that share columns, steps of a wave: X of a workgroup is M x kw x nl x 128 bytes, 64 KB at most, and as few
+// parts as that allows.  Beyond (kw = 0): 32 rt rows a workgroup, parts that make the workgroups fill the chip, two stages each at least.
+struct MxPlan {
+  int kw, nl, rt, parts, stages;
+};
+constexpr int kMxPartsMax = 16;
+int mx4_parts_max(int d1) {
+  const int n = (d1 + kMxK - 1) / kMxK / 2;
+  return n < 1 ? 1 : n < kMxPartsMax ? n : kMxPartsMax;
+}
+constexpr int kShotRows = 32;
+int shot_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
+int shot_parts(int64_t M, int d1) { return (d1 + shot_waves(M) * 512 - 1) / (shot_waves(M) * 512); }
+MxPlan mx4_plan(int64_t M, int d1, int d2, int sites) {
+  MxPlan p{};
+  if (M <= kShotRows) {
+    p.kw = shot_waves(M);
+    p.nl = 8;
+    p.parts = shot_parts(M, d1);
+    return p;
+  }
+  p.rt = M <= 64 ? 2 : 4;
+  const int all = (d1 + kMxK - 1) / kMxK;
+  const int64_t units = (int64_t)sites * ((d2 + kMxCols - 1) / kMxCols) * ((M + 32 * p.rt - 1) / (32 * p.rt));
+  int64_t parts = (p.rt > 2 ? 256 : 512) / units;
+  parts = parts < 1 ? 1 : parts > mx4_parts_max(d1) ? mx4_parts_max(d1) : parts;
+  p.stages = (int)((all + parts - 1) / parts);
+  p.parts = (all + p.stages - 1) / p.stages;
+  return p;
+}
+// The most partial sums (floats) of a call of up to these sizes; no size lowers it.
+size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
+  const size_t D = (size_t)sites * d2;
+  const int64_t few = M < kShotRows ? M : kShotRows;
+  size_t n = (size_t)few * D * shot_parts(few, d1);
+  if (few > 16 && (size_t)16 * D * shot_parts(16, d1) > n) n = (size_t)16 * D * shot_parts(16, d1);
+  if (few > 8 && (size_t)8 * D * shot_parts(8, d1) > n) n = (size_t)8 * D * shot_parts(8, d1);
+  if (M > kShotRows) {
+    const size_t most = (size_t)mx4_parts_max(d1) * M * D, cap = (size_t)(M <= 64 ? 512 * 64 : 256 * 128) * kMxCols + (size_t)M * D;
+    const size_t k = most < cap ? most : cap;
+    n = k > n ? k : n;
+  }
+  return n;
+}
+// Parts of the shrink: 1024 inputs each (few rows), or those of the matrix-core shrink.
+int mx4_shrink_parts(int64_t M, int d1) { return M <= kShotRows ? (d1 + kShotShrinkK - 1) / kShotShrinkK : shrink_parts(M, d1); }
+size_t mx4_shrink_floats(int64_t M, int d1) {
+  const int64_t few = M < kShotRows ? M : kShotRows;
+  const size_t a = (size_t)few * mx4_shrink_parts(few, d1), b = M > kShotRows ? shrink_rows_bound(M, d1) : 0;
+  return a > b ? a : b;
 }
 
 // Groups of eight of one launch: a grid has to stay below 2^32 threads.
@@ -437,9 +753,45 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
   return rc;
 }
 
-int launch_mx4_rows(const MxArgs& g, int sites, bool gated, hipStream_t st) {
-  if (g.M <= 16) return gated ? launch_rows<1, 2, true>(g, 1, st) : launch_rows<1, 1, false>(g, sites, st);
-  return gated ? launch_rows<2, 2, true>(g, 1, st) : launch_rows<2, 2, false>(g, sites, st);
+size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites) {
+  return align_up(mx4_shrink_floats(M, d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256) +
+         align_up(mx4_partial_floats(M, d1, d2, sites) * sizeof(float), 256);
+}
+
+int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st) {
+  if (g.M > 65535) return MILORA_ERANGE;
+  const int r_max = g.ad.r_max, t_parts = mx4_shrink_parts(g.M, g.d1);
+  float* const t = (float*)workspace;
+  int2* const lora = (int2*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
+  float* const partial = (float*)((char*)lora + align_up((size_t)g.M * sites * sizeof(int2), 256));
+  const MxPlan pl = mx4_plan(g.M, g.d1, g.d2, sites);
+  MxBase b{};
+  b.X = g.X; b.ldx = g.ldx; b.M = g.M; b.d1 = g.d1; b.d2 = g.d2;
+  for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
+  b.sites = sites;
+  b.parts = pl.parts;
+  b.stages = pl.stages;
+  b.partial = partial;
+  b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, lora, nullptr,
+                        sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
+  b.shrink_parts = t_parts;
+  int rc;
+  if (pl.kw) {
+    b.col_groups = (g.d2 + kMxCols / pl.kw - 1) / (kMxCols / pl.kw);
+    rc = pl.kw == 8 ? launch_shot<8, 8>(b, st) : pl.kw == 4 ? launch_shot<4, 8>(b, st) : launch_shot<2, 8>(b, st);
+  } else {
+    b.col_groups = (g.d2 + kMxCols - 1) / kMxCols;
+    b.row_groups = (g.M + 32 * pl.rt - 1) / (32 * pl.rt);
+    b.shrink_blocks = (g.M + 15) / 16;
+    b.shrink_z = sites * shrink_shares(b.shrink_blocks, t_parts, sites, g.B, g.ad);
+    rc = pl.rt == 2 ? launch_base<2>(b, st) : launch_base<4>(b, st);
+  }
+  if (rc) return rc;
+  MxFinish f{g, pl.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, lora};
+  const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
+  if (gated) hipLaunchKernelGGL(mx4_finish_kernel<true>, grid, dim3(kFinT), 0, st, f);
+  else hipLaunchKernelGGL(mx4_finish_kernel<false>, grid, dim3(kFinT), 0, st, f);
+  return check_launch();
 }
 
 }  // namespace milora

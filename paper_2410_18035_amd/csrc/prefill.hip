@@ -812,14 +812,8 @@ static int launch_shrinks(ShrinkArgs g, bool trans, hipStream_t stream) {
     g.t = all.t + (size_t)r0 * g.ad.r_max;
     g.row_lora = all.row_lora ? all.row_lora + r0 : nullptr;
     if (M <= kTileMaxRows) {
-      // Workgroups share the units of a block (32 ranks of a tenant each) while there can be units for them and all are resident
-      // at once, two per compute unit.  64 packed rows of 64 tenants, rank 256, 4096 x 4096, a call: 189 us with four at
-      // most, 87 so; 45 rows of one request have one unit a block, and no workgroup comes for nothing.
       const int64_t blocks = (g.M + 15) / 16;
-      const int tenants = g.B < g.ad.n_tenants ? g.B : g.ad.n_tenants;
-      const int units = (tenants < 16 ? tenants : 16) * ((g.ad.r_max + kShrinkC - 1) / kShrinkC);
-      int shares = 1;
-      while (shares < units && blocks * parts * g.sites * shares * 2 <= 512) shares *= 2;
+      const int shares = shrink_shares(blocks, parts, g.sites, g.B, g.ad);
       launch_shrink_block<1>(g, dim3((unsigned)blocks, parts, shares * g.sites), trans, stream);
     }
     else
