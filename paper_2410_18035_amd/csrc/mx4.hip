@@ -134,246 +134,130 @@ __global__ void __launch_bounds__(kQuantT) mx4_dequantize_kernel(const uint32_t*
 }
 
 // ---- few rows: two launches a level -----------------------------------------------------------------------------------------
-// First launch: the base products and the LoRA shrinks, which do not depend on each other.  A workgroup of eight waves takes 256 columns (32 a wave),
-// 32 RT rows and one part of the reduction, in stages of 256 inputs.  A lane holds one group of 32 inputs of one column: 16
-// bytes of codes straight from global memory, two stages on their way; the rows of X go through LDS, shared by the waves, two buffers.  Four
-// matrix instructions of 8 inputs a lane multiply 64 inputs (which inputs stand at which place does not matter as long as both operands agree).
-// The sums of a part go to memory in fp32.  The workgroups in front of those are the shrink's (shrink.h).
+// First launch: the base products and the LoRA shrinks, which do not depend on each other.  A workgroup of eight waves takes 256 / KW columns, 32 a
+// wave, and KW x NL x 64 inputs, all of them at once: a lane holds one group of 32 inputs of one column for each of NL steps, 16 bytes of codes straight
+// from global memory, every load on its way together; KW waves share the columns and split the inputs, so that few rows, whose X is small, need few
+// parts of the reduction or none.  X goes through LDS, 32 rows at a time; with more rows the codes stay in registers and the next rows' X is on its
+// way while these are multiplied.  Four matrix instructions of 8 inputs a lane multiply 64 inputs (which inputs stand at which place does not
+// matter as long as both operands agree).  The waves' sums meet in LDS, those of the parts in memory, in fp32.
 // Second launch: adds the parts in part order, the LoRA term t W^B, bias and glue, and rounds once.
-// Bound: the stream of the codes; many workgroups with short reductions keep it in flight, at the price of their sums' way through memory.
+// Bound: the stream of the codes; what short reductions cost is their sums' way through memory.  Tried: stages of 256 inputs with the next ones on
+// their way over a longer reduction (M = 64, 4096 x 4096: 23 us a call against 15), the whole reduction and the term in one launch with 2 x 8
+// waves a compute unit (gated, 32 rows of 4096 x 11008: 60 us against 28).
 constexpr int kMxW = 8;
 constexpr int kMxT = kMxW * 64;
 constexpr int kMxCols = kMxW * 32;
-constexpr int kMxK = 256;    // inputs of a stage
-constexpr int kMxAhead = 2;  // stages of codes on their way, and buffers of X
 
 struct MxBase {
   const bf16_t* X;
   int64_t ldx;
   int M, d1, d2;
   const unsigned char* W[3];
-  int sites, col_groups, row_groups, parts, stages;  // stages of a part
+  int sites, col_groups, row_groups, row_split, parts;  // row groups of 32; a workgroup takes every row_split-th
   float* partial;  // [site][part][M][d2]
-  int shrink_blocks, shrink_parts, shrink_z;         // workgroups of the shrink: row blocks x parts x (sites x shares)
+  int shrink_parts, shrink_z;  // the shrink: parts of a row, workgroups in all (a multiple of 8)
   ShrinkArgs shrink;
 };
 
-template <int RT>
-__global__ void __launch_bounds__(kMxT, RT > 2 ? 2 : 4) mx4_base_kernel(const MxBase g) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int tid = threadIdx.x;
-  int id = blockIdx.x;
-  const int shrinks = g.shrink_blocks * g.shrink_parts * g.shrink_z;
-  if (id < shrinks) {
-    __shared__ int row_ten[32];
-    const int block = id % g.shrink_blocks, part = id / g.shrink_blocks % g.shrink_parts, z = id / (g.shrink_blocks * g.shrink_parts);
-    const int shares = g.shrink_z / g.shrink.sites, s = z / shares;
-    ShrinkArgs one = g.shrink;
-    one.site += s;
-    one.t += s * one.t_site;
-    one.row_lora += s * one.lora_site;
-    shrink_block<1, kMxW, true, true>(one, block, part, g.shrink_parts, z % shares, shares, lds, row_ten, [](float* p, float v) { *p = v; });
-    return;
-  }
-  id -= shrinks;
-  const int lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
+constexpr int kMxShrinkK = 1024;
+// Workgroup `id` of those in front: the shrink of one row, site and 1024 inputs; most rows have no term and end at once.
+__device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned char* lds) {
+  const ShrinkArgs& sh = g.shrink;
+  const int tid = threadIdx.x, lane = tid & 63, d1 = g.d1;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rg = id % g.row_groups, part = id / g.row_groups % g.parts, cg = id / (g.row_groups * g.parts) % g.col_groups,
-            site = id / (g.row_groups * g.parts * g.col_groups);
-  const int m0 = rg * 32 * RT, rows = g.M - m0 < 32 * RT ? g.M - m0 : 32 * RT;
-  const int n0 = cg * kMxCols + w * 32, d1 = g.d1;
-  const bool active = n0 < g.d2;  // (a wave without columns helps with X)
-  const int all = (d1 + kMxK - 1) / kMxK, st0 = part * g.stages, n_st = all - st0 < g.stages ? all - st0 : g.stages;
-
-  const unsigned char* wp;
-  const uint8_t* sp;
-  {
-    int col = n0 + l32;
-    col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
-    wp = g.W[site] + (size_t)col * (d1 >> 1) + lh * 16;
-    sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5);
-  }
-  typedef uint64_t u64_a1 __attribute__((aligned(1)));
-  u32x4 c[kMxAhead][4];
-  uint64_t sc[kMxAhead];
-  auto ask_w = [&](int i, u32x4 (&cv)[4], uint64_t& sv) __attribute__((always_inline)) {
-    const int st = st0 + (i < n_st ? i : n_st - 1);
-    if (!active) return;
-    if ((st + 1) * kMxK <= d1) {
+  if (id >= g.M * g.sites * g.shrink_parts) return;
+  const int part = id % g.shrink_parts, m = id / g.shrink_parts % g.M, s = id / (g.shrink_parts * g.M), site = sh.site + s;
+  const int64_t req = sh.row_to_req ? (int64_t)sh.row_to_req[m] : m;
+  int ten = -1;
+  const int r = req >= 0 && req < sh.B ? routed_rank(sh.ad, sh.tenant_id, sh.route, (int)req, sh.B, site, &ten) : 0;
+  if (part == 0 && tid == 0) sh.row_lora[s * sh.lora_site + m] = int2{r ? ten : -1, r};
+  if (r == 0) return;
+  gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
+  const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
+  // lane: eight ranks (piece) of every kpl-th input of the wave's 128
+  const int pieces = (r + 7) >> 3;
+  int p2 = 1;
+  while (p2 < pieces) p2 <<= 1;
+  const int piece = lane & (p2 - 1), kpl = 64 / p2, left = r - piece * 8;
+  const int k0 = part * kMxShrinkK + w * (kMxShrinkK / kMxW), k1 = k0 + kMxShrinkK / kMxW < d1 ? k0 + kMxShrinkK / kMxW : d1;
+  float sum[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) cv[k] = *reinterpret_cast<const u32x4*>(wp + (size_t)st * (kMxK / 2) + k * 32);
-      sv = *reinterpret_cast<const u64_a1*>(sp + st * (kMxK / 32)) >> (8 * lh);
-    } else {  // the last stage: zeros past the end of the reduction
-      sv = 0x007f007f007f007full;
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  if (left > 0)
+    for (int k = k0 + lane / p2; k < k1; k += 8 * kpl) {
+      u32x4 a[8];
+      float xv[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int at = st * kMxK + k * 64 + lh * 32;
-        cv[k] = u32x4{0u, 0u, 0u, 0u};
-        if (at < d1) {
-          cv[k] = *reinterpret_cast<const u32x4*>(wp + (size_t)st * (kMxK / 2) + k * 32);
-          sv = (sv & ~(0xffffull << (16 * k))) | ((uint64_t)sp[at >> 5] << (16 * k));
-        }
+      for (int u = 0; u < 8; ++u) {
+        const int kk = k + u * kpl < k1 ? k + u * kpl : k;
+        gbf16* const q = A + (size_t)kk * r + piece * 8;
+        if (left >= 8) a[u] = *(gu32x4_any*)q;
+        else a[u] = load8(q, left, false);
+        xv[u] = bf16_to_f32(x[kk]);
       }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (k + u * kpl < k1)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sum[2 * e] += xv[u] * __uint_as_float(a[u][e] << 16);
+            sum[2 * e + 1] += xv[u] * __uint_as_float(a[u][e] & 0xffff0000u);
+          }
     }
-  };
-  // X: thread -> 16-byte piece tid % 32 of rows tid / 32 + 16 i of a stage's 512 bytes a row; pieces permuted by the row so that an
-  // operand read of neighbouring rows at one piece hits different banks
-  constexpr int kXRows = 2 * RT;
-  constexpr int kXBytes = 32 * RT * kMxK * 2;
-  const int piece = tid & 31, xr0 = tid >> 5;
-  const bf16_t* const xb = g.X + (size_t)m0 * g.ldx + piece * 8;
-  u32x4 x[kXRows];
-  auto ask_x = [&](int i) __attribute__((always_inline)) {
-    const int st = st0 + (i < n_st ? i : n_st - 1);
-    const bool in = st * kMxK + piece * 8 < d1;
+  float* const red = reinterpret_cast<float*>(lds);  // [wave][256]
 #pragma unroll
-    for (int k = 0; k < kXRows; ++k) {
-      const int r = xr0 + 16 * k;
-      x[k] = u32x4{0u, 0u, 0u, 0u};
-      if (in && r < rows) x[k] = *reinterpret_cast<const u32x4*>(xb + (size_t)r * g.ldx + st * kMxK);
-    }
-  };
-  auto put_x = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < kXRows; ++k) {
-      const int r = xr0 + 16 * k;
-      if (r < rows) *reinterpret_cast<u32x4*>(lds + buf * kXBytes + r * (kMxK * 2) + ((piece ^ (r & 31)) << 4)) = x[k];
-    }
-  };
-  f32x16 acc[RT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-  auto barrier = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS reads and writes done; what is on its way from memory stays so
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  auto stage = [&](const u32x4 (&cv)[4], uint64_t sv, int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float scale = mx4_scale((uint32_t)(sv >> (16 * k)) & 255u);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_bf16(cv[k][e], scale));
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          const int at = (k * 8 + lh * 4 + e) ^ l32;
-          const bf16x8 xv = *reinterpret_cast<const bf16x8*>(lds + buf * kXBytes + (i * 32 + l32) * (kMxK * 2) + (at << 4));
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv, acc[i], 0, 0, 0);
-        }
-      }
-    }
-  };
-  ask_x(0);
-#pragma unroll
-  for (int i = 0; i < kMxAhead; ++i) ask_w(i, c[i], sc[i]);
-  put_x(0);
-  ask_x(1);
-  barrier();
-  for (int i0 = 0; i0 < n_st; i0 += kMxAhead) {
-#pragma unroll
-    for (int u = 0; u < kMxAhead; ++u) {
-      if (i0 + u >= n_st) break;
-      if (active) stage(c[u], sc[u], u);
-      ask_w(i0 + u + kMxAhead, c[u], sc[u]);
-      put_x(u ^ 1);
-      ask_x(i0 + u + 2);
-      barrier();
-    }
+  for (int e = 0; e < 8; ++e) {
+    for (int off = p2; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
+    if (lane < p2) red[w * 256 + lane * 8 + e] = sum[e];
   }
-  if (!active) return;
-  // (lane: row l % 32, registers 4 q .. + 3: columns 8 q + 4 (l / 32) ..)
-  float* const out = g.partial + ((size_t)(site * g.parts + part) * g.M + m0) * g.d2 + n0;
+  __syncthreads();
+  if (tid < r) {
+    float v = 0.f;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int r = i * 32 + l32;
-    if (r >= rows) continue;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = q * 8 + lh * 4;
-      if (n0 + n < g.d2) *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
-    }
+    for (int k = 0; k < kMxW; ++k) v += red[k * 256 + tid];
+    sh.t[s * sh.t_site + part * sh.t_stride + (size_t)m * sh.ad.r_max + tid] = v;
   }
 }
 
-// ---- the first launch of up to 32 rows -------------------------------------------------------------------------------------
-// All of a workgroup's reduction at once: a wave takes 32 columns and NL steps of 64 inputs, every load of it and of its X on its way together;
-// KW waves share the columns and split a reduction of KW x NL x 64 inputs, so that few rows, whose X is small, need few parts or none.
-// Their sums meet in LDS.  The shrink's workgroups are of one row, site and 1024 inputs each; most rows have no term and end at once.
-constexpr int kShotShrinkK = 1024;
-
-template <int KW, int NL>
-__global__ void __launch_bounds__(kMxT, 4) mx4_shot_kernel(const MxBase g) {
+// MORE: more than 32 rows.
+template <int KW, int NL, bool MORE>
+__global__ void __launch_bounds__(kMxT, 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d1 = g.d1;
   int id = blockIdx.x;
-  const int shrinks = g.M * g.sites * g.shrink_parts;
-  if (id < shrinks) {
-    const ShrinkArgs& sh = g.shrink;
-    const int part = id % g.shrink_parts, m = id / g.shrink_parts % g.M, s = id / (g.shrink_parts * g.M), site = sh.site + s;
-    const int64_t req = sh.row_to_req ? (int64_t)sh.row_to_req[m] : m;
-    int ten = -1;
-    const int r = req >= 0 && req < sh.B ? routed_rank(sh.ad, sh.tenant_id, sh.route, (int)req, sh.B, site, &ten) : 0;
-    if (part == 0 && tid == 0) sh.row_lora[s * sh.lora_site + m] = int2{r ? ten : -1, r};
-    if (r == 0) return;
-    gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
-    const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
-    // lane: eight ranks (piece) of every kpl-th input of the wave's 128
-    const int pieces = (r + 7) >> 3;
-    int p2 = 1;
-    while (p2 < pieces) p2 <<= 1;
-    const int piece = lane & (p2 - 1), kpl = 64 / p2, left = r - piece * 8;
-    const int k0 = part * kShotShrinkK + w * (kShotShrinkK / kMxW), k1 = k0 + kShotShrinkK / kMxW < d1 ? k0 + kShotShrinkK / kMxW : d1;
-    float sum[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-    if (left > 0)
-      for (int k = k0 + lane / p2; k < k1; k += 8 * kpl) {
-        u32x4 a[8];
-        float xv[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int kk = k + u * kpl < k1 ? k + u * kpl : k;
-          gbf16* const q = A + (size_t)kk * r + piece * 8;
-          if (left >= 8) a[u] = *(gu32x4_any*)q;
-          else a[u] = load8(q, left, false);
-          xv[u] = bf16_to_f32(x[kk]);
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (k + u * kpl < k1)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              sum[2 * e] += xv[u] * __uint_as_float(a[u][e] << 16);
-              sum[2 * e + 1] += xv[u] * __uint_as_float(a[u][e] & 0xffff0000u);
-            }
-      }
-    float* const red = reinterpret_cast<float*>(lds);  // [wave][256]
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      for (int off = p2; off < 64; off <<= 1) sum[e] += __shfl_xor(sum[e], off, 64);
-      if (lane < p2) red[w * 256 + lane * 8 + e] = sum[e];
-    }
-    __syncthreads();
-    if (tid < r) {
-      float v = 0.f;
-#pragma unroll
-      for (int k = 0; k < kMxW; ++k) v += red[k * 256 + tid];
-      sh.t[s * sh.t_site + part * sh.t_stride + (size_t)m * sh.ad.r_max + tid] = v;
-    }
+  if (id < g.shrink_z) {
+    mx4_shrink_row(g, id, lds);
     return;
   }
-  id -= shrinks;
+  // workgroup -> tile: ids go round-robin over the 8 XCDs (those in front are a multiple of 8); with more than 32 rows an XCD takes a contiguous
+  // run of an order in which the workgroups of the same codes follow one another, so that its L2 serves them after the first
+  id -= g.shrink_z;
+  const int row_split = MORE ? g.row_split : 1;
+  const int total = g.sites * g.col_groups * row_split * g.parts, per = (total + 7) >> 3;
+  if (MORE) id = (id & 7) * per + (id >> 3);
+  if (id >= total) return;
   constexpr int kCols = kMxCols / KW, kPart = KW * NL * 64;  // columns and inputs of the workgroup
+  constexpr int kPitch = kPart * 2 + 16;                     // a row of X in LDS: 16 bytes past a multiple of all banks
   const int l32 = lane & 31, lh = lane >> 5, kw = w % KW, cw = w / KW;
-  const int part = id % g.parts, cg = id / g.parts % g.col_groups, site = id / (g.parts * g.col_groups);
+  int rg = id % row_split;
+  const int part = id / row_split % g.parts, cg = id / (row_split * g.parts) % g.col_groups, site = id / (row_split * g.parts * g.col_groups);
   const int n0 = cg * kCols + cw * 32, k_part = part * kPart, k0 = k_part + kw * NL * 64;
-  const int rows = g.M;
 
+  // ---- X: [row][kPart], asked for in front of the codes, which may come later ----
+  constexpr int kPieces = kPart / 8, kXMost = 8;  // (rows x kPieces is kXMost x kMxT at most: MxPlan)
+  u32x4 x[kXMost];
+  auto ask_x = [&](int m0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kXMost; ++u) {
+      const int e = tid + u * kMxT, m = m0 + e / kPieces, p = e % kPieces;
+      x[u] = u32x4{0u, 0u, 0u, 0u};
+      if (e < 32 * kPieces && m < g.M && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(g.X + (size_t)m * g.ldx + k_part + p * 8);
+    }
+  };
+  ask_x(rg * 32);
+  __builtin_amdgcn_sched_barrier(0);
   // ---- codes and scales: NL steps ----
   u32x4 c[NL];
   uint64_t sc[NL / 4];
@@ -401,60 +285,59 @@ __global__ void __launch_bounds__(kMxT, 4) mx4_shot_kernel(const MxBase g) {
       }
     }
   }
-  // ---- X: [row][kPart], 16-byte pieces permuted by the row inside 512 bytes ----
-  constexpr int kPieces = kPart / 8;
-  for (int e0 = tid; e0 < rows * kPieces; e0 += kMxT * 4) {
-    u32x4 x[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int e = e0 + u * kMxT, r = e / kPieces, p = e % kPieces;
-      x[u] = u32x4{0u, 0u, 0u, 0u};
-      if (r < rows && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(g.X + (size_t)r * g.ldx + k_part + p * 8);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int e = e0 + u * kMxT, r = e / kPieces, p = e % kPieces;
-      if (r < rows) *reinterpret_cast<u32x4*>(lds + r * (kPart * 2) + ((p ^ (r & 31)) << 4)) = x[u];
-    }
-  }
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  f32x16 acc;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  if (n0 < g.d2 && k0 < d1) {
-    const int row = l32 < rows ? l32 : rows - 1;  // (rows past the end: results dropped)
-    const unsigned char* const xr = lds + row * (kPart * 2);
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const float scale = mx4_scale((uint32_t)(sc[i / 4] >> (16 * (i & 3))) & 255u);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int p = ((kw * NL + i) * 8 + lh * 4 + e) ^ (row & 31);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mx4_bf16(c[i][e], scale)),
-                                                      *reinterpret_cast<const bf16x8*>(xr + (p << 4)), acc, 0, 0, 0);
-      }
-    }
-  }
-  // ---- the waves' sums ----
-  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+  auto barrier = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS reads and writes done; what is on its way from memory stays so
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
   constexpr int Ld = kMxCols + 4;  // a row of all waves' columns: [row][wave][32]
   float* const red = reinterpret_cast<float*>(lds);
-  if (l32 < rows)
+  for (;;) {
+    const int m0 = rg * 32, rows = g.M - m0 < 32 ? g.M - m0 : 32;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4*>(red + l32 * Ld + w * 32 + q * 8 + lh * 4) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
-  __syncthreads();
-  float* const out = g.partial + (size_t)(site * g.parts + part) * g.M * g.d2 + cg * kCols;
-  for (int e = tid; e < rows * (kCols / 4); e += kMxT) {
-    const int r = e / (kCols / 4), n = e % (kCols / 4) * 4;
-    if (cg * kCols + n >= g.d2) continue;
-    const float* const q = red + r * Ld + (n / 32) * KW * 32 + n % 32;
-    f32x4 v = *reinterpret_cast<const f32x4*>(q);
+    for (int u = 0; u < kXMost; ++u) {
+      const int e = tid + u * kMxT, r = e / kPieces, p = e % kPieces;
+      if (r < rows) *reinterpret_cast<u32x4*>(lds + r * kPitch + p * 16) = x[u];
+    }
+    barrier();
+    rg += row_split;
+    const bool more = MORE && rg < g.row_groups;
+    if (more) ask_x(rg * 32);
+    f32x16 acc;
 #pragma unroll
-    for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4*>(q + k * 32);
-    *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = v;
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    if (n0 < g.d2 && k0 < d1) {
+      const int row = l32 < rows ? l32 : rows - 1;  // (rows past the end: results dropped)
+      const unsigned char* const xr = lds + row * kPitch + kw * NL * 128 + lh * 64;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const float scale = mx4_scale((uint32_t)(sc[i / 4] >> (16 * (i & 3))) & 255u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mx4_bf16(c[i][e], scale)),
+                                                        *reinterpret_cast<const bf16x8*>(xr + i * 128 + e * 16), acc, 0, 0, 0);
+      }
+    }
+    // ---- the waves' sums ----
+    barrier();
+    if (l32 < rows)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(red + l32 * Ld + w * 32 + q * 8 + lh * 4) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    barrier();
+    float* const out = g.partial + ((size_t)(site * g.parts + part) * g.M + m0) * g.d2 + cg * kCols;
+    for (int e = tid; e < rows * (kCols / 4); e += kMxT) {
+      const int r = e / (kCols / 4), n = e % (kCols / 4) * 4;
+      if (cg * kCols + n >= g.d2) continue;
+      const float* const q = red + r * Ld + (n / 32) * KW * 32 + n % 32;
+      f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+      for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4*>(q + k * 32);
+      *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = v;
+    }
+    if (!more) return;
+    barrier();
   }
 }
 
@@ -618,95 +501,34 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
   *reinterpret_cast<u32x2_a8*>(g.Y[s0] + (size_t)m * g.ldy + n) = o;
 }
 
-template <int KW, int NL>
-int launch_shot(const MxBase& b, hipStream_t st) {
+template <int KW, int NL, bool MORE>
+int launch_base(const MxBase& b, hipStream_t st) {
   constexpr int kPart = KW * NL * 64, kRed = 32 * (kMxCols + 4) * 4;
-  const int x = b.M * kPart * 2, red = b.M * (kMxCols + 4) * 4;
+  const int rows = b.M < 32 ? b.M : 32, x = rows * (kPart * 2 + 16), red = rows * (kMxCols + 4) * 4;
   int bytes = x > red ? x : red;
   if (bytes < kMxW * 256 * 4) bytes = kMxW * 256 * 4;  // (the shrink's sums)
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    const int most = 32 * kPart * 2 > kRed ? 32 * kPart * 2 : kRed;
-    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_shot_kernel<KW, NL>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
+    const int most = 32 * (kPart * 2 + 16) > kRed ? 32 * (kPart * 2 + 16) : kRed;
+    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
     lds_set_for = dev;
   }
-  const int64_t grid = (int64_t)b.M * b.sites * b.shrink_parts + (int64_t)b.sites * b.col_groups * b.parts;
+  const int64_t total = (int64_t)b.sites * b.col_groups * b.row_split * b.parts, grid = b.shrink_z + (total + 7) / 8 * 8;
   if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
-  hipLaunchKernelGGL((mx4_shot_kernel<KW, NL>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
+  hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
   return check_launch();
 }
 
-template <int RT>
-int launch_base(const MxBase& b, hipStream_t st) {
-  constexpr int kX = kMxAhead * 32 * RT * kMxK * 2, kShrink = kMxW * kShrinkWaveBytes;
-  constexpr int kBytes = kX > kShrink ? kX : kShrink;
-  static thread_local int lds_set_for = -1;
-  int dev = 0;
-  MILORA_HIP(hipGetDevice(&dev));
-  if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<RT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes));
-    lds_set_for = dev;
-  }
-  const int64_t grid = (int64_t)b.shrink_blocks * b.shrink_parts * b.shrink_z + (int64_t)b.sites * b.col_groups * b.row_groups * b.parts;
-  if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
-  hipLaunchKernelGGL(mx4_base_kernel<RT>, dim3((unsigned)grid), dim3(kMxT), kBytes, st, b);
-  return check_launch();
-}
-
-// How the first launch cuts a call; a function of the sizes alone, shared by the launch and the workspace's sizing.
-// Up to 32 rows (kw > 0): waves that share columns, steps of a wave: X of a workgroup is M x kw x nl x 128 bytes, 64 KB at most, and as few
-// parts as that allows.  Beyond (kw = 0): 32 rt rows a workgroup, parts that make the workgroups fill the chip, two stages each at least.
-struct MxPlan {
-  int kw, nl, rt, parts, stages;
-};
-constexpr int kMxPartsMax = 16;
-int mx4_parts_max(int d1) {
-  const int n = (d1 + kMxK - 1) / kMxK / 2;
-  return n < 1 ? 1 : n < kMxPartsMax ? n : kMxPartsMax;
-}
-constexpr int kShotRows = 32;
-int shot_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
-int shot_parts(int64_t M, int d1) { return (d1 + shot_waves(M) * 512 - 1) / (shot_waves(M) * 512); }
-MxPlan mx4_plan(int64_t M, int d1, int d2, int sites) {
-  MxPlan p{};
-  if (M <= kShotRows) {
-    p.kw = shot_waves(M);
-    p.nl = 8;
-    p.parts = shot_parts(M, d1);
-    return p;
-  }
-  p.rt = M <= 64 ? 2 : 4;
-  const int all = (d1 + kMxK - 1) / kMxK;
-  const int64_t units = (int64_t)sites * ((d2 + kMxCols - 1) / kMxCols) * ((M + 32 * p.rt - 1) / (32 * p.rt));
-  int64_t parts = (p.rt > 2 ? 256 : 512) / units;
-  parts = parts < 1 ? 1 : parts > mx4_parts_max(d1) ? mx4_parts_max(d1) : parts;
-  p.stages = (int)((all + parts - 1) / parts);
-  p.parts = (all + p.stages - 1) / p.stages;
-  return p;
-}
-// The most partial sums (floats) of a call of up to these sizes; no size lowers it.
-size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
-  const size_t D = (size_t)sites * d2;
-  const int64_t few = M < kShotRows ? M : kShotRows;
-  size_t n = (size_t)few * D * shot_parts(few, d1);
-  if (few > 16 && (size_t)16 * D * shot_parts(16, d1) > n) n = (size_t)16 * D * shot_parts(16, d1);
-  if (few > 8 && (size_t)8 * D * shot_parts(8, d1) > n) n = (size_t)8 * D * shot_parts(8, d1);
-  if (M > kShotRows) {
-    const size_t most = (size_t)mx4_parts_max(d1) * M * D, cap = (size_t)(M <= 64 ? 512 * 64 : 256 * 128) * kMxCols + (size_t)M * D;
-    const size_t k = most < cap ? most : cap;
-    n = k > n ? k : n;
-  }
-  return n;
-}
-// Parts of the shrink: 1024 inputs each (few rows), or those of the matrix-core shrink.
-int mx4_shrink_parts(int64_t M, int d1) { return M <= kShotRows ? (d1 + kShotShrinkK - 1) / kShotShrinkK : shrink_parts(M, d1); }
-size_t mx4_shrink_floats(int64_t M, int d1) {
-  const int64_t few = M < kShotRows ? M : kShotRows;
-  const size_t a = (size_t)few * mx4_shrink_parts(few, d1), b = M > kShotRows ? shrink_rows_bound(M, d1) : 0;
-  return a > b ? a : b;
-}
+// How the first launch cuts a call; functions of the sizes alone, shared by the launch and the workspace's sizing.  Waves that share columns:
+// X of a row group is rows x KW x NL x 128 bytes, 64 KB of LDS at most (two workgroups a compute unit), and as few parts as that allows.
+constexpr int kMxSteps = 8;
+int mx4_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
+int mx4_parts(int64_t M, int d1) { return (d1 + mx4_waves(M) * kMxSteps * 64 - 1) / (mx4_waves(M) * kMxSteps * 64); }
+// (parts grow with the rows: no size lowers it)
+size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) { return (size_t)M * d2 * sites * mx4_parts(M, d1); }
+int mx4_shrink_parts(int d1) { return (d1 + kMxShrinkK - 1) / kMxShrinkK; }
 
 // Groups of eight of one launch: a grid has to stay below 2^32 threads.
 constexpr int64_t kQuantSlice = (int64_t)1 << 30;
@@ -754,40 +576,38 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
 }
 
 size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites) {
-  return align_up(mx4_shrink_floats(M, d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256) +
+  return align_up((size_t)M * mx4_shrink_parts(d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256) +
          align_up(mx4_partial_floats(M, d1, d2, sites) * sizeof(float), 256);
 }
 
 int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st) {
   if (g.M > 65535) return MILORA_ERANGE;
-  const int r_max = g.ad.r_max, t_parts = mx4_shrink_parts(g.M, g.d1);
+  const int r_max = g.ad.r_max, t_parts = mx4_shrink_parts(g.d1);
   float* const t = (float*)workspace;
   int2* const lora = (int2*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
   float* const partial = (float*)((char*)lora + align_up((size_t)g.M * sites * sizeof(int2), 256));
-  const MxPlan pl = mx4_plan(g.M, g.d1, g.d2, sites);
   MxBase b{};
   b.X = g.X; b.ldx = g.ldx; b.M = g.M; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
   b.sites = sites;
-  b.parts = pl.parts;
-  b.stages = pl.stages;
+  b.parts = mx4_parts(g.M, g.d1);
   b.partial = partial;
   b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, lora, nullptr,
                         sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
   b.shrink_parts = t_parts;
-  int rc;
-  if (pl.kw) {
-    b.col_groups = (g.d2 + kMxCols / pl.kw - 1) / (kMxCols / pl.kw);
-    rc = pl.kw == 8 ? launch_shot<8, 8>(b, st) : pl.kw == 4 ? launch_shot<4, 8>(b, st) : launch_shot<2, 8>(b, st);
-  } else {
-    b.col_groups = (g.d2 + kMxCols - 1) / kMxCols;
-    b.row_groups = (g.M + 32 * pl.rt - 1) / (32 * pl.rt);
-    b.shrink_blocks = (g.M + 15) / 16;
-    b.shrink_z = sites * shrink_shares(b.shrink_blocks, t_parts, sites, g.B, g.ad);
-    rc = pl.rt == 2 ? launch_base<2>(b, st) : launch_base<4>(b, st);
-  }
+  b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
+  const int kw = mx4_waves(g.M);
+  b.col_groups = (g.d2 + kMxCols / kw - 1) / (kMxCols / kw);
+  // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
+  b.row_groups = (g.M + 31) / 32;
+  const int64_t units = (int64_t)sites * b.col_groups * b.parts;
+  b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
+  const int rc = kw == 8   ? launch_base<8, kMxSteps, false>(b, st)
+                 : kw == 4 ? launch_base<4, kMxSteps, false>(b, st)
+                 : b.row_groups == 1 ? launch_base<2, kMxSteps, false>(b, st)
+                                     : launch_base<2, kMxSteps, true>(b, st);
   if (rc) return rc;
-  MxFinish f{g, pl.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, lora};
+  MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, lora};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
   if (gated) hipLaunchKernelGGL(mx4_finish_kernel<true>, grid, dim3(kFinT), 0, st, f);
   else hipLaunchKernelGGL(mx4_finish_kernel<false>, grid, dim3(kFinT), 0, st, f);
