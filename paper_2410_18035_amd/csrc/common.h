@@ -177,11 +177,13 @@ int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, c
                           const void* W, const void* bias, const AdapterView& ad, int site,
                           const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y, hipStream_t stream);
 
-// The same without bias, from shrinks that are there already, in fp32.
-int launch_linear_f32(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req, const void* W, const AdapterView& ad,
-                      int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, float* Y, hipStream_t stream);
+// The gated block of any shape: Y = silu(linear at `site` with Wg) * linear at site + 1 with Wu, both in fp32, which also go to gate_out and
+// up_out ([M][F] or null).  t: scratch of [2][M][r_max] floats.
+int launch_gated_generic(const void* X, int64_t M, int d, int F, int dtype, const int32_t* row_to_req, const void* Wg, const void* Wu,
+                         const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y,
+                         float* gate_out, float* up_out, hipStream_t stream);
 
-// The same for up to kFewRows rows, with the glue of a layer's decode step in its store.
+// A linear for up to kFewRows rows, with the glue of a layer's decode step in its store.
 constexpr int kFewRows = 16;
 constexpr int kFuseRank = 16;  // the largest rank that can be shrunk inside the launch
 enum FewMode {

@@ -43,32 +43,35 @@ struct Carver {
   }
 };
 
-// ---- forward ---------------------------------------------------------------------------------------------------------------
-template <typename T>
-__global__ void __launch_bounds__(kThreads) gated_glue_kernel(const float* __restrict__ g, const float* __restrict__ u, int64_t n, T* __restrict__ y) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i < n) Elem<T>::store(y, i, silu(g[i]) * u[i]);
-}
-
-template <typename T>
-int launch_glue(const float* g, const float* u, int64_t n, void* y, hipStream_t st) {
-  const int64_t slice = (int64_t)1 << 31;  // a grid has to stay below 2^32 threads
-  int rc = MILORA_OK;
-  for (int64_t i = 0; i < n && !rc; i += slice) {
-    const int64_t c = n - i < slice ? n - i : slice;
-    hipLaunchKernelGGL(gated_glue_kernel<T>, dim3((unsigned)((c + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, g + i, u + i, c, (T*)y + i);
-    rc = check_launch();
+// The scales of the ranks (X W^A, dz W^B^T: fp32, [site][part][M][r_max]) as two bf16 halves, about 17 of their bits: zero past the rank and for
+// rows without a term.  A row's 32 ranks by 32 lanes.
+constexpr int kHalvesRowsWg = kThreads / 32;
+__global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __restrict__ v, size_t part, int parts, int64_t M, int r_max,
+                                                                const int2* __restrict__ row_lora, Halves out) {
+  const int64_t i = (int64_t)blockIdx.x * kHalvesRowsWg + (threadIdx.x >> 5);  // line
+  if (i > M) return;
+  const int chunk = blockIdx.y, s = blockIdx.z, c = chunk * 32 + (threadIdx.x & 31);
+  float x = 0.f;
+  if (i > 0 && c < row_lora[s * M + i - 1].y) {
+    const float* const q = v + (size_t)s * part * parts + (size_t)(i - 1) * r_max + c;
+    for (int p = 0; p < parts; ++p) x += q[p * part];
   }
-  return rc;
+  const bf16_t hi = f32_to_bf16(x);
+  bf16_t* const line = out.at + s * out.site + chunk * out.chunk + (size_t)i * 64 + (threadIdx.x & 31);
+  line[0] = hi;
+  line[32] = f32_to_bf16(x - bf16_to_f32(hi));
 }
 
+int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, const Halves& out, hipStream_t st) {
+  const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), 2);
+  hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, v, (size_t)M * r_max, parts, M, r_max, row_lora, out);
+  return check_launch();
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------------------------
 }  // namespace
 
 constexpr int64_t kMxGatedRows = 128;  // up to this many rows the few-row kernel reads the codes, beyond the weights are written out in bf16
-
-// The any-shape path holds g and u of so many rows at a time in fp32, 64 MB of both unless 64 rows are more.
-constexpr int64_t kAnyFloats = (int64_t)1 << 23;
-int64_t any_rows(int F) { return kAnyFloats / F > 64 ? kAnyFloats / F : 64; }
 
 size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
   size_t most = 0;
@@ -78,6 +81,7 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
     c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
     c.take<int2>((size_t)M * 2);
     c.take<char>(partial_bytes_bound(M, d, 2 * F));
+    c.take<bf16_t>(halves_of(nullptr, M, r_max).site * 2);
     if (mx4 && M > kMxGatedRows) c.take<bf16_t>((size_t)d * F * 2);
     most = c.off;
     if (mx4) {
@@ -86,14 +90,8 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
       most = few > most ? few : most;
     }
   }
-  if (!mx4) {  // (bf16 too: whatever the alignment of its tensors)
-    Carver c{nullptr};
-    c.take<float>((size_t)M * r_max * 2);
-    const size_t held = (size_t)(kAnyFloats > (int64_t)64 * F ? kAnyFloats : (int64_t)64 * F), all = (size_t)M * F;
-    c.take<float>(2 * (all < held ? all : held));
-    most = c.off > most ? c.off : most;
-  }
-  return most;
+  const size_t any = align_up((size_t)M * r_max * 2 * sizeof(float), 256);  // (bf16 too: whatever the alignment of its tensors)
+  return any > most ? any : most;
 }
 
 int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void* workspace, hipStream_t st) {
@@ -111,7 +109,7 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
   const void* const like = g.mx4 ? (const void*)(uintptr_t)256 : nullptr;  // (in the workspace: aligned)
   const void *Wg = like ? like : g.Wg, *Wu = like ? like : g.Wu;
   const bool small = g.dtype == MILORA_BF16 && g.F < 1 << 30 && tiles_supported(M, g.d, 2 * g.F, packed, g.X, Wg, Y) && aligned16(Wu) && g.F % 16 == 0;
-  const bool large = g.dtype == MILORA_BF16 && !packed && prefill_supported(M, g.d, g.F, g.X, Wg, Y) && aligned16(Wu);
+  const bool large = g.dtype == MILORA_BF16 && !packed && M <= kHalvesRows && prefill_supported(M, g.d, g.F, g.X, Wg, Y) && aligned16(Wu);
   if (small || large) {
     Carver c{(char*)workspace};
     char* const ctrl = c.take<char>(kStreamCtrlBytes);
@@ -123,6 +121,8 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     float* const t = c.take<float>(shrink_rows_bound(M, g.d) * g.ad.r_max * 2);
     int2* const looked_up = c.take<int2>((size_t)M * 2);
     a.partial = c.take<float>(partial_bytes_bound(M, g.d, 2 * g.F) / sizeof(float));
+    a.halves = halves_of(nullptr, M, g.ad.r_max);
+    a.halves.at = c.take<bf16_t>(a.halves.site * 2);
     if (g.mx4) {
       bf16_t* const w = c.take<bf16_t>((size_t)g.d * g.F * 2);
       rc = mx4_dequantize(g.Wg, w, MILORA_BF16, g.d, g.F, packed, st);
@@ -135,10 +135,12 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     a.Wu = (const bf16_t*)Wu;
     // slices of rows where the smaller tiles are the only ones and the call has more than a launch of them takes
     const int64_t slice = large || M <= kTileMaxRows ? M : kTileMaxRows;
-    const TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large);
-    int2* const row_lora = large ? nullptr : looked_up;
+    const TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large, true);
+    const bool big = first.shape == kTiles256;
+    int2* const row_lora = large && !big ? nullptr : looked_up;
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, row_lora,
-                             row_lora || first.S > 1 ? a.cnt : nullptr, st);
+                             !big && (row_lora || first.S > 1) ? a.cnt : nullptr, st);
+    if (!rc && big) rc = launch_halves(t, parts, M, g.ad.r_max, looked_up, a.halves, st);
     for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
       a.M = M - m0 < slice ? M - m0 : slice;
       a.row_base = m0;
@@ -149,42 +151,15 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
       a.row_to_req = g.row_to_req ? g.row_to_req + m0 : nullptr;
       a.t = t + (size_t)m0 * g.ad.r_max;
       a.row_lora = row_lora ? row_lora + m0 : nullptr;
-      const TilePlan pl = a.M == slice ? first : plan_tiles(a.M, g.d, 2 * g.F, small, large);
+      const TilePlan pl = a.M == slice ? first : plan_tiles(a.M, g.d, 2 * g.F, small, large, true);
       rc = pl.shape == kTiles256 ? gated_prefill(a, st) : gated_tiles(a, pl, st);
     }
     return rc;
   }
   // any shape and type
   if (g.mx4) return MILORA_EUNSUPPORTED;
-  Carver c{(char*)workspace};
-  float* const t = c.take<float>((size_t)M * g.ad.r_max * 2);
-  if (M <= kFewRows) {
-    FewArgs a{};
-    a.X = g.X; a.ldx = g.d; a.M = (int)M; a.d1 = g.d; a.d2 = g.F;
-    a.W[0] = g.Wg; a.W[1] = g.Wu; a.Y[0] = Y; a.ldy = g.F; a.site[0] = kGate; a.site[1] = kGate + 1;
-    a.row_to_req = g.row_to_req; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B; a.ad = g.ad;
-    a.gate_out = gate_out; a.up_out = up_out;
-    return launch_few_rows(a, g.dtype, 2, kFewGated, t, st);
-  }
-  if (M > (int64_t)65535 * 64) return MILORA_ERANGE;
-  rc = launch_shrink(g.X, g.d, M, g.d, g.dtype, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, st);
-  const int64_t slice = any_rows(g.F);
-  const size_t es = dtype_size(g.dtype);
-  float* const held = c.take<float>(0);
-  for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
-    const int64_t rows = M - m0 < slice ? M - m0 : slice;
-    const char* const x = (const char*)g.X + (size_t)m0 * g.d * es;
-    char* const y = (char*)Y + (size_t)m0 * g.F * es;
-    const int32_t* const map = g.row_to_req ? g.row_to_req + m0 : nullptr;
-    const int64_t b0 = map ? 0 : m0;  // (unmapped rows: the slice's requests)
-    float* const gate = gate_out ? gate_out + (size_t)m0 * g.F : held;
-    float* const up = up_out ? up_out + (size_t)m0 * g.F : held + (size_t)rows * g.F;
-    for (int s = 0; s < 2 && !rc; ++s)
-      rc = launch_linear_f32(x, rows, g.d, g.F, g.dtype, map, s ? g.Wu : g.Wg, g.ad, kGate + s, g.tenant_id + b0, g.route + b0, (int)(g.B - b0),
-                             t + ((size_t)s * M + m0) * g.ad.r_max, s ? up : gate, st);
-    if (!rc) rc = g.dtype == MILORA_BF16 ? launch_glue<bf16_t>(gate, up, rows * g.F, y, st) : launch_glue<float>(gate, up, rows * g.F, y, st);
-  }
-  return rc;
+  return launch_gated_generic(g.X, M, g.d, g.F, g.dtype, g.row_to_req, g.Wg, g.Wu, g.ad, kGate, g.tenant_id, g.route, g.B, (float*)workspace, Y,
+                              gate_out, up_out, st);
 }
 
 // ---- backward --------------------------------------------------------------------------------------------------------------
@@ -459,23 +434,6 @@ __global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) 
 }
 
 // ---- the same on the bf16 matrix cores -------------------------------------------------------------------------------------
-// The scales of a rank (low, x A: fp32) as two bf16 halves, about 17 of their bits: line [chunk of 32 ranks][m] of 64 values, 32 high and 32 low
-// halves, zero past the rank and for rows without a term.
-__global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __restrict__ v, size_t part, int parts, int64_t M, int r_max,
-                                                                const int2* __restrict__ row_lora, bf16_t* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);  // a row
-  if (i >= M) return;
-  const int c = blockIdx.y * 32 + (threadIdx.x & 31);
-  const int r = row_lora[i].y;
-  float x = 0.f;
-  if (c < r)
-    for (int p = 0; p < parts; ++p) x += v[p * part + (size_t)i * r_max + c];
-  const bf16_t hi = f32_to_bf16(x);
-  bf16_t* const line = out + ((size_t)blockIdx.y * M + i) * 64 + (threadIdx.x & 31);
-  line[0] = hi;
-  line[32] = f32_to_bf16(x - bf16_to_f32(hi));
-}
-
 // out[col][c] = sum over the tenant's rows of P[m][col] s[m][c]: a workgroup of eight waves takes 64 columns and 32 ranks of one of a
 // tenant's matrices, a wave every eighth 64 rows of the call.  A wave lists the tenant's rows among its own and takes 32 of them at a time: their 128 bytes
 // of P and of s go through registers (the next 32 rows' are on their way while these are multiplied) into the wave's LDS, and the
@@ -487,8 +445,7 @@ struct GradTileArgs {
   int d, F, tiles_a, tiles_b;  // tiles of 64 columns
   const int2 *row_lora, *among;
   AdapterView ad;
-  const bf16_t *low, *t;  // halves, [site][chunk][M][64]
-  size_t half_site;
+  Halves low, t;
   void* const* dA;
   void* const* dB;
 };
@@ -511,7 +468,8 @@ __global__ void __launch_bounds__(kGradW * 64, 4) gated_grad_tile_kernel(const G
   const int cols = is_b ? g.F : g.d, n0 = (is_b ? tile - g.tiles_a : tile) * 64;
   const bf16_t* const P = is_b ? g.dz + (int64_t)s * g.F : g.X;
   const int64_t ldp = is_b ? 2 * (int64_t)g.F : g.d;
-  const bf16_t* const sc = (is_b ? g.t : g.low) + s * g.half_site + (size_t)chunk * g.M * 64;
+  const Halves& half = is_b ? g.t : g.low;
+  const bf16_t* const sc = half.at + s * half.site + chunk * half.chunk + 64;  // (behind the zero line)
   const int blocks = (int)((g.M + 63) / 64);
   if (tid == 0) { span[0] = blocks; span[1] = 0; }
   __syncthreads();
@@ -642,7 +600,7 @@ struct BackWs {
   int2* row_lora;  // [2][M]
   int2* among;     // [2][M / 64]
   void* W;         // 4-bit weights in bf16
-  bf16_t* halves;  // bf16 shapes of the matrix cores: [low, t][site][chunk][M][64]
+  Halves low_halves, t_halves;  // of the bf16 matrix cores
   float* partial;
   size_t bytes;
 };
@@ -658,7 +616,9 @@ BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int 
   w.among = c.take<int2>((size_t)((M + 63) / 64) * 2);
   w.W = c.take<bf16_t>(mx4 ? (size_t)d * F * 2 : 0);
   const bool tiles = dtype == MILORA_BF16;  // (whatever the other sizes: none may go down when one goes up)
-  w.halves = c.take<bf16_t>(tiles ? (size_t)((r_max + 31) / 32) * M * 64 * 4 : 0);
+  w.low_halves = w.t_halves = halves_of(nullptr, M, r_max);
+  w.low_halves.at = c.take<bf16_t>(tiles ? w.low_halves.site * 2 : 0);
+  w.t_halves.at = c.take<bf16_t>(tiles ? w.t_halves.site * 2 : 0);
   w.partial = c.take<float>(tiles ? back_partial_floats(M, d, F) : 0);
   w.bytes = c.off;
   return w;
@@ -714,42 +674,34 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   int rc = launch_dz<bf16_t>(dY, gate, up, M, g.F, w.dz, st);
   if (!rc) rc = launch_low_sites(dz, M, g.F, g.row_to_req, g.ad, g.tenant_id, g.route, g.B, w.low, st);
   if (rc) return rc;
+  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
+                     g.route, g.B, w.row_lora, w.among);
+  if ((rc = check_launch())) return rc;
   const int low_parts = shrink_parts(M, g.F);
   const size_t row_floats = (size_t)M * r_max;
+  if ((rc = launch_halves(w.low, low_parts, M, r_max, w.row_lora, w.low_halves, st))) return rc;
   if (dX) {
     GatedBackArgs a{};
     a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
     a.Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
     a.Wu = g.mx4 ? (const bf16_t*)w.W + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
+    a.row_lora = w.row_lora; a.lora_site = (size_t)M; a.halves = w.low_halves;
     a.low = w.low; a.low_stride = row_floats; a.low_site = row_floats * low_parts; a.parts = low_parts;
     a.partial = w.partial; a.dX = (bf16_t*)dX;
     if ((rc = gated_dx_tiles(a, st))) return rc;
   }
   if (!dA && !dB) return rc;
-  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
-                     g.route, g.B, w.row_lora, w.among);
-  if ((rc = check_launch())) return rc;
-  const int chunks = (r_max + 31) / 32;
-  const size_t half_site = (size_t)chunks * M * 64;
-  bf16_t* const halves[2] = {w.halves, w.halves + 2 * half_site};  // of low, of t
-  const int t_parts = shrink_parts(M, g.d);
-  if (dB && (rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st)))
-    return rc;
-  for (int k = 0; k < 2; ++k) {
-    if (!(k ? dB : dA)) continue;
-    const int parts = k ? t_parts : low_parts;
-    for (int s = 0; s < 2 && !rc; ++s) {
-      hipLaunchKernelGGL(gated_halves_kernel, dim3((unsigned)((M + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)chunks), dim3(kThreads), 0, st,
-                         (k ? w.t : w.low) + s * row_floats * parts, row_floats, parts, M, r_max, w.row_lora + s * M, halves[k] + s * half_site);
-      rc = check_launch();
-    }
+  if (dB) {
+    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
+    if (!rc) rc = launch_halves(w.t, shrink_parts(M, g.d), M, r_max, w.row_lora, w.t_halves, st);
     if (rc) return rc;
   }
+  const int chunks = (r_max + 31) / 32;
   GradTileArgs a{};
   a.X = (const bf16_t*)g.X; a.dz = dz; a.M = M; a.d = g.d; a.F = g.F;
   a.tiles_a = dA ? (g.d + 63) / 64 : 0;
   a.tiles_b = dB ? (g.F + 63) / 64 : 0;
-  a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = halves[0]; a.t = halves[1]; a.half_site = half_site; a.dA = dA; a.dB = dB;
+  a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = w.low_halves; a.t = w.t_halves; a.dA = dA; a.dB = dB;
   hipLaunchKernelGGL(gated_grad_tile_kernel, dim3((unsigned)((a.tiles_a + a.tiles_b) * chunks), (unsigned)(2 * tenants)), dim3(kGradW * 64), 0, st, a);
   return check_launch();
 }

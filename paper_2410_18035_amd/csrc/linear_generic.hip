@@ -300,20 +300,24 @@ typedef GenCfg<32, 32, 16> GenSmall;
 typedef GenCfg<64, 64, 32> GenLarge;
 constexpr int kGenLargeTiles = 128;
 
-template <typename T, class C, bool WIDE, typename TO>
+// GATED: the columns of a tile are as many of the gate (W, t) and then of the up projection (W2, t of the next site): Y = silu(g) u, with g
+// and u in fp32, which go to gate_out and up_out, if given.
+template <typename T, class C, bool WIDE, bool GATED>
 __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restrict__ X, int64_t M, int d1, int d2, int col0,
                                                            const int32_t* __restrict__ row_to_req, const T* __restrict__ W,
-                                                           const T* __restrict__ bias, AdapterView ad, int site,
+                                                           const T* __restrict__ W2, const T* __restrict__ bias, AdapterView ad, int site,
                                                            const int32_t* __restrict__ tenant_id,
                                                            const uint8_t* __restrict__ route, int B,
-                                                           const float* __restrict__ t, TO* __restrict__ Y) {
+                                                           const float* __restrict__ t, int64_t t_site, T* __restrict__ Y,
+                                                           float* __restrict__ gate_out, float* __restrict__ up_out) {
+  constexpr int kSites = GATED ? 2 : 1, kOutN = C::BN / kSites;
   extern __shared__ __attribute__((aligned(16))) float buf[];
-  __shared__ int s_rank[C::BM], s_ten[C::BM], s_most;
+  __shared__ int s_rank[kSites][C::BM], s_ten[kSites][C::BM], s_most[kSites];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = w / (C::WM * C::WN), wm = w % (C::WM * C::WN) % C::WM, wn = w % (C::WM * C::WN) / C::WM;
   const int64_t m0 = (int64_t)blockIdx.y * C::BM;
-  const int n0 = col0 + blockIdx.x * C::BN;
+  const int n0 = col0 + blockIdx.x * kOutN;
 
   const T* src[C::Items];
   const int kq = tid % (C::SK / 4) * 4;
@@ -325,8 +329,8 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
       const int64_t m = m0 + row < M ? m0 + row : M - 1;  // past the edge: the last row again, its results are dropped
       src[i] = X + (size_t)m * d1;
     } else {
-      const int n = n0 + row - C::BM < d2 ? n0 + row - C::BM : d2 - 1;
-      src[i] = W + (size_t)n * d1;
+      const int c = row - C::BM, n = n0 + c % kOutN < d2 ? n0 + c % kOutN : d2 - 1;
+      src[i] = (GATED && c >= kOutN ? W2 : W) + (size_t)n * d1;
     }
     dst[i] = row * C::Ld + kq;
   }
@@ -369,20 +373,23 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
   };
 #pragma unroll
   for (int j = 0; j < kSets; ++j) load(j, r[j]);
-  if (tid == 0) s_most = 0;
+  if (tid < kSites) s_most[tid] = 0;
   store(0, r[0]);
   load(kSets, r[0]);
   __syncthreads();
   if (tid < C::BM) {  // which rows carry a LoRA term
     const int64_t m = m0 + tid;
-    int tenant = 0, r = 0;
-    if (m < M) {
-      const int64_t req = row_to_req ? (int64_t)row_to_req[m] : m;
-      r = (req >= 0 && req < B) ? routed_rank(ad, tenant_id, route, (int)req, B, site, &tenant) : 0;
+#pragma unroll
+    for (int s = 0; s < kSites; ++s) {
+      int tenant = 0, r = 0;
+      if (m < M) {
+        const int64_t req = row_to_req ? (int64_t)row_to_req[m] : m;
+        r = (req >= 0 && req < B) ? routed_rank(ad, tenant_id, route, (int)req, B, site + s, &tenant) : 0;
+      }
+      s_rank[s][tid] = r;
+      s_ten[s][tid] = tenant;
+      if (r) atomicMax(&s_most[s], r);
     }
-    s_rank[tid] = r;
-    s_ten[tid] = tenant;
-    if (r) atomicMax(&s_most, r);
   }
   for (int s0 = 0; s0 < stages; s0 += kSets) {
 #pragma unroll
@@ -402,7 +409,7 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
     *reinterpret_cast<f32x4*>(buf + (size_t)(q * C::BM + wm * 32 + l32) * C::LdR + wn * 32 + g * 8 + lh * 4) =
         f32x4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
   __syncthreads();
-  const int nc = tid % C::BN, r0 = tid / C::BN, n = n0 + nc;
+  const int nc = tid % C::BN, r0 = tid / C::BN, n = n0 + nc % kOutN, my = GATED ? nc / kOutN : 0;
   constexpr int kStep = C::T / C::BN;
   const int ns = n < d2 ? n : d2 - 1;
   const float bv = bias ? Elem<T>::load(bias, ns) : 0.f;
@@ -417,21 +424,24 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
 
   // LoRA expand, 32 ranks at a time; eight rows of W^B for all of a thread's outputs on their way together (one output after
   // the other, each waited for its own loads: 43.4 us a call of 300 rows on 1000 x 2730 against 37.8 us)
-  const int most = s_most;
   float* const ts = buf + C::TsOff;
-  if (most > 0) {
+#pragma unroll 1
+  for (int s = 0; s < kSites; ++s) {
+    const int most = s_most[s];
+    if (most <= 0) continue;
+    const float* const t_of = t + s * t_site;
     const T* Bm[C::Outs];
     int last[C::Outs];
 #pragma unroll
     for (int i = 0; i < C::Outs; ++i) {
       const int row = r0 + i * kStep;
-      last[i] = s_rank[row] - 1;
-      Bm[i] = last[i] >= 0 ? (const T*)ad.B[s_ten[row] * MILORA_NUM_SITES + site] + ns : nullptr;
+      last[i] = !GATED || my == s ? s_rank[s][row] - 1 : -1;
+      Bm[i] = last[i] >= 0 ? (const T*)ad.B[s_ten[s][row] * MILORA_NUM_SITES + site + s] + ns : nullptr;
     }
     for (int c0 = 0; c0 < most; c0 += 32) {
       for (int e = tid; e < C::BM * 32; e += C::T) {
         const int row = e >> 5, c = c0 + (e & 31);
-        ts[e] = c < s_rank[row] ? t[(size_t)(m0 + row) * ad.r_max + c] : 0.f;
+        ts[e] = c < s_rank[s][row] ? t_of[(size_t)(m0 + row) * ad.r_max + c] : 0.f;
       }
       __syncthreads();
       for (int c1 = 0; c1 < 32 && c0 + c1 < most; c1 += 8) {
@@ -446,7 +456,8 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
 #pragma unroll
         for (int i = 0; i < C::Outs; ++i)
 #pragma unroll
-          for (int u = 0; u < 8; ++u) val[i] += ts[(r0 + i * kStep) * 32 + c1 + u] * b[i][u];
+          for (int u = 0; u < 8; ++u)
+            if (!GATED || my == s) val[i] += ts[(r0 + i * kStep) * 32 + c1 + u] * b[i][u];
       }
       __syncthreads();
     }
@@ -454,30 +465,65 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
 #pragma unroll
   for (int i = 0; i < C::Outs; ++i) {
     const int64_t m = m0 + r0 + i * kStep;
-    if (m < M && n < d2) Elem<TO>::store(Y, (size_t)m * d2 + n, val[i]);
+    if constexpr (GATED) {
+      const float up = __shfl_xor(val[i], kOutN, 64);
+      if (m >= M || n >= d2) continue;
+      const size_t at = (size_t)m * d2 + n;
+      float* const save = my ? up_out : gate_out;
+      if (save) save[at] = val[i];
+      if (my == 0) Elem<T>::store(Y, at, silu(val[i]) * up);
+    } else {
+      if (m < M && n < d2) Elem<T>::store(Y, (size_t)m * d2 + n, val[i]);
+    }
   }
 }
 
-template <typename T, class C, bool WIDE, typename TO>
-int launch_tile(const void* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const void* bias,
-                const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, void* Y,
-                hipStream_t stream) {
+struct TileArgs {
+  const void* X;
+  int64_t M;
+  int d1, d2;
+  const int32_t* row_to_req;
+  const void *W, *W2, *bias;
+  AdapterView ad;
+  int site;
+  const int32_t* tenant_id;
+  const uint8_t* route;
+  int B;
+  const float* t;
+  int64_t t_site;
+  void* Y;
+  float *gate_out, *up_out;
+};
+
+template <typename T, class C, bool WIDE, bool GATED>
+int launch_tile(const TileArgs& g, hipStream_t stream) {
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)linear_tile_kernel<T, C, WIDE, TO>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
+    MILORA_HIP(hipFuncSetAttribute((const void*)linear_tile_kernel<T, C, WIDE, GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
     lds_set_for = dev;
   }
+  constexpr int kOutN = GATED ? C::BN / 2 : C::BN, kCols = kLaunchCols / 64 * kOutN;
   int rc = MILORA_OK;
-  for (int64_t col0 = 0; col0 < d2 && !rc; col0 += kLaunchCols) {
-    const int cols = d2 - col0 < kLaunchCols ? (int)(d2 - col0) : kLaunchCols;
-    dim3 grid((unsigned)((cols + C::BN - 1) / C::BN), (unsigned)((M + C::BM - 1) / C::BM));
-    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE, TO>), grid, dim3(C::T), C::LdsBytes, stream, (const T*)X, M, d1, d2, (int)col0,
-                       row_to_req, (const T*)W, (const T*)bias, ad, site, tenant_id, route, B, t, (TO*)Y);
+  for (int64_t col0 = 0; col0 < g.d2 && !rc; col0 += kCols) {
+    const int cols = g.d2 - col0 < kCols ? (int)(g.d2 - col0) : kCols;
+    dim3 grid((unsigned)((cols + kOutN - 1) / kOutN), (unsigned)((g.M + C::BM - 1) / C::BM));
+    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE, GATED>), grid, dim3(C::T), C::LdsBytes, stream, (const T*)g.X, g.M, g.d1, g.d2, (int)col0,
+                       g.row_to_req, (const T*)g.W, (const T*)g.W2, (const T*)g.bias, g.ad, g.site, g.tenant_id, g.route, g.B, g.t, g.t_site,
+                       (T*)g.Y, g.gate_out, g.up_out);
     rc = check_launch();
   }
   return rc;
+}
+
+// Tiles of more than kFewRows rows, from shrinks that are there.
+template <typename T, bool GATED>
+int launch_tiles_any(const TileArgs& g, hipStream_t stream) {
+  const int64_t large = ((g.M + 63) / 64) * (((int64_t)g.d2 * (GATED ? 2 : 1) + 63) / 64);
+  if (g.d1 < 4) return launch_tile<T, GenLarge, false, GATED>(g, stream);
+  if (large >= kGenLargeTiles) return launch_tile<T, GenLarge, true, GATED>(g, stream);
+  return launch_tile<T, GenSmall, true, GATED>(g, stream);
 }
 
 }  // namespace
@@ -558,17 +604,6 @@ int launch_few_rows(const FewArgs& args, int dtype, int sites, int mode, float* 
   return bf ? launch_few_rows_t<bf16_t, 8, true>(g, sites, mode, st) : launch_few_rows_t<float, 8, true>(g, sites, mode, st);
 }
 
-// Tiles of more than kFewRows rows; t: the shrinks.
-template <typename T, typename TO>
-static int launch_tiles_any(const void* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const void* bias,
-                            const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, void* Y,
-                            hipStream_t stream) {
-  const int64_t large = ((M + 63) / 64) * (int64_t)((d2 + 63) / 64);
-  if (d1 < 4) return launch_tile<T, GenLarge, false, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
-  if (large >= kGenLargeTiles) return launch_tile<T, GenLarge, true, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
-  return launch_tile<T, GenSmall, true, TO>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
-}
-
 int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req,
                           const void* W, const void* bias, const AdapterView& ad, int site,
                           const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y, hipStream_t stream) {
@@ -582,17 +617,26 @@ int launch_linear_generic(const void* X, int64_t M, int d1, int d2, int dtype, c
   }
   const int rc = launch_shrink(X, d1, M, d1, dtype, row_to_req, ad, site, 1, tenant_id, route, B, t, stream);
   if (rc) return rc;
-  if (dtype == MILORA_BF16)
-    return launch_tiles_any<bf16_t, bf16_t>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
-  return launch_tiles_any<float, float>(X, M, d1, d2, row_to_req, W, bias, ad, site, tenant_id, route, B, t, Y, stream);
+  const TileArgs g{X, M, d1, d2, row_to_req, W, nullptr, bias, ad, site, tenant_id, route, B, t, 0, Y, nullptr, nullptr};
+  return dtype == MILORA_BF16 ? launch_tiles_any<bf16_t, false>(g, stream) : launch_tiles_any<float, false>(g, stream);
 }
 
-int launch_linear_f32(const void* X, int64_t M, int d1, int d2, int dtype, const int32_t* row_to_req, const void* W, const AdapterView& ad,
-                      int site, const int32_t* tenant_id, const uint8_t* route, int B, const float* t, float* Y, hipStream_t stream) {
+int launch_gated_generic(const void* X, int64_t M, int d, int F, int dtype, const int32_t* row_to_req, const void* Wg, const void* Wu,
+                         const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, float* t, void* Y,
+                         float* gate_out, float* up_out, hipStream_t stream) {
   if ((M + 63) / 64 > 65535) return MILORA_ERANGE;
-  if (dtype == MILORA_BF16)
-    return launch_tiles_any<bf16_t, float>(X, M, d1, d2, row_to_req, W, nullptr, ad, site, tenant_id, route, B, t, Y, stream);
-  return launch_tiles_any<float, float>(X, M, d1, d2, row_to_req, W, nullptr, ad, site, tenant_id, route, B, t, Y, stream);
+  if (M <= kFewRows) {
+    FewArgs g{};
+    g.X = X; g.ldx = d; g.M = (int)M; g.d1 = d; g.d2 = F;
+    g.W[0] = Wg; g.W[1] = Wu; g.Y[0] = Y; g.ldy = F; g.site[0] = site; g.site[1] = site + 1;
+    g.row_to_req = row_to_req; g.tenant_id = tenant_id; g.route = route; g.B = B; g.ad = ad;
+    g.gate_out = gate_out; g.up_out = up_out;
+    return launch_few_rows(g, dtype, 2, kFewGated, t, stream);
+  }
+  const int rc = launch_shrink(X, d, M, d, dtype, row_to_req, ad, site, 2, tenant_id, route, B, t, stream);
+  if (rc) return rc;
+  const TileArgs g{X, M, d, F, row_to_req, Wg, Wu, nullptr, ad, site, tenant_id, route, B, t, M * ad.r_max, Y, gate_out, up_out};
+  return dtype == MILORA_BF16 ? launch_tiles_any<bf16_t, true>(g, stream) : launch_tiles_any<float, true>(g, stream);
 }
 
 }  // namespace milora

@@ -55,6 +55,12 @@ struct PParams {
   float* gate_out;    // kGated: [M][d2] each, or null
   float* up_out;
   size_t t_site;      // kGated, kBack: floats to the shrinks of the next site
+  // kGated, kBack: [site][M of the call] tenant and rank of each row, and the shrinks as two bf16 halves: [site][chunk of 32 ranks][1 + M] lines
+  // of 64 values, 32 high halves and 32 low ones; the first line is zero
+  const int2* row_lora;
+  size_t lora_site;
+  const bf16_t* halves;
+  size_t half_site, half_chunk;
   float* partial;     // kBack, S > 1: [part][M][d2] sums of the parts of the reduction
   size_t partial_stride;
   int S, steps;       // kBack: parts, and k steps of a part
@@ -178,6 +184,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     for (int j = 0; j < 8; ++j) issue_one(kt, hh, slot, j);
   };
 
+  int2 lora[2] = {int2{-1, 0}, int2{-1, 0}};  // (kGated, kBack) of row tid, at the two sites
+  if (MODE != kPlain && m0 + tid < p.M && (!BACK || part == p.S - 1))
+#pragma unroll
+    for (int s = 0; s < 2; ++s) lora[s] = p.row_lora[s * p.lora_site + p.row_base + m0 + tid];
+
   // acc[i][j]: rows 32 i .. 32 i + 31 of the wave's X part against rows 32 j .. of its W part
   f32x16 acc[4][4];
 #pragma unroll
@@ -296,28 +307,19 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // t by way of LDS, one step at a time: a call of 777 rows on 4096 x 11008 with a tenant of rank 64 131 us, 120 so, 97 without).
   int* ctl = (int*)(lds + 4 * kHalfBytes);  // ring slots 0 .. 3 hold the operand blocks
   int* const row_ten = ctl + 16;            // tenant of each row of the tile, -1: no LoRA term
-  int my_ten = -1, my_ten2 = -1;  // (of the second site)
+  if (tid == 0) ctl[1] = 0;  // set: a matrix of some tenant of the tile holds Inf or NaN
+  if constexpr (MODE == kPlain) {
+  int my_ten = -1;
   {
     const int64_t m = m0 + tid;
-    if (m < p.M && (!BACK || part == p.S - 1)) {
+    if (m < p.M) {
       const int64_t req = p.row_to_req ? (int64_t)p.row_to_req[m] : p.row_base + m;
-      const bool in = req >= 0 && req < p.B;
       int tenant = 0;
-      int r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
+      const int r = (req >= 0 && req < p.B) ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site, &tenant) : 0;
       if (r) my_ten = tenant;
-      if (kSites > 1) {
-        r = in ? routed_rank(p.ad, p.tenant_id, p.route, (int)req, p.B, p.site + 1, &tenant) : 0;
-        if (r) my_ten2 = tenant;
-      }
     }
   }
-  if (tid == 0) ctl[1] = 0;  // set: W^B of some tenant of the tile holds Inf or NaN
-#pragma unroll 1
-  for (int s = 0; s < kSites; ++s) {
-  if (s) my_ten = my_ten2;
-  row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
-  const float* const t_of = p.t + (kSites > 1 ? s * p.t_site : 0);
-  const int site = p.site + (kSites > 1 ? s : 0);
+  row_ten[tid] = my_ten;
   int last = -1;
   for (;;) {
     if (tid == 0) ctl[0] = 0x7fffffff;
@@ -333,8 +335,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     const int cur = ctl[0];
     if (cur == 0x7fffffff) break;
     const int r = p.ad.rank[cur];
-    gbf16* Bm = in_global((BACK ? p.ad.A : p.ad.B)[cur * MILORA_NUM_SITES + site]);
-    const bool vec_a = BACK && (r & 7) == 0 && ((uintptr_t)Bm & 15) == 0;
+    gbf16* Bm = in_global(p.ad.B[cur * MILORA_NUM_SITES + p.site]);
     for (int c0 = 0; c0 < r; c0 += 64) {
       int tb = tid;  // opaque: addresses formed from it stay inside the loop instead of being spilled in front of it
       asm volatile("" : "+v"(tb));
@@ -345,15 +346,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       u32x4 a[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = u32x4{0u, 0u, 0u, 0u};
-      // (GATED: of a wave's 128 columns the first 64 are the gate's; the other projection's stay zero)
-      const int n_piece = n0 + (GATED ? (pc >> 4) * 64 + (pc & 7) * 8 : pc * 8);
-      if (wput && n_piece < p.d2 && (!GATED || ((pc >> 3) & 1) == s)) {
-        gbf16* b = BACK ? Bm + (size_t)n_piece * r + cw : Bm + (size_t)cw * p.d2 + n_piece;
+      if (wput && n0 + pc * 8 < p.d2) {
+        gbf16* b = Bm + (size_t)cw * p.d2 + n0 + pc * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (BACK) {  // column n_piece + i, eight ranks of it (zero past the last)
-            if (cw < r) a[i] = load8(b + (size_t)i * r, r - cw, vec_a);
-          } else if (cw + i < r) a[i] = *(gu32x4_a2*)(b + (size_t)i * p.d2);  // (whole pieces of 8 columns, d2 % 16 == 0, at any alignment)
+          if (cw + i < r) a[i] = *(gu32x4_a2*)(b + (size_t)i * p.d2);  // (whole pieces of 8 columns, d2 % 16 == 0, at any alignment)
       }
       // X side: eight lanes take 32 ranks of a row, the shrink's parts added in part order
       const int rq = tb & 7;
@@ -368,7 +365,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           for (int i = 0; i < 4; ++i) {
             v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             const int64_t mr = m0 + (tb >> 3) + 32 * (i0 + i);
-            q[i] = t_of + (size_t)(mr < p.M ? mr : p.M - 1) * p.ad.r_max + cq;
+            q[i] = p.t + (size_t)(mr < p.M ? mr : p.M - 1) * p.ad.r_max + cq;
           }
           if (vec) {
             for (int k0 = 0; k0 < p.parts; k0 += 4) {  // four rows and four parts in flight
@@ -425,12 +422,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           ctl[1] = 1;
         }
         u32x4 at[8];
-        if constexpr (BACK) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) at[i] = a[i];
-        } else {
-          transpose8(a, at);
-        }
+        transpose8(a, at);
         // (columns 8 pc .. + 7: one half of a block of 16)
         unsigned char* const wst = lds + (2 * (gq >> 2) + (pc >> 4)) * kHalfBytes + (kBlocksM / 2 + ((pc >> 1) & 7)) * kBlockBytes;
 #pragma unroll
@@ -446,6 +438,109 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
     last = cur;
   }
+  } else {
+    // The same for two sites, from the halves prepared in front of the launch: a line of them is a row of a step as it lies, copied straight into
+    // LDS, the zero line for rows of other tenants; one round trip for 64 ranks of a tenant (with the shrinks' parts added and split here,
+    // 777 rows of 5 requests, three sites each, ranks 8 to 64, gated block of 4096 x 11008: 287 us a call).  kGated: 32 rows of W^B go in as they lie,
+    // [k][column], and are read transposed; the columns of the other projection are zero.  kBack: eight ranks of a column are eight consecutive
+    // values of W^A.
+#pragma unroll 1
+    for (int s = 0; s < 2; ++s) {
+      const int my_ten = lora[s].y ? lora[s].x : -1;
+      row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
+      int last = -1;
+      for (;;) {
+        if (tid == 0) ctl[0] = 0x7fffffff;
+        __syncthreads();
+        int cand = my_ten > last ? my_ten : 0x7fffffff;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const int o = __shfl_xor(cand, off, 64);
+          cand = o < cand ? o : cand;
+        }
+        if (lane == 0) atomicMin(&ctl[0], cand);
+        __syncthreads();
+        const int cur = __builtin_amdgcn_readfirstlane(ctl[0]);
+        if (cur == 0x7fffffff) break;
+        const int r = p.ad.rank[cur];
+        gbf16* const Wm = in_global((BACK ? p.ad.A : p.ad.B)[cur * MILORA_NUM_SITES + p.site + s]);
+        const bool vec_a = (r & 7) == 0 && ((uintptr_t)Wm & 15) == 0;
+        for (int c0 = 0; c0 < r; c0 += 64) {
+          int tb = tid;  // opaque: addresses formed from it stay inside the loop instead of being spilled in front of it
+          asm volatile("" : "+v"(tb));
+          const int steps = r - c0 > 32 ? 2 : 1;
+          // X side: eight copies of a step by each wave, eight rows each
+          for (int st = 0; st < steps; ++st) {
+            const bf16_t* const lines = p.halves + s * p.half_site + (size_t)((c0 >> 5) + st) * p.half_chunk;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int q = wave * 8 + j, i = q & 15, row = (q >> 4) * 128 + i * 8 + ((tb & 63) >> 3);
+              const uint32_t line = row_ten[row] == cur ? (uint32_t)(p.row_base + m0 + row + 1) : 0u;
+              copy_to_lds16(lines, line * 128u + (uint32_t)((tb & 7) ^ swz(row & 15)) * 16u, lds0 + (2 * st + (q >> 4)) * kHalfBytes + i * 1024);
+            }
+          }
+          // W side
+          u32x4 a[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) a[i] = u32x4{0u, 0u, 0u, 0u};
+          const int pc = tb & 31, gq = tb >> 5;  // kBack: columns 8 pc .. + 7, ranks c0 + 8 gq .. + 7
+          if constexpr (BACK) {
+            const int cw = c0 + gq * 8;
+            if (gq < steps * 4 && n0 + pc * 8 < p.d2 && cw < r)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) a[i] = load8(Wm + (size_t)(n0 + pc * 8 + i) * r + cw, r - cw, vec_a);
+          } else {  // rank c0 + 32 (i / 2) + .., eight columns of the site: 512 pieces of a step, two a thread
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int e = (i & 1) * 256 + tb, c = c0 + (i >> 1) * 32 + (e >> 4), n = n0 + (e & 15) * 8;
+              if ((i >> 1) < steps && c < r && n < p.d2) a[i] = *(gu32x4_a2*)(Wm + (size_t)c * p.d2 + n);
+            }
+          }
+          float taints[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < (BACK ? 8 : 4); ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) taints[e] = taint(taints[e], a[i][e]);
+          if ((taints[0] + taints[1]) + (taints[2] + taints[3]) != 0.f) {
+#pragma unroll
+            for (int i = 0; i < (BACK ? 8 : 4); ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) a[i][e] = finite2(a[i][e]);
+            ctl[1] = 1;
+          }
+          if constexpr (BACK) {
+            if (gq < steps * 4) {
+              unsigned char* const wst = lds + (2 * (gq >> 2) + (pc >> 4)) * kHalfBytes + (kBlocksM / 2 + ((pc >> 1) & 7)) * kBlockBytes;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int n = (pc & 1) * 8 + i;
+                *(u32x4*)(wst + n * 128 + (((gq & 3) ^ swz(n)) << 4)) = a[i];
+                *(u32x4*)(wst + n * 128 + ((((gq & 3) + 4) ^ swz(n)) << 4)) = a[i];
+              }
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if ((i >> 1) >= steps) continue;
+              // columns 8 (e % 16) of the site: half (e % 16) / 8, piece of 16 columns there: 4 s + ((e % 16) % 8) / 2
+              const int e = (i & 1) * 256 + tb, k = e >> 4, cp = e & 15;
+              unsigned char* const wst = lds + (2 * (i >> 1) + (cp >> 3)) * kHalfBytes + (kBlocksM / 2) * kBlockBytes + (cp & 1) * 16;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                unsigned char* const line = wst + (k + 32 * h) * 256;
+                *(u32x4*)(line + (((4 * s + ((cp & 7) >> 1)) ^ swz_tr(k)) & 7) * 32) = a[i];
+                *(u32x4*)(line + (((4 * (1 - s) + ((cp & 7) >> 1)) ^ swz_tr(k)) & 7) * 32) = u32x4{0u, 0u, 0u, 0u};
+              }
+            }
+          }
+          wait_vm<0>();
+          __syncthreads();
+          for (int st = 0; st < steps; ++st) mma64(std::integral_constant<bool, GATED>{}, 2 * st + wm, 2 * st + wn, []() {}, [](int) {});
+          __syncthreads();
+        }
+        last = cur;
+      }
+    }
   }
 
   // ---- bias, one rounding, store: of a 32 x 32 tile a lane holds row l % 32 and, in registers 4 g .. 4 g + 3, the
@@ -736,6 +831,7 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
   p.X = g.X; p.W = g.Wg; p.W2 = g.Wu; p.Y = g.Y; p.gate_out = g.gate_out; p.up_out = g.up_out;
   p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
+  p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
   p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
   return launch_prefill<kGated>(p, g.M, g.row_base, stream);
 }
@@ -759,7 +855,7 @@ size_t back_partial_floats(int64_t M, int d, int F) {
 }
 
 bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX) {
-  if (F % kTK != 0 || d % 16 != 0 || M < 1) return false;
+  if (F % kTK != 0 || d % 16 != 0 || M < 1 || M > kHalvesRows) return false;
   if ((((uintptr_t)dz | (uintptr_t)Wg | (uintptr_t)Wu) & 15) != 0 || ((uintptr_t)dX & 7) != 0) return false;
   return (uint64_t)d * kTK * 2u < (1ull << 31) && (uint64_t)F * 4u * kTM < (1ull << 32) && (int64_t)((d + kTN - 1) / kTN) <= 1 << 16;
 }
@@ -788,6 +884,7 @@ int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
   PParams p{};
   p.X = g.dz; p.W = g.Wg; p.W2 = g.Wu; p.Y = g.dX; p.t = g.low; p.t_stride = g.low_stride; p.t_site = g.low_site; p.parts = g.parts;
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
+  p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
   p.d1 = 2 * g.F; p.d2 = g.d; p.site = 4; p.B = g.B;
   p.S = back_parts(g.M, g.d, g.F, &p.steps);
   p.partial = p.S > 1 ? g.partial : nullptr;

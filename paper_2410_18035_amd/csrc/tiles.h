@@ -25,7 +25,7 @@ constexpr int kTileCtrlOffset = kStreamCtrlBytes - kTileCtrlBytes;
 
 // `small`: the tiles of tiles.hip are a choice up to kTileMaxRows rows (tiles_supported); `large`: the 256 x 256 kernel is one
 // (row-major weights, 64 rows or more).  At least one of them.
-TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large);
+TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated = false);
 // The most partial_bytes over the plans of all calls of up to these sizes; never less for a larger size.
 size_t partial_bytes_bound(int64_t M, int d1, int d2);
 bool tiles_supported(int64_t M, int d1, int d2, bool packed, const void* X, const void* W, const void* Y);
@@ -37,6 +37,17 @@ int routed_linear_tiles(const bf16_t* X, int64_t M, int d1, int d2, const int32_
 
 // The gated block Y = silu(X Wg + its term) * (X Wu + its term): gate and up columns side by side in a tile (plan_tiles and
 // tiles_supported with 2 F columns).  kTiles256: gated_prefill.
+// Shrinks of the two sites as bf16 halves (gated.hip): [site][chunk of 32 ranks][1 + M] lines of 64 values, 32 high and 32 low, the first line zero.
+struct Halves {
+  bf16_t* at;
+  size_t site, chunk;  // elements from one's to the next's
+};
+constexpr int64_t kHalvesRows = (int64_t)1 << 24;  // (32-bit byte offsets of the lines)
+inline Halves halves_of(bf16_t* at, int64_t M, int r_max) {
+  const size_t chunk = (size_t)(M + 1) * 64;
+  return Halves{at, chunk * ((r_max + 31) / 32), chunk};
+}
+
 struct GatedTileArgs {
   const bf16_t* X;
   int64_t M, row_base;  // rows of the launch, index of the first in the caller's matrix (requests of unmapped rows)
@@ -44,8 +55,9 @@ struct GatedTileArgs {
   const int32_t* row_to_req;
   const bf16_t *Wg, *Wu;
   bool packed;
-  const int2* row_lora;  // [2][lora_site], or null: the terms by the matrix cores
+  const int2* row_lora;  // [2][lora_site]; kTiles64, kTiles128: or null, the terms by the matrix cores
   size_t lora_site;
+  Halves halves;         // kTiles256
   AdapterView ad;
   const int32_t* tenant_id;
   const uint8_t* route;
@@ -72,6 +84,9 @@ struct GatedBackArgs {
   const int32_t* tenant_id;
   const uint8_t* route;
   int B;
+  const int2* row_lora;  // [2][lora_site]
+  size_t lora_site;
+  Halves halves;     // of low
   const float* low;  // [2][part][M][r_max] = dz W^B^T, to be added in part order
   size_t low_stride, low_site;
   int parts;

@@ -733,7 +733,10 @@ int launch_tiles(const TParams& p, hipStream_t st) {
 // 2.7 turns; below that, 300 rows on 4096 x 11008: 258, 70.2 us against 66.5 with 64 x 64; packed weights, for which there is no
 // 256 x 256 kernel, keep the choice between 64 and 128 that was timed for them); cutting the reduction costs the
 // partial tiles and the last workgroup's sums (M = 64 on 4096 x 4096: one part 25.0 us a call, two 19.8, four 16.4, six 22.2).
-TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large) {
+// The gated block (gate and up columns: twice its width): what a turn costs more with two terms and the activation, 10 us with 128 x 128
+// tiles, 12 with 256 x 256 (4096 x 11008, requests of three sites, ranks 8 to 64, 128 x 128 / 256 x 256 tiles: 300 rows 142 / 126 us, 500
+// 177 / 132, 777 267 / 228, 2000 585 / 359).
+TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated) {
   const int KT = (d1 + 63) / 64;
   TilePlan best{};
   int64_t best_t = INT64_MAX;
@@ -752,10 +755,10 @@ TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large) {
   };
   if (small && M <= kTileMaxRows)
     for (int S = 1; S <= kMaxParts; ++S) {
-      offer(kTiles64, 64, 26, 200, S, 400 + 70 * S);
-      offer(kTiles128, 128, 58, 400, S, 250 + 220 * S);
+      offer(kTiles64, 64, 26, gated ? 700 : 200, S, 400 + 70 * S);
+      offer(kTiles128, 128, 58, gated ? 1400 : 400, S, 250 + 220 * S);
     }
-  if (large) offer(kTiles256, 256, 163, 775, 1, 0);
+  if (large) offer(kTiles256, 256, 163, gated ? 1975 : 775, 1, 0);
   return best;
 }
 
