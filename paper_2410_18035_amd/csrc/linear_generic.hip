@@ -292,13 +292,14 @@ struct GenCfg {
   static constexpr int BufFloats = (BM + BN) * Ld;
   static constexpr int LdR = BN + 4;
   static constexpr int Outs = BM * BN / T;                           // outputs per thread
-  static constexpr int TsOff = KQ * BM * LdR;                        // after the sums: t of the rows, 32 ranks at a time
-  static constexpr int LdsBytes = (2 * BufFloats > TsOff + BM * 32 ? 2 * BufFloats : TsOff + BM * 32) * 4;
+  static constexpr int TsOff = KQ * BM * LdR;                        // after the sums: t of the rows (of two sites), 32 ranks at a time
+  static constexpr int LdsBytes = (2 * BufFloats > TsOff + 2 * BM * 32 ? 2 * BufFloats : TsOff + 2 * BM * 32) * 4;
   static_assert((BM + BN) * (SK / 4) % T == 0 && BM * BN % T == 0 && KW % 8 == 0 && 2 * LdsBytes <= 158 * 1024, "tile shape");
 };
 typedef GenCfg<32, 32, 16> GenSmall;
 typedef GenCfg<64, 64, 32> GenLarge;
 constexpr int kGenLargeTiles = 128;
+constexpr int kGenGroupM = 8;  // row tiles of a column tile before the next one
 
 // GATED: the columns of a tile are as many of the gate (W, t) and then of the up projection (W2, t of the next site): Y = silu(g) u, with g
 // and u in fp32, which go to gate_out and up_out, if given.
@@ -309,15 +310,23 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
                                                            const int32_t* __restrict__ tenant_id,
                                                            const uint8_t* __restrict__ route, int B,
                                                            const float* __restrict__ t, int64_t t_site, T* __restrict__ Y,
-                                                           float* __restrict__ gate_out, float* __restrict__ up_out) {
+                                                           float* __restrict__ gate_out, float* __restrict__ up_out, int tiles_m, int tiles_n) {
   constexpr int kSites = GATED ? 2 : 1, kOutN = C::BN / kSites;
   extern __shared__ __attribute__((aligned(16))) float buf[];
   __shared__ int s_rank[kSites][C::BM], s_ten[kSites][C::BM], s_most[kSites];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = w / (C::WM * C::WN), wm = w % (C::WM * C::WN) % C::WM, wn = w % (C::WM * C::WN) / C::WM;
-  const int64_t m0 = (int64_t)blockIdx.y * C::BM;
-  const int n0 = col0 + blockIdx.x * kOutN;
+  // workgroup -> tile: ids go round-robin over the 8 XCDs; each XCD takes a contiguous run of an order that walks kGroupM row tiles of one column
+  // tile before the next column tile, so that its L2 serves the re-reads of W (gated block, 300 rows of 1000 x 2730, columns first: 52 us without
+  // LoRA rows)
+  const int total = tiles_m * tiles_n, per = (total + 7) >> 3;
+  const int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const int first = id / (kGenGroupM * tiles_n) * kGenGroupM, in_group = id % (kGenGroupM * tiles_n);
+  const int gsz = tiles_m - first < kGenGroupM ? tiles_m - first : kGenGroupM;
+  const int64_t m0 = (int64_t)(first + in_group % gsz) * C::BM;
+  const int n0 = col0 + in_group / gsz * kOutN;
 
   const T* src[C::Items];
   const int kq = tid % (C::SK / 4) * 4;
@@ -409,8 +418,7 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
     *reinterpret_cast<f32x4*>(buf + (size_t)(q * C::BM + wm * 32 + l32) * C::LdR + wn * 32 + g * 8 + lh * 4) =
         f32x4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
   __syncthreads();
-  const int nc = tid % C::BN, r0 = tid / C::BN, n = n0 + nc % kOutN, my = GATED ? nc / kOutN : 0;
-  constexpr int kStep = C::T / C::BN;
+  const int nc = tid % C::BN, r0 = tid / C::BN * C::Outs, n = n0 + nc % kOutN, my = GATED ? nc / kOutN : 0;
   const int ns = n < d2 ? n : d2 - 1;
   const float bv = bias ? Elem<T>::load(bias, ns) : 0.f;
   float val[C::Outs];
@@ -418,53 +426,53 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
   for (int i = 0; i < C::Outs; ++i) {
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < C::KQ; ++k) v += buf[(size_t)(k * C::BM + r0 + i * kStep) * C::LdR + nc];
+    for (int k = 0; k < C::KQ; ++k) v += buf[(size_t)(k * C::BM + r0 + i) * C::LdR + nc];
     val[i] = v + bv;
   }
 
-  // LoRA expand, 32 ranks at a time; eight rows of W^B for all of a thread's outputs on their way together (one output after
-  // the other, each waited for its own loads: 43.4 us a call of 300 rows on 1000 x 2730 against 37.8 us)
-  float* const ts = buf + C::TsOff;
-#pragma unroll 1
-  for (int s = 0; s < kSites; ++s) {
-    const int most = s_most[s];
-    if (most <= 0) continue;
-    const float* const t_of = t + s * t_site;
-    const T* Bm[C::Outs];
-    int last[C::Outs];
-#pragma unroll
-    for (int i = 0; i < C::Outs; ++i) {
-      const int row = r0 + i * kStep;
-      last[i] = !GATED || my == s ? s_rank[s][row] - 1 : -1;
-      Bm[i] = last[i] >= 0 ? (const T*)ad.B[s_ten[s][row] * MILORA_NUM_SITES + site + s] + ns : nullptr;
-    }
+  // LoRA expand, 32 ranks at a time: t of the rows by way of LDS; a thread's rows follow one another, so that they mostly belong to one tenant, whose
+  // sixteen rows of W^B it reads once for all of its outputs (eight rows of W^B for each output on their way together: 43.4 us a call of 300
+  // rows on 1000 x 2730 against 37.8 us; gated block of the same 82 us against 70)
+  float* const ts = buf + C::TsOff;  // [site][row][32]
+  int most = s_most[0];
+  if (GATED) most = s_most[kSites - 1] > most ? s_most[kSites - 1] : most;
+  if (most > 0) {
     for (int c0 = 0; c0 < most; c0 += 32) {
-      for (int e = tid; e < C::BM * 32; e += C::T) {
-        const int row = e >> 5, c = c0 + (e & 31);
-        ts[e] = c < s_rank[s][row] ? t_of[(size_t)(m0 + row) * ad.r_max + c] : 0.f;
+      for (int e = tid; e < kSites * C::BM * 32; e += C::T) {
+        const int s = e / (C::BM * 32), row = e / 32 % C::BM, c = c0 + (e & 31);
+        ts[e] = c < s_rank[s][row] ? t[s * t_site + (size_t)(m0 + row) * ad.r_max + c] : 0.f;
       }
       __syncthreads();
-      for (int c1 = 0; c1 < 32 && c0 + c1 < most; c1 += 8) {
-        float b[C::Outs][8];
+      const float* const tr = ts + (my * C::BM + r0) * 32;
+      unsigned left = 0;  // rows whose term is still to be added
+#pragma unroll
+      for (int i = 0; i < C::Outs; ++i)
+        if (s_rank[my][r0 + i] > c0) left |= 1u << i;
+      while (__any(left != 0)) {
+        const int row = r0 + (left ? __builtin_ctz(left) : 0), ten = s_ten[my][row], ranks = left ? s_rank[my][row] - c0 : 0;
+        const T* const b1 = ranks > 0 ? (const T*)ad.B[ten * MILORA_NUM_SITES + site + my] + (size_t)c0 * d2 + ns : nullptr;
+        unsigned mine = 0;
 #pragma unroll
         for (int i = 0; i < C::Outs; ++i)
+          if ((left >> i & 1) && s_ten[my][r0 + i] == ten) mine |= 1u << i;
+        for (int c1 = 0; __any(c1 < ranks) && c1 < 32; c1 += 16) {
+          float b[16];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int c = c0 + c1 + u;
-            b[i][u] = c <= last[i] ? Elem<T>::load(Bm[i], (size_t)c * d2) : 0.f;
-          }
+          for (int u = 0; u < 16; ++u) b[u] = c1 + u < ranks ? Elem<T>::load(b1, (size_t)(c1 + u) * d2) : 0.f;
 #pragma unroll
-        for (int i = 0; i < C::Outs; ++i)
+          for (int i = 0; i < C::Outs; ++i)
+            if (mine >> i & 1)
 #pragma unroll
-          for (int u = 0; u < 8; ++u)
-            if (!GATED || my == s) val[i] += ts[(r0 + i * kStep) * 32 + c1 + u] * b[i][u];
+              for (int u = 0; u < 16; ++u) val[i] += tr[i * 32 + c1 + u] * b[u];  // (past the rank both are zero)
+        }
+        left &= ~mine;
       }
       __syncthreads();
     }
   }
 #pragma unroll
   for (int i = 0; i < C::Outs; ++i) {
-    const int64_t m = m0 + r0 + i * kStep;
+    const int64_t m = m0 + r0 + i;
     if constexpr (GATED) {
       const float up = __shfl_xor(val[i], kOutN, 64);
       if (m >= M || n >= d2) continue;
@@ -504,14 +512,18 @@ int launch_tile(const TileArgs& g, hipStream_t stream) {
     MILORA_HIP(hipFuncSetAttribute((const void*)linear_tile_kernel<T, C, WIDE, GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LdsBytes));
     lds_set_for = dev;
   }
-  constexpr int kOutN = GATED ? C::BN / 2 : C::BN, kCols = kLaunchCols / 64 * kOutN;
+  constexpr int kOutN = GATED ? C::BN / 2 : C::BN;
+  const int tiles_m = (int)((g.M + C::BM - 1) / C::BM);
+  const int64_t most = (int64_t)1 << 22;  // tiles of a launch: a grid has to stay below 2^32 threads
+  const int64_t cols_most = (most / tiles_m > 0 ? most / tiles_m : 1) * kOutN;
   int rc = MILORA_OK;
-  for (int64_t col0 = 0; col0 < g.d2 && !rc; col0 += kCols) {
-    const int cols = g.d2 - col0 < kCols ? (int)(g.d2 - col0) : kCols;
-    dim3 grid((unsigned)((cols + kOutN - 1) / kOutN), (unsigned)((g.M + C::BM - 1) / C::BM));
-    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE, GATED>), grid, dim3(C::T), C::LdsBytes, stream, (const T*)g.X, g.M, g.d1, g.d2, (int)col0,
-                       g.row_to_req, (const T*)g.W, (const T*)g.W2, (const T*)g.bias, g.ad, g.site, g.tenant_id, g.route, g.B, g.t, g.t_site,
-                       (T*)g.Y, g.gate_out, g.up_out);
+  for (int64_t col0 = 0; col0 < g.d2 && !rc; col0 += cols_most) {
+    const int64_t cols = g.d2 - col0 < cols_most ? g.d2 - col0 : cols_most;
+    const int tiles_n = (int)((cols + kOutN - 1) / kOutN);
+    const int64_t grid = ((int64_t)tiles_m * tiles_n + 7) / 8 * 8;
+    hipLaunchKernelGGL((linear_tile_kernel<T, C, WIDE, GATED>), dim3((unsigned)grid), dim3(C::T), C::LdsBytes, stream, (const T*)g.X, g.M, g.d1,
+                       g.d2, (int)col0, g.row_to_req, (const T*)g.W, (const T*)g.W2, (const T*)g.bias, g.ad, g.site, g.tenant_id, g.route, g.B,
+                       g.t, g.t_site, (T*)g.Y, g.gate_out, g.up_out, tiles_m, tiles_n);
     rc = check_launch();
   }
   return rc;
