@@ -387,6 +387,13 @@ constexpr int64_t kMxFewRows = 128;
 
 bool mx4_rowmajor(int d1) { return d1 % 64 == 0; }  // the layout a weight is written out in
 
+// Do 256 x 256 tiles multiply the codes themselves?  Unless other tiles (pl) make up for writing the weight out.
+bool mx4_linear_direct(int64_t M, int d1, int d2, const LinearPlan& pl) {
+  if (!mx4_prefill_supported(M, d1, d2)) return false;
+  const int64_t other = pl.kind == MILORA_KERNEL_TILES && pl.slice == M ? pl.tiles.time : INT64_MAX / 2;
+  return plan_tiles(M, d1, d2, false, true).time <= other + write_out_time(d1, d2);
+}
+
 int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const bf16_t* bias,
                    const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, bf16_t* Y, void* workspace,
                    hipStream_t st) {
@@ -397,6 +404,21 @@ int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* ro
     return launch_mx4_rows(g, 1, false, workspace, st);
   }
   const bool packed = !mx4_rowmajor(d1);
+  const LinearPlan pl = plan_linear(M, d1, d2, MILORA_BF16, packed, X, (const void*)(uintptr_t)256, Y);
+  if (mx4_linear_direct(M, d1, d2, pl)) {
+    GatedTileArgs a{};
+    const int parts = shrink_parts(M, d1);
+    float* const t = (float*)workspace;
+    int2* const looked_up = (int2*)((char*)t + align_up((size_t)M * ad.r_max * parts * sizeof(float), 256));
+    a.X = X; a.M = M; a.d = d1; a.F = d2; a.row_to_req = row_to_req; a.Wg = (const bf16_t*)W; a.mx4 = true;
+    a.row_lora = looked_up; a.lora_site = (size_t)M; a.halves = halves_of(nullptr, M, ad.r_max);
+    a.halves.at = (bf16_t*)((char*)looked_up + align_up((size_t)M * sizeof(int2), 256));
+    a.ad = ad; a.tenant_id = tenant_id; a.route = route; a.B = B; a.t = t; a.t_stride = (size_t)M * ad.r_max; a.t_site = a.t_stride * parts; a.parts = parts;
+    a.Y = Y;
+    int rc = launch_shrink_sites(X, d1, M, d1, row_to_req, ad, site, 1, tenant_id, route, B, t, looked_up, nullptr, st);
+    if (!rc) rc = launch_halves(t, parts, M, ad.r_max, looked_up, 1, a.halves, st);
+    return rc ? rc : linear_prefill_mx4(a, bias, site, st);
+  }
   const int rc = mx4_dequantize(W, workspace, MILORA_BF16, d1, d2, packed, st);
   if (rc) return rc;
   return run_linear(X, M, d1, d2, MILORA_BF16, row_to_req, workspace, packed, bias, ad, site, tenant_id, route, B, Y,
@@ -439,7 +461,10 @@ extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int
   const size_t few = mx4_rows_workspace_bytes(M < kMxFewRows ? M : kMxFewRows, d1, d2, r_max, 1);
   if (M <= kMxFewRows) return few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
-  return many > few ? many : few;
+  const size_t direct = align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256) + align_up((size_t)M * sizeof(int2), 256) +
+                        align_up(halves_of(nullptr, M, r_max).site * sizeof(bf16_t), 256);
+  const size_t most = many > direct ? many : direct;
+  return most > few ? most : few;
 }
 
 extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype, int w_layout) {
@@ -462,6 +487,7 @@ extern "C" int milora_routed_linear_tile(int64_t M, int d1, int d2, int dtype, i
   if (w_layout == MILORA_W_MX4 && kernel == MILORA_KERNEL_STREAM) return 0;
   const bool packed = w_layout == MILORA_W_PACKED || (w_layout == MILORA_W_MX4 && !mx4_rowmajor(d1));
   const LinearPlan p = plan_linear(M, d1, d2, dtype, packed, aligned, aligned, aligned);
+  if (w_layout == MILORA_W_MX4 && mx4_linear_direct(M, d1, d2, p)) return 256;
   if (p.kind != MILORA_KERNEL_TILES) return 0;
   return p.tiles.shape == kTiles256 ? 256 : p.tiles.shape == kTiles128 ? 128 : 64;
 }

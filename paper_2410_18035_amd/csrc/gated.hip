@@ -62,14 +62,14 @@ __global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __r
   line[32] = f32_to_bf16(x - bf16_to_f32(hi));
 }
 
-int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, const Halves& out, hipStream_t st) {
-  const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), 2);
+// ---- forward ---------------------------------------------------------------------------------------------------------------
+}  // namespace
+
+int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st) {
+  const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), (unsigned)sites);
   hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, v, (size_t)M * r_max, parts, M, r_max, row_lora, out);
   return check_launch();
 }
-
-// ---- forward ---------------------------------------------------------------------------------------------------------------
-}  // namespace
 
 constexpr int64_t kMxGatedRows = 128;  // up to this many rows the few-row kernel reads the codes, beyond the weights are written out in bf16
 
@@ -123,7 +123,20 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     a.partial = c.take<float>(partial_bytes_bound(M, g.d, 2 * g.F) / sizeof(float));
     a.halves = halves_of(nullptr, M, g.ad.r_max);
     a.halves.at = c.take<bf16_t>(a.halves.site * 2);
-    if (g.mx4) {
+    // slices of rows where the smaller tiles are the only ones and the call has more than a launch of them takes
+    int64_t slice = large || M <= kTileMaxRows ? M : kTileMaxRows;
+    TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large, true);
+    if (g.mx4 && mx4_prefill_supported(M, g.d, g.F)) {  // the codes themselves by 256 x 256 tiles, unless smaller ones make up for writing them out
+      const TilePlan direct = plan_tiles(M, g.d, 2 * g.F, false, true, true);
+      if (direct.time <= first.time + 2 * write_out_time(g.d, g.F)) {
+        first = direct;
+        slice = M;
+        a.mx4 = true;
+        Wg = g.Wg;
+        Wu = g.Wu;
+      }
+    }
+    if (g.mx4 && !a.mx4) {
       bf16_t* const w = c.take<bf16_t>((size_t)g.d * g.F * 2);
       rc = mx4_dequantize(g.Wg, w, MILORA_BF16, g.d, g.F, packed, st);
       if (!rc) rc = mx4_dequantize(g.Wu, w + (size_t)g.d * g.F, MILORA_BF16, g.d, g.F, packed, st);
@@ -133,14 +146,11 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     }
     a.Wg = (const bf16_t*)Wg;
     a.Wu = (const bf16_t*)Wu;
-    // slices of rows where the smaller tiles are the only ones and the call has more than a launch of them takes
-    const int64_t slice = large || M <= kTileMaxRows ? M : kTileMaxRows;
-    const TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large, true);
     const bool big = first.shape == kTiles256;
     int2* const row_lora = large && !big ? nullptr : looked_up;
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, row_lora,
                              !big && (row_lora || first.S > 1) ? a.cnt : nullptr, st);
-    if (!rc && big) rc = launch_halves(t, parts, M, g.ad.r_max, looked_up, a.halves, st);
+    if (!rc && big) rc = launch_halves(t, parts, M, g.ad.r_max, looked_up, 2, a.halves, st);
     for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
       a.M = M - m0 < slice ? M - m0 : slice;
       a.row_base = m0;
@@ -679,7 +689,7 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   if ((rc = check_launch())) return rc;
   const int low_parts = shrink_parts(M, g.F);
   const size_t row_floats = (size_t)M * r_max;
-  if ((rc = launch_halves(w.low, low_parts, M, r_max, w.row_lora, w.low_halves, st))) return rc;
+  if ((rc = launch_halves(w.low, low_parts, M, r_max, w.row_lora, 2, w.low_halves, st))) return rc;
   if (dX) {
     GatedBackArgs a{};
     a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
@@ -693,7 +703,7 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   if (!dA && !dB) return rc;
   if (dB) {
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
-    if (!rc) rc = launch_halves(w.t, shrink_parts(M, g.d), M, r_max, w.row_lora, w.t_halves, st);
+    if (!rc) rc = launch_halves(w.t, shrink_parts(M, g.d), M, r_max, w.row_lora, 2, w.t_halves, st);
     if (rc) return rc;
   }
   const int chunks = (r_max + 31) / 32;

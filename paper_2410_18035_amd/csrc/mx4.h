@@ -1,6 +1,6 @@
 // Interface of the 4-bit base weights (mx4.hip): storage, conversion, the few-row linears.
 #pragma once
-#include "common.h"
+#include "shrink.h"
 
 namespace milora {
 
@@ -10,6 +10,18 @@ constexpr int kMxGroup = 32;
 inline bool mx4_shape_ok(int d1, int d2) { return d1 >= 1 && d2 >= 1 && d1 % kMxGroup == 0; }
 inline size_t mx4_code_bytes(int d1, int d2) { return (size_t)d1 * d2 / 2; }
 inline size_t mx4_bytes(int d1, int d2) { return mx4_code_bytes(d1, d2) + (size_t)d1 * d2 / kMxGroup; }
+
+__device__ __forceinline__ float mx4_scale(uint32_t s) { return __uint_as_float(s << 23); }  // 255: the conversion gives NaN
+
+// Eight codes to eight bf16.
+__device__ __forceinline__ u32x4 mx4_bf16(uint32_t c, float scale) {
+  u32x4 v;
+  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+  return v;
+}
 
 int mx4_quantize(const void* src, int dtype, void* dst, int d1, int d2, hipStream_t st);
 // To [d2][d1] of `dtype`, or (bf16, d2 % 16 == 0) to the packed layout.

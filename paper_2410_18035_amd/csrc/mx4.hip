@@ -7,8 +7,6 @@
 // s = 255, its weights are NaN.
 #include "mx4.h"
 
-#include "shrink.h"
-
 namespace milora {
 namespace {
 
@@ -83,18 +81,6 @@ __global__ void __launch_bounds__(kQuantT) mx4_quantize_kernel(const T* __restri
       if ((threadIdx.x & 3) == 0) scales[i >> 2] = finite ? (uint8_t)s : (uint8_t)255;
     }
   }
-}
-
-__device__ __forceinline__ float mx4_scale(uint32_t s) { return __uint_as_float(s << 23); }  // 255: the conversion gives NaN
-
-// Eight codes to eight bf16.
-__device__ __forceinline__ u32x4 mx4_bf16(uint32_t c, float scale) {
-  u32x4 v;
-  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
-  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
-  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
-  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
-  return v;
 }
 
 // A thread takes eight codes at a time.  PACKED: in the order of the packed layout (16 columns x 32 inputs a block).  Bound: HBM.

@@ -16,7 +16,7 @@
 // Bias is added and the result rounded once at the store.
 #include <type_traits>
 
-#include "shrink.h"
+#include "mx4.h"
 #include "tiles.h"
 
 namespace milora {
@@ -109,10 +109,19 @@ __device__ __forceinline__ bf16x8 read_tr(uint32_t at) {  // rows k .. k + 3 and
   return __builtin_bit_cast(bf16x8, v);
 }
 
-template <int MODE>
+//
+// MX: W (and W2) are 4-bit weights; a half's W side is 128 columns x 32 bytes of codes, four copies, and a wave brings four copies of X and one of
+// W.  A lane reads the 32 codes of one group of one column at once, so sub-step ks holds the inputs 32 (l / 32) + 8 ks .. + 7 on both sides, and
+// turns eight of them into an operand by four conversions between the matrix instructions of the sub-step before.  The scales come sixteen bytes
+// of a column at a time, for eight steps, into the ends of ring slots 0 and 1.  (A weight written out in bf16 first costs 20 us per 45 M values.)
+constexpr int kScaleAt = 24 * 1024, kScaleBytes = kTN * 16;
+template <int MODE, bool MX>
 __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   constexpr bool GATED = MODE == kGated, BACK = MODE == kBack;
+  constexpr bool HALVES = MODE != kPlain || MX;  // LoRA terms from prepared halves
   constexpr int kSites = MODE == kPlain ? 1 : 2;
+  constexpr int kCopies = MX ? 5 : 8;  // of a half by a wave
+  static_assert(!(BACK && MX), "the backward pass multiplies rows of W");
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -147,23 +156,39 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const unsigned char* src = is_w ? (const unsigned char*)(GATED && wave == 3 ? p.W2 : p.W) : (const unsigned char*)p.X;
   const int64_t row0 = is_w ? (int64_t)n0 : m0;
   const int64_t rlim = is_w ? (int64_t)p.d2 : p.M;
-  uint32_t voff[2][8];
+  uint32_t voff[2][kCopies];
+  if constexpr (MX) {
 #pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
+    for (int hh = 0; hh < 2; ++hh) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int rr = lane >> 3;
-      const int block = GATED && is_w ? hh * 4 + (j >> 1) : hh * 8 + (wave & 1) * 4 + (j >> 1);
-      int64_t r = row0 + block * 16 + (j & 1) * 8 + rr;
-      r = r < rlim ? r : rlim - 1;
-      voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((j & 1) * 8 + rr)) * 16u);
-      if (BACK && is_w) {  // four rows of 128 columns
-        const int k = ((wave & 1) * 8 + j) * 4 + (lane >> 4);
-        int n = n0 + hh * 128 + (((lane & 15) >> 1) ^ swz_tr(k)) * 16 + (lane & 1) * 8;
-        n = n < p.d2 ? n : p.d2 - 8;  // past the edge: results dropped
-        voff[hh][j] = (uint32_t)k * (uint32_t)p.d2 * 2u + (uint32_t)n * 2u;
+      for (int j = 0; j < 4; ++j) {
+        const int i = wave * 4 + j, rr = lane >> 3;
+        int64_t r = m0 + hh * 128 + i * 8 + rr;
+        r = r < p.M ? r : p.M - 1;
+        voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((i & 1) * 8 + rr)) * 16u);
       }
+      int n = GATED ? n0 + hh * 64 + (wave & 1) * 32 + (lane >> 1) : n0 + hh * 128 + wave * 32 + (lane >> 1);
+      n = n < p.d2 ? n : p.d2 - 1;
+      voff[hh][4] = (uint32_t)n * (uint32_t)(p.d1 >> 1) + (uint32_t)(lane & 1) * 16u;
     }
+  } else {
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int rr = lane >> 3;
+        const int block = GATED && is_w ? hh * 4 + (j >> 1) : hh * 8 + (wave & 1) * 4 + (j >> 1);
+        int64_t r = row0 + block * 16 + (j & 1) * 8 + rr;
+        r = r < rlim ? r : rlim - 1;
+        voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((j & 1) * 8 + rr)) * 16u);
+        if (BACK && is_w) {  // four rows of 128 columns
+          const int k = ((wave & 1) * 8 + j) * 4 + (lane >> 4);
+          int n = n0 + hh * 128 + (((lane & 15) >> 1) ^ swz_tr(k)) * 16 + (lane & 1) * 8;
+          n = n < p.d2 ? n : p.d2 - 8;  // past the edge: results dropped
+          voff[hh][j] = (uint32_t)k * (uint32_t)p.d2 * 2u + (uint32_t)n * 2u;
+        }
+      }
+  }
   // (BACK: the second half of the reduction is the second weight's)
   const int half_steps = p.d1 / kTK / 2, back_by = BACK && is_w ? half_steps : 0;
   const unsigned char* const src2 = BACK && is_w ? (const unsigned char*)p.W2 : src;
@@ -172,22 +197,40 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // half H = 2 * (k step) + hh lives in ring slot H % kHalves
   // copy j (0..7) of a half; a wave's eight copies of a half are spread between its matrix instructions: issued
   // back to back they would hold the wave at the issue of the memory instructions while the matrix cores idle
+  const unsigned char* const codes = (const unsigned char*)(GATED && wave >= 2 ? p.W2 : p.W);  // (MX) of this wave's copies
   auto issue_one = [&](int kt, int hh, int slot, int j) __attribute__((always_inline)) {
+    if constexpr (MX) {
+      const int kk = kt < KT ? kt : KT - 1;
+      if (j < 4) copy_to_lds16((const unsigned char*)p.X + (size_t)kk * (kTK * 2), voff[hh][j], lds0 + slot * kHalfBytes + (wave * 4 + j) * 1024);
+      else copy_to_lds16(codes + (size_t)kk * 32, voff[hh][4], lds0 + slot * kHalfBytes + (kBlocksM / 2) * kBlockBytes + wave * 1024);
+      return;
+    }
     const int kk = kt0 + (kt < KT ? kt : KT - 1);  // past the end: re-read the last step into a slot nobody reads
     const bool second = BACK && kk >= half_steps;
     const unsigned char* b = (second ? src2 : src) + (size_t)(second ? kk - back_by : kk) * (BACK ? k_bytes : kTK * 2);
     const uint32_t dst = lds0 + slot * kHalfBytes + dst_in_half;
     copy_to_lds16(b, voff[hh][j], dst + j * 1024);
   };
+  // (MX) scales of steps 8 gr .. + 7 of the tile's 256 columns, 64 of them by a wave; the last sixteen bytes of a column where it ends sooner
+  const int scale_bytes = p.d1 >> 5;
+  auto issue_scales = [&](int gr) __attribute__((always_inline)) {
+    const unsigned char* const w = (const unsigned char*)(GATED && (wave & 1) ? p.W2 : p.W) + (size_t)p.d1 * p.d2 / 2;
+    int n = GATED ? n0 + (wave >> 1) * 64 + lane : n0 + wave * 64 + lane;
+    n = n < p.d2 ? n : p.d2 - 1;
+    const int at = gr * 16 < scale_bytes - 16 ? gr * 16 : scale_bytes - 16;
+    copy_to_lds16(w + at, (uint32_t)n * (uint32_t)scale_bytes, lds0 + (gr & 1) * kHalfBytes + kScaleAt + wave * 1024);
+  };
   auto issue = [&](int kt, int hh, int slot) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) issue_one(kt, hh, slot, j);
+    for (int j = 0; j < kCopies; ++j) issue_one(kt, hh, slot, j);
   };
 
-  int2 lora[2] = {int2{-1, 0}, int2{-1, 0}};  // (kGated, kBack) of row tid, at the two sites
-  if (MODE != kPlain && m0 + tid < p.M && (!BACK || part == p.S - 1))
+  int2 lora[kSites];  // (HALVES) of row tid, at the sites
 #pragma unroll
-    for (int s = 0; s < 2; ++s) lora[s] = p.row_lora[s * p.lora_site + p.row_base + m0 + tid];
+  for (int s = 0; s < kSites; ++s) lora[s] = int2{-1, 0};
+  if (HALVES && m0 + tid < p.M && (!BACK || part == p.S - 1))
+#pragma unroll
+    for (int s = 0; s < kSites; ++s) lora[s] = p.row_lora[s * p.lora_site + p.row_base + m0 + tid];
 
   // acc[i][j]: rows 32 i .. 32 i + 31 of the wave's X part against rows 32 j .. of its W part
   f32x16 acc[4][4];
@@ -253,6 +296,46 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
   };
 
+  // (MX) the same for a step whose W side are codes
+  int rdx[4];
+  if constexpr (MX)
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+      rdx[ks] = (rrow >> 4) * kBlockBytes + (rrow & 15) * 128 + ((((lane >> 5) * 4 + ks) ^ swz(rrow & 15)) << 4);
+  auto mma64_mx = [&](int slot_x, int slot_w, const unsigned char* scales, auto mid, auto copy) __attribute__((always_inline)) {
+    const unsigned char* sa = lds + slot_x * kHalfBytes;
+    const unsigned char* sb = wbase + slot_w * kHalfBytes + rrow * 32 + (lane >> 5) * 16;
+    bf16x8 a[4][4], b[4][4];
+    u32x4 c[4];
+    float scale[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      c[j] = *(const u32x4*)(sb + j * 1024);
+      scale[j] = mx4_scale(scales[j * 512]);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[ks][i] = *(const bf16x8*)(sa + rdx[ks] + i * 2 * kBlockBytes);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[0][j] = __builtin_bit_cast(bf16x8, mx4_bf16(c[j][0], scale[j]));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 64; ++q) {
+      const int ks = q >> 4;
+      acc[(q >> 2) & 3][q & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[ks][q & 3], a[ks][(q >> 2) & 3], acc[(q >> 2) & 3][q & 3], 0, 0, 0);
+      if (q < 16 && !(q & 1)) a[2 + (q >> 3)][(q >> 1) & 3] = *(const bf16x8*)(sa + rdx[2 + (q >> 3)] + ((q >> 1) & 3) * 2 * kBlockBytes);
+      if (ks < 3 && (q & 3) == 1) b[ks + 1][(q >> 2) & 3] = __builtin_bit_cast(bf16x8, mx4_bf16(c[(q >> 2) & 3][ks + 1], scale[(q >> 2) & 3]));
+      copy(q);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q == 15) {
+        mid();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+
+  if constexpr (MX) issue_scales(0);
   issue(0, 0, 0);
   issue(0, 1, 1);
   issue(1, 0, 2);
@@ -275,24 +358,30 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     const int h1 = h0 + 1 >= kHalves ? h0 + 1 - kHalves : h0 + 1;
     const int h2 = h0 + 2 >= kHalves ? h0 + 2 - kHalves : h0 + 2;
     const int h4 = h0 + 4 >= kHalves ? h0 + 4 - kHalves : h0 + 4;
-    wait_vm<16>();                  // all but the two halves issued last have landed: both halves of this step
+    wait_vm<2 * kCopies>();         // all but the two halves issued last have landed: both halves of this step
     __builtin_amdgcn_s_barrier();   // for every wave
     asm volatile("" ::: "memory");
-    mma64(
-        std::integral_constant<bool, BACK>{}, wm ? h1 : h0, wn ? h1 : h0,
-        [&]() __attribute__((always_inline)) {
-          __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's operand reads have returned
-          __builtin_amdgcn_s_barrier();        // and every other wave's
-          asm volatile("" ::: "memory");
-        },
-        [&](int q) __attribute__((always_inline)) {
-          // first half of the step after next into the free slot, second half into this step's first slot
-          if (q < kCopyB0) {
-            if (q % kCopyAStride == 0 && q / kCopyAStride < 8) issue_one(kt + 2, 0, h4, q / kCopyAStride);
-          } else if ((q - kCopyB0) % kCopyBStride == 0 && (q - kCopyB0) / kCopyBStride < 8) {
-            issue_one(kt + 2, 1, h0, (q - kCopyB0) / kCopyBStride);
-          }
-        });
+    if (MX && (kt & 7) == 0 && kt + 8 < KT) issue_scales((kt >> 3) + 1);
+    auto mid = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's operand reads have returned
+      __builtin_amdgcn_s_barrier();        // and every other wave's
+      asm volatile("" ::: "memory");
+    };
+    // first half of the step after next into the free slot, second half into this step's first slot
+    auto copy = [&](int q) __attribute__((always_inline)) {
+      if (q < kCopyB0) {
+        if (q % kCopyAStride == 0 && q / kCopyAStride < kCopies) issue_one(kt + 2, 0, h4, q / kCopyAStride);
+      } else if ((q - kCopyB0) % kCopyBStride == 0 && (q - kCopyB0) / kCopyBStride < kCopies) {
+        issue_one(kt + 2, 1, h0, (q - kCopyB0) / kCopyBStride);
+      }
+    };
+    if constexpr (MX) {
+      const int gr = kt >> 3, from = gr * 16 < scale_bytes - 16 ? gr * 16 : scale_bytes - 16;
+      mma64_mx(wm ? h1 : h0, wn ? h1 : h0,
+               lds + (gr & 1) * kHalfBytes + kScaleAt + (wn * 128 + rrow) * 16 + kt * 2 + (lane >> 5) - from, mid, copy);
+    } else {
+      mma64(std::integral_constant<bool, BACK>{}, wm ? h1 : h0, wn ? h1 : h0, mid, copy);
+    }
     asm volatile("" ::: "memory");
     h0 = h2;
   }
@@ -308,7 +397,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   int* ctl = (int*)(lds + 4 * kHalfBytes);  // ring slots 0 .. 3 hold the operand blocks
   int* const row_ten = ctl + 16;            // tenant of each row of the tile, -1: no LoRA term
   if (tid == 0) ctl[1] = 0;  // set: a matrix of some tenant of the tile holds Inf or NaN
-  if constexpr (MODE == kPlain) {
+  if constexpr (!HALVES) {
   int my_ten = -1;
   {
     const int64_t m = m0 + tid;
@@ -441,11 +530,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   } else {
     // The same for two sites, from the halves prepared in front of the launch: a line of them is a row of a step as it lies, copied straight into
     // LDS, the zero line for rows of other tenants; one round trip for 64 ranks of a tenant (with the shrinks' parts added and split here,
-    // 777 rows of 5 requests, three sites each, ranks 8 to 64, gated block of 4096 x 11008: 287 us a call).  kGated: 32 rows of W^B go in as they lie,
-    // [k][column], and are read transposed; the columns of the other projection are zero.  kBack: eight ranks of a column are eight consecutive
+    // 777 rows of 5 requests, three sites each, ranks 8 to 64, gated block of 4096 x 11008: 287 us a call).  32 rows of W^B go in as they lie,
+    // [k][column], and are read transposed; kGated: the columns of the other projection are zero.  kBack: eight ranks of a column are eight consecutive
     // values of W^A.
 #pragma unroll 1
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kSites; ++s) {
       const int my_ten = lora[s].y ? lora[s].x : -1;
       row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
       int last = -1;
@@ -489,21 +578,27 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
             if (gq < steps * 4 && n0 + pc * 8 < p.d2 && cw < r)
 #pragma unroll
               for (int i = 0; i < 8; ++i) a[i] = load8(Wm + (size_t)(n0 + pc * 8 + i) * r + cw, r - cw, vec_a);
-          } else {  // rank c0 + 32 (i / 2) + .., eight columns of the site: 512 pieces of a step, two a thread
+          } else if constexpr (GATED) {  // rank c0 + 32 (i / 2) + .., eight columns of the site: 512 pieces of a step, two a thread
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int e = (i & 1) * 256 + tb, c = c0 + (i >> 1) * 32 + (e >> 4), n = n0 + (e & 15) * 8;
               if ((i >> 1) < steps && c < r && n < p.d2) a[i] = *(gu32x4_a2*)(Wm + (size_t)c * p.d2 + n);
             }
+          } else {  // 1024 pieces of a step, four a thread
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int e = (i & 3) * 256 + tb, c = c0 + (i >> 2) * 32 + (e >> 5), n = n0 + (e & 31) * 8;
+              if ((i >> 2) < steps && c < r && n < p.d2) a[i] = *(gu32x4_a2*)(Wm + (size_t)c * p.d2 + n);
+            }
           }
           float taints[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < (BACK ? 8 : 4); ++i)
+          for (int i = 0; i < (GATED ? 4 : 8); ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) taints[e] = taint(taints[e], a[i][e]);
           if ((taints[0] + taints[1]) + (taints[2] + taints[3]) != 0.f) {
 #pragma unroll
-            for (int i = 0; i < (BACK ? 8 : 4); ++i)
+            for (int i = 0; i < (GATED ? 4 : 8); ++i)
 #pragma unroll
               for (int e = 0; e < 4; ++e) a[i][e] = finite2(a[i][e]);
             ctl[1] = 1;
@@ -517,6 +612,15 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
                 *(u32x4*)(wst + n * 128 + (((gq & 3) ^ swz(n)) << 4)) = a[i];
                 *(u32x4*)(wst + n * 128 + ((((gq & 3) + 4) ^ swz(n)) << 4)) = a[i];
               }
+            }
+          } else if constexpr (!GATED) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              if ((i >> 2) >= steps) continue;
+              const int e = (i & 3) * 256 + tb, k = e >> 5, cp = e & 31;
+              unsigned char* const wst = lds + (2 * (i >> 2) + (cp >> 4)) * kHalfBytes + (kBlocksM / 2) * kBlockBytes + (cp & 1) * 16;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) *(u32x4*)(wst + (k + 32 * h) * 256 + ((((cp & 15) >> 1) ^ swz_tr(k)) & 7) * 32) = a[i];
             }
           } else {
 #pragma unroll
@@ -535,7 +639,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           }
           wait_vm<0>();
           __syncthreads();
-          for (int st = 0; st < steps; ++st) mma64(std::integral_constant<bool, GATED>{}, 2 * st + wm, 2 * st + wn, []() {}, [](int) {});
+          for (int st = 0; st < steps; ++st) mma64(std::integral_constant<bool, !BACK>{}, 2 * st + wm, 2 * st + wn, []() {}, [](int) {});
           __syncthreads();
         }
         last = cur;
@@ -776,13 +880,13 @@ bool prefill_supported(int64_t M, int d1, int d2, const void* X, const void* W, 
   return (uint64_t)d2 * (uint64_t)d1 * 2u < (1ull << 32);  // 32-bit byte offsets inside W (X is cut into row slices)
 }
 
-template <int MODE>
+template <int MODE, bool MX>
 static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t stream) {
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel<MODE>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
+    MILORA_HIP(hipFuncSetAttribute((const void*)prefill_kernel<MODE, MX>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytesP));
     lds_set_for = dev;
   }
   // rows are independent: slices whose byte offsets inside X fit 32 bits and whose tile count fits a launch
@@ -807,7 +911,7 @@ static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t st
     p.tilesN = tilesN;
     const int total = p.tilesM * p.tilesN * (MODE == kBack ? p.S : 1);
     const int per = (total + 7) / 8;
-    hipLaunchKernelGGL(prefill_kernel<MODE>, dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
+    hipLaunchKernelGGL((prefill_kernel<MODE, MX>), dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
     const int rc = check_launch();
     if (rc) return rc;
   }
@@ -823,7 +927,7 @@ int routed_linear_prefill(const bf16_t* X, int64_t M, int d1, int d2, const int3
   p.parts = shrink_parts(M, d1);
   p.row_to_req = row_to_req; p.tenant_id = tenant_id; p.route = route; p.ad = ad;
   p.d1 = d1; p.d2 = d2; p.site = site; p.B = B;
-  return launch_prefill<kPlain>(p, M, 0, stream);
+  return launch_prefill<kPlain, false>(p, M, 0, stream);
 }
 
 int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
@@ -833,7 +937,24 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
   p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
   p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
-  return launch_prefill<kGated>(p, g.M, g.row_base, stream);
+  return g.mx4 ? launch_prefill<kGated, true>(p, g.M, g.row_base, stream) : launch_prefill<kGated, false>(p, g.M, g.row_base, stream);
+}
+
+// The same tiles on 4-bit weights (p.W in their place): LoRA terms from the halves of one site.
+int linear_prefill_mx4(const GatedTileArgs& g, const bf16_t* bias, int site, hipStream_t stream) {
+  PParams p{};
+  p.X = g.X; p.W = g.Wg; p.bias = bias; p.Y = g.Y;
+  p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
+  p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
+  p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
+  p.d1 = g.d; p.d2 = g.F; p.site = site; p.B = g.B;
+  return launch_prefill<kPlain, true>(p, g.M, g.row_base, stream);
+}
+
+// (scales are copied sixteen bytes at a time, from addresses that are multiples of four, the last ones from the end of a column's)
+bool mx4_prefill_supported(int64_t M, int d1, int d2) {
+  return M >= 64 && M <= kHalvesRows && d1 % 128 == 0 && d1 >= 512 && d2 % 16 == 0 && (uint64_t)d1 * 2u * kTM < (1ull << 32) &&
+         (uint64_t)d2 * d1 / 2 < (1ull << 32);
 }
 
 // Parts of the reduction: as many as make the tiles fill the compute units once, whole k steps each, eight at least.
@@ -889,7 +1010,7 @@ int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
   p.S = back_parts(g.M, g.d, g.F, &p.steps);
   p.partial = p.S > 1 ? g.partial : nullptr;
   p.partial_stride = (size_t)g.M * g.d;
-  const int rc = launch_prefill<kBack>(p, g.M, 0, stream);
+  const int rc = launch_prefill<kBack, false>(p, g.M, 0, stream);
   if (rc || p.S == 1) return rc;
   const int64_t fours = g.M * g.d / 4;
   hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, stream, g.partial, p.S, p.partial_stride, fours, g.dX);

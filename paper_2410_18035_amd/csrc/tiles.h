@@ -12,7 +12,10 @@ struct TilePlan {
   int tilesM, tilesN;
   int S, steps;          // parts of the reduction, stages of 64 k per part
   size_t partial_bytes;  // fp32 partial tiles in the workspace (0 when S == 1)
+  int64_t time;          // what the choice reckons, in 10 ns
 };
+// What writing a 4-bit weight out in bf16 takes, in 10 ns (4096 x 11008: 20 us).
+inline int64_t write_out_time(int d1, int d2) { return 300 + (int64_t)d1 * d2 / 26000; }
 constexpr int kStreamRows = 32;      // rows up to which a packed linear takes the weight-streaming kernel (decode.hip)
 constexpr int kMaxSplitUnits = 512;  // tiles x parts of a launch that cuts its reduction
 constexpr int kMaxParts = 8;         // of one reduction
@@ -55,6 +58,7 @@ struct GatedTileArgs {
   const int32_t* row_to_req;
   const bf16_t *Wg, *Wu;
   bool packed;
+  bool mx4;              // (kTiles256) Wg and Wu are 4-bit weights
   const int2* row_lora;  // [2][lora_site]; kTiles64, kTiles128: or null, the terms by the matrix cores
   size_t lora_site;
   Halves halves;         // kTiles256
@@ -72,6 +76,11 @@ struct GatedTileArgs {
 };
 int gated_tiles(const GatedTileArgs& g, const TilePlan& pl, hipStream_t st);
 int gated_prefill(const GatedTileArgs& g, hipStream_t st);
+bool mx4_prefill_supported(int64_t M, int d1, int d2);
+// A linear on 4-bit weights (g.Wg, g.d inputs, g.F columns), [1][..] shrinks, look-ups and halves.
+int linear_prefill_mx4(const GatedTileArgs& g, const bf16_t* bias, int site, hipStream_t st);
+// (gated.hip) v [site][part][M][r_max] to `sites` sites' halves.
+int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st);
 
 // dX = [dg | du] [W_gate; W_up] + sum over the two sites of low A^T on 256 x 256 tiles (prefill.hip).
 struct GatedBackArgs {

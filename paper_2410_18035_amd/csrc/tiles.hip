@@ -740,6 +740,7 @@ TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gate
   const int KT = (d1 + 63) / 64;
   TilePlan best{};
   int64_t best_t = INT64_MAX;
+  best.time = INT64_MAX;
   auto offer = [&](int shape, int side, int64_t per_step, int64_t per_tile, int S, int64_t split_cost) {
     const int64_t tm = (M + side - 1) / side, tn = (d2 + side - 1) / side, units = tm * tn * S;
     if (S > 1 && (units > kMaxSplitUnits || S > KT)) return;
@@ -750,7 +751,7 @@ TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gate
     if (rest && shape == kTiles256) t -= 46 * (256 - rest) / 256 * steps;
     if (t >= best_t) return;
     best_t = t;
-    best = TilePlan{shape, (int)tm, (int)tn, (KT + steps - 1) / steps, steps, 0};  // (no empty part)
+    best = TilePlan{shape, (int)tm, (int)tn, (KT + steps - 1) / steps, steps, 0, t};  // (no empty part)
     if (best.S > 1) best.partial_bytes = (size_t)(tm * tn) * best.S * side * side * sizeof(float);
   };
   if (small && M <= kTileMaxRows)

@@ -195,7 +195,8 @@ def test_forward_bf16(M, d, F, rows, ranks):
 
 @gpu
 @pytest.mark.parametrize("M,d,F,rows", [(1, 96, 16, "own"), (5, 1056, 48, "mixed"), (16, 64, 528, "own"), (33, 160, 80, "mixed"), (128, 512, 272, "own"),
-                                        (129, 96, 48, "mixed"), (200, 192, 272, "mixed"), (700, 512, 1040, "sorted"), (600, 1056, 304, "mixed")])
+                                        (129, 96, 48, "mixed"), (200, 192, 272, "mixed"), (700, 512, 1040, "sorted"), (600, 1056, 304, "mixed"),
+                                                        (1100, 512, 2064, "mixed"), (2049, 640, 2064, "sorted"), (1300, 1152, 2048, "mixed")])
 @pytest.mark.parametrize("ranks", [(8,), (5, 33, 256)])
 def test_forward_quantised(M, d, F, rows, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 6), 3, d, F, ranks, M + d, torch.bfloat16, rows, mx4=True)

@@ -199,6 +199,44 @@ def test_linear(M, d1, d2, rows, ranks):
 
 
 @gpu
+@pytest.mark.parametrize("M,d1,d2,rows,tile", [(2100, 512, 4112, "mixed", 256), (2049, 640, 4096, "sorted", 256), (2304, 1152, 4208, "sorted", 256),
+                                                (1800, 4224, 2064, "mixed", 128), (1800, 4224, 8080, "mixed", 256)])
+@pytest.mark.parametrize("ranks", [(8,), (5, 33, 256)])
+def test_linear_in_large_tiles(M, d1, d2, rows, tile, ranks):
+    """256 x 256 tiles read the codes: reductions of one to several groups of scales, the last one not whole."""
+    assert mb.milora_routed_linear_tile(M, d1, d2, torch.bfloat16, mb.W_MX4) == tile
+    test_linear(M, d1, d2, rows, ranks)
+
+
+@gpu
+def test_large_tiles_keep_nans_where_they_belong():
+    M, d1, d2, site = 2100, 640, 4112, 1
+    c = plain.Case(M, 4, 3, {site: (d1, d2)}, (8, 40, 16), 53, DEV, rows="mixed", sites=[site])
+    c.tid[:] = torch.tensor([0, 1, 2, 1])
+    x, w = c.rnd(M, d1), c.rnd(d2, d1)
+    tid, route = c.requests()
+    run = lambda x, w: mb.milora_routed_linear(x, mb.milora_quantize_weight(w), c.tab, site, tid, route, row_to_req=c.rows(), w_layout=mb.W_MX4, d2=d2)
+    clean = run(x, w)
+    assert torch.isfinite(clean).all()
+    w2 = w.clone()
+    w2[d2 - 1, 600] = w2[130, 0] = float("nan")
+    Y = run(x, w2)
+    keep = torch.ones(d2, dtype=torch.bool, device=DEV)
+    keep[[130, d2 - 1]] = False
+    assert torch.equal(Y[:, keep], clean[:, keep]) and torch.isnan(Y[:, ~keep]).all()
+    x2 = x.clone()
+    x2[M - 1, 639] = x2[300, 32] = float("inf")
+    Y = run(x2, w)
+    keep = torch.ones(M, dtype=torch.bool, device=DEV)
+    keep[[300, M - 1]] = False
+    assert torch.equal(Y[keep], clean[keep]) and not torch.isfinite(Y[~keep]).all(dim=1).any()
+    c.Bm[site][0][3, 7] = float("inf")
+    Y = run(x, w)
+    mine = (torch.tensor(c.tenants(site)) == 0).to(DEV)
+    assert mine.any() and torch.equal(Y[~mine], clean[~mine]) and not torch.isfinite(Y[mine][:, 7]).any()
+
+
+@gpu
 @pytest.mark.parametrize("M", [5, 40, 200])
 def test_linear_keeps_infinities_and_nans_where_they_belong(M):
     """A NaN group stays in its column, an Inf of X in its row, a tenant's Inf in its rows."""
