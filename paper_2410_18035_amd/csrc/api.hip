@@ -382,9 +382,8 @@ int run_linear(const void* X, int64_t M, int d1, int d2, int dtype, const int32_
 }
 
 // ---- 4-bit weights ----
-// Up to kMxFewRows rows the kernels of mx4.hip multiply the codes; beyond, the weight is written out in bf16 once per call, row-major or, where the row-major tiles do not take its reduction, packed.
-constexpr int64_t kMxFewRows = 128;
-
+// Few rows: the kernels of mx4.hip multiply the codes.  More: 256 x 256 tiles do, or the weight is written out in bf16 once per call, row-major or,
+// where the row-major tiles do not take its reduction, packed.
 bool mx4_rowmajor(int d1) { return d1 % 64 == 0; }  // the layout a weight is written out in
 
 // Do 256 x 256 tiles multiply the codes themselves?  Unless other tiles (pl) make up for writing the weight out.
@@ -397,7 +396,7 @@ bool mx4_linear_direct(int64_t M, int d1, int d2, const LinearPlan& pl) {
 int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const bf16_t* bias,
                    const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, bf16_t* Y, void* workspace,
                    hipStream_t st) {
-  if (M <= kMxFewRows) {
+  if (mx4_few_rows(M, d1, d2)) {
     MxArgs g{};
     g.X = X; g.ldx = d1; g.M = (int)M; g.d1 = d1; g.d2 = d2; g.W[0] = (const unsigned char*)W; g.bias = bias; g.Y[0] = Y; g.ldy = d2;
     g.ad = ad; g.site[0] = site; g.row_to_req = row_to_req; g.tenant_id = tenant_id; g.route = route; g.B = B;
@@ -458,8 +457,8 @@ extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2
 
 extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
   if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
-  const size_t few = mx4_rows_workspace_bytes(M < kMxFewRows ? M : kMxFewRows, d1, d2, r_max, 1);
-  if (M <= kMxFewRows) return few;
+  const size_t few = mx4_rows_workspace_bytes(M < kMxMostFew ? M : kMxMostFew, d1, d2, r_max, 1);
+  if (M <= kMxAlwaysFew) return few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
   const size_t direct = align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256) + align_up((size_t)M * sizeof(int2), 256) +
                         align_up(halves_of(nullptr, M, r_max).site * sizeof(bf16_t), 256);
@@ -472,7 +471,7 @@ extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype,
   if (!valid_layout(w_layout)) return MILORA_EINVAL;
   if (w_layout != MILORA_W_ROWMAJOR) {
     if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2)) return MILORA_EUNSUPPORTED;
-    if (w_layout == MILORA_W_PACKED || M <= kMxFewRows) return MILORA_KERNEL_STREAM;
+    if (w_layout == MILORA_W_PACKED || mx4_few_rows(M, d1, d2)) return MILORA_KERNEL_STREAM;
     return MILORA_KERNEL_TILES;
   }
   const void* aligned = (const void*)(uintptr_t)256;

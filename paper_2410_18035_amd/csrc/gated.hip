@@ -71,7 +71,6 @@ int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* r
   return check_launch();
 }
 
-constexpr int64_t kMxGatedRows = 128;  // up to this many rows the few-row kernel reads the codes, beyond the weights are written out in bf16
 
 size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
   size_t most = 0;
@@ -82,11 +81,11 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
     c.take<int2>((size_t)M * 2);
     c.take<char>(partial_bytes_bound(M, d, 2 * F));
     c.take<bf16_t>(halves_of(nullptr, M, r_max).site * 2);
-    if (mx4 && M > kMxGatedRows) c.take<bf16_t>((size_t)d * F * 2);
+    if (mx4 && M > kMxAlwaysFew) c.take<bf16_t>((size_t)d * F * 2);
     most = c.off;
     if (mx4) {
-      const size_t few = mx4_rows_workspace_bytes(M < kMxGatedRows ? M : kMxGatedRows, d, F, r_max, 2);
-      if (M <= kMxGatedRows) return few;
+      const size_t few = mx4_rows_workspace_bytes(M < kMxMostFew ? M : kMxMostFew, d, F, r_max, 2);
+      if (M <= kMxAlwaysFew) return few;
       most = few > most ? few : most;
     }
   }
@@ -97,7 +96,7 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
 int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void* workspace, hipStream_t st) {
   const int64_t M = g.M;
   int rc;
-  if (g.mx4 && M <= kMxGatedRows) {
+  if (g.mx4 && mx4_few_rows(M, g.d, 2 * (int64_t)g.F)) {
     MxArgs a{};
     a.X = (const bf16_t*)g.X; a.ldx = g.d; a.M = (int)M; a.d1 = g.d; a.d2 = g.F;
     a.W[0] = (const unsigned char*)g.Wg; a.W[1] = (const unsigned char*)g.Wu; a.Y[0] = (bf16_t*)Y; a.ldy = g.F;

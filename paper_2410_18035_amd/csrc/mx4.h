@@ -50,6 +50,13 @@ struct MxArgs {
   const uint8_t* route;
   int B;
 };
+// The few-row kernels read the codes for up to 128 rows, and for up to 512 while the products of all sites stay below 24e9.  Beyond, tiles are
+// faster, whose time hardly falls below 256 rows (us, few-row kernels / tiles: 4096 x 11008, 320 rows 76 / 115, 512 rows 107 / 107, 768 rows
+// 153 / 108; 5120 x 13824, 320 rows 115 / 136, 384 rows 137 / 131; gated 4096 x 11008, 256 rows 114 / 126, 320 rows 125 / 124).
+constexpr int64_t kMxAlwaysFew = 128, kMxMostFew = 512;
+inline bool mx4_few_rows(int64_t M, int d1, int64_t columns) {
+  return M <= kMxAlwaysFew || (M <= kMxMostFew && (double)M * d1 * columns <= 24e9);
+}
 size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites);
 // gated: sites = 2
 int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st);
