@@ -121,11 +121,11 @@ __global__ void __launch_bounds__(kQuantT) mx4_dequantize_kernel(const uint32_t*
 
 // ---- few rows: two launches a level -----------------------------------------------------------------------------------------
 // First launch: the base products and the LoRA shrinks, which do not depend on each other.  A workgroup of eight waves takes 256 / KW columns, 32 a
-// wave, and KW x NL x 64 inputs, all of them at once: a lane holds one group of 32 inputs of one column for each of NL steps, 16 bytes of codes straight
+// wave, and KW x NL x 64 inputs, all of them at once: a lane holds NL groups of 32 inputs, 16 bytes of codes each, straight
 // from global memory, every load on its way together; KW waves share the columns and split the inputs, so that few rows, whose X is small, need few
 // parts of the reduction or none.  X goes through LDS, 32 rows at a time; with more rows the codes stay in registers and the next rows' X is on its
-// way while these are multiplied.  Four matrix instructions of 8 inputs a lane multiply 64 inputs (which inputs stand at which place does not
-// matter as long as both operands agree).  The waves' sums meet in LDS, those of the parts in memory, in fp32.
+// way while these are multiplied.  Matrix instructions of 8 inputs a lane multiply the groups (which inputs stand at which place does not matter
+// as long as both operands agree), those of 16 x 16 up to 16 rows, which take half the time.  The waves' sums meet in LDS, those of the parts in memory, in fp32.
 // Second launch: adds the parts in part order, the LoRA term t W^B, bias and glue, and rounds once.
 // Bound: the stream of the codes; what short reductions cost is their sums' way through memory.  Tried: stages of 256 inputs with the next ones on
 // their way over a longer reduction (M = 64, 4096 x 4096: 23 us a call against 15), the whole reduction and the term in one launch with 2 x 8
@@ -205,9 +205,10 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   }
 }
 
-// MORE: more than 32 rows.
-template <int KW, int NL, bool MORE>
-__global__ void __launch_bounds__(kMxT, 4) mx4_base_kernel(const MxBase g) {
+// MORE: more than 32 rows.  XM: pieces of X a thread brings; with four (rows below five) the registers allow three workgroups a compute unit
+// (gated, one row of 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3).
+template <int KW, int NL, bool MORE, int XM>
+__global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -226,13 +227,16 @@ __global__ void __launch_bounds__(kMxT, 4) mx4_base_kernel(const MxBase g) {
   if (id >= total) return;
   constexpr int kCols = kMxCols / KW, kPart = KW * NL * 64;  // columns and inputs of the workgroup
   constexpr int kPitch = kPart * 2 + 16;                     // a row of X in LDS: 16 bytes past a multiple of all banks
-  const int l32 = lane & 31, lh = lane >> 5, kw = w % KW, cw = w / KW;
+  // Up to 16 rows: matrix instructions of 16 x 16, 32 inputs.  A lane's group g of a column: inputs 32 g of every kG x 32, kH columns a lane
+  constexpr bool k16 = KW >= 4;
+  constexpr int kSide = k16 ? 16 : 32, kG = 64 / kSide, kH = 32 / kSide, kS = NL / kH;  // kS steps of kG groups
+  const int ln = lane & (kSide - 1), lg = lane / kSide, kw = w % KW, cw = w / KW;
   int rg = id % row_split;
   const int part = id / row_split % g.parts, cg = id / (row_split * g.parts) % g.col_groups, site = id / (row_split * g.parts * g.col_groups);
   const int n0 = cg * kCols + cw * 32, k_part = part * kPart, k0 = k_part + kw * NL * 64;
 
   // ---- X: [row][kPart], asked for in front of the codes, which may come later ----
-  constexpr int kPieces = kPart / 8, kXMost = 8;  // (rows x kPieces is kXMost x kMxT at most: MxPlan)
+  constexpr int kPieces = kPart / 8, kXMost = XM;  // (rows x kPieces is kXMost x kMxT at most)
   u32x4 x[kXMost];
   auto ask_x = [&](int m0) __attribute__((always_inline)) {
 #pragma unroll
@@ -245,29 +249,32 @@ __global__ void __launch_bounds__(kMxT, 4) mx4_base_kernel(const MxBase g) {
   ask_x(rg * 32);
   __builtin_amdgcn_sched_barrier(0);
   // ---- codes and scales: NL steps ----
-  u32x4 c[NL];
-  uint64_t sc[NL / 4];
-  {
-    typedef uint64_t u64_a1 __attribute__((aligned(1)));
-    int col = n0 + l32;
+  u32x4 c[kH][kS];
+  typedef typename std::conditional<k16, uint32_t, uint16_t>::type scales_t;  // of a step: kG bytes
+  typedef scales_t scales_a1 __attribute__((ext_vector_type(4), aligned(1)));
+  scales_a1 sc[kH][kS / 4];
+#pragma unroll
+  for (int h = 0; h < kH; ++h) {
+    int col = n0 + h * kSide + ln;
     col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
-    const unsigned char* const wp = g.W[site] + (size_t)col * (d1 >> 1) + lh * 16 + (k0 >> 1);
+    const unsigned char* const wp = g.W[site] + (size_t)col * (d1 >> 1) + lg * 16 + (k0 >> 1);
     const uint8_t* const sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5) + (k0 >> 5);
     if (k0 + NL * 64 <= d1) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) c[i] = *reinterpret_cast<const u32x4*>(wp + i * 32);
+      for (int i = 0; i < kS; ++i) c[h][i] = *reinterpret_cast<const u32x4*>(wp + i * kG * 16);
 #pragma unroll
-      for (int i = 0; i < NL / 4; ++i) sc[i] = *reinterpret_cast<const u64_a1*>(sp + i * 8) >> (8 * lh);
+      for (int i = 0; i < kS / 4; ++i) sc[h][i] = *reinterpret_cast<const scales_a1*>(sp + i * 4 * kG);
     } else {  // zeros past the end of the reduction
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        if (i % 4 == 0) sc[i / 4] = 0x007f007f007f007full;
-        const int at = k0 + i * 64 + lh * 32;
-        c[i] = u32x4{0u, 0u, 0u, 0u};
+      for (int i = 0; i < kS; ++i) {
+        const int at = k0 + (i * kG + lg) * 32;
+        c[h][i] = u32x4{0u, 0u, 0u, 0u};
+        scales_t one = 127;
         if (at < d1) {
-          c[i] = *reinterpret_cast<const u32x4*>(wp + i * 32);
-          sc[i / 4] = (sc[i / 4] & ~(0xffffull << (16 * (i & 3)))) | ((uint64_t)sp[i * 2 + lh] << (16 * (i & 3)));
+          c[h][i] = *reinterpret_cast<const u32x4*>(wp + i * kG * 16);
+          one = sp[i * kG + lg];
         }
+        sc[h][i / 4][i & 3] = (scales_t)(one << (8 * lg));
       }
     }
   }
@@ -290,27 +297,40 @@ __global__ void __launch_bounds__(kMxT, 4) mx4_base_kernel(const MxBase g) {
     rg += row_split;
     const bool more = MORE && rg < g.row_groups;
     if (more) ask_x(rg * 32);
-    f32x16 acc;
+    typename std::conditional<k16, f32x4, f32x16>::type acc[kH];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    for (int h = 0; h < kH; ++h)
+#pragma unroll
+      for (int e = 0; e < (k16 ? 4 : 16); ++e) acc[h][e] = 0.f;
     if (n0 < g.d2 && k0 < d1) {
-      const int row = l32 < rows ? l32 : rows - 1;  // (rows past the end: results dropped)
-      const unsigned char* const xr = lds + row * kPitch + kw * NL * 128 + lh * 64;
+      const int row = ln < rows ? ln : rows - 1;  // (rows past the end: results dropped)
+      const unsigned char* const xr = lds + row * kPitch + kw * NL * 128 + lg * 64;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const float scale = mx4_scale((uint32_t)(sc[i / 4] >> (16 * (i & 3))) & 255u);
+      for (int i = 0; i < kS; ++i) {
+        float scale[kH];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mx4_bf16(c[i][e], scale)),
-                                                        *reinterpret_cast<const bf16x8*>(xr + i * 128 + e * 16), acc, 0, 0, 0);
+        for (int h = 0; h < kH; ++h) scale[h] = mx4_scale(((uint32_t)sc[h][i / 4][i & 3] >> (8 * lg)) & 255u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bf16x8 xv = *reinterpret_cast<const bf16x8*>(xr + i * kG * 64 + e * 16);
+#pragma unroll
+          for (int h = 0; h < kH; ++h) {
+            const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_bf16(c[h][i][e], scale[h]));
+            if constexpr (k16) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv, acc[h], 0, 0, 0);
+            else acc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv, acc[h], 0, 0, 0);
+          }
+        }
       }
     }
     // ---- the waves' sums ----
     barrier();
-    if (l32 < rows)
+    if (ln < rows)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(red + l32 * Ld + w * 32 + q * 8 + lh * 4) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+      for (int h = 0; h < kH; ++h)
+#pragma unroll
+        for (int q = 0; q < (k16 ? 1 : 4); ++q)
+          *reinterpret_cast<f32x4*>(red + ln * Ld + w * 32 + h * kSide + q * 8 + lg * 4) =
+              f32x4{acc[h][4 * q], acc[h][4 * q + 1], acc[h][4 * q + 2], acc[h][4 * q + 3]};
     barrier();
     float* const out = g.partial + ((size_t)(site * g.parts + part) * g.M + m0) * g.d2 + cg * kCols;
     for (int e = tid; e < rows * (kCols / 4); e += kMxT) {
@@ -487,7 +507,7 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
   *reinterpret_cast<u32x2_a8*>(g.Y[s0] + (size_t)m * g.ldy + n) = o;
 }
 
-template <int KW, int NL, bool MORE>
+template <int KW, int NL, bool MORE, int XM>
 int launch_base(const MxBase& b, hipStream_t st) {
   constexpr int kPart = KW * NL * 64, kRed = 32 * (kMxCols + 4) * 4;
   const int rows = b.M < 32 ? b.M : 32, x = rows * (kPart * 2 + 16), red = rows * (kMxCols + 4) * 4;
@@ -498,12 +518,12 @@ int launch_base(const MxBase& b, hipStream_t st) {
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
     const int most = 32 * (kPart * 2 + 16) > kRed ? 32 * (kPart * 2 + 16) : kRed;
-    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
+    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE, XM>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
     lds_set_for = dev;
   }
   const int64_t total = (int64_t)b.sites * b.col_groups * b.row_split * b.parts, grid = b.shrink_z + (total + 7) / 8 * 8;
   if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
-  hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
+  hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE, XM>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
   return check_launch();
 }
 
@@ -588,10 +608,11 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.row_groups = (g.M + 31) / 32;
   const int64_t units = (int64_t)sites * b.col_groups * b.parts;
   b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
-  const int rc = kw == 8   ? launch_base<8, kMxSteps, false>(b, st)
-                 : kw == 4 ? launch_base<4, kMxSteps, false>(b, st)
-                 : b.row_groups == 1 ? launch_base<2, kMxSteps, false>(b, st)
-                                     : launch_base<2, kMxSteps, true>(b, st);
+  const int rc = kw == 8 && g.M <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
+                 : kw == 8 ? launch_base<8, kMxSteps, false, 8>(b, st)
+                 : kw == 4 ? launch_base<4, kMxSteps, false, 8>(b, st)
+                 : b.row_groups == 1 ? launch_base<2, kMxSteps, false, 8>(b, st)
+                                     : launch_base<2, kMxSteps, true, 8>(b, st);
   if (rc) return rc;
   MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, lora};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
