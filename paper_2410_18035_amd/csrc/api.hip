@@ -390,7 +390,7 @@ bool mx4_rowmajor(int d1) { return d1 % 64 == 0; }  // the layout a weight is wr
 bool mx4_linear_direct(int64_t M, int d1, int d2, const LinearPlan& pl) {
   if (!mx4_prefill_supported(M, d1, d2)) return false;
   const int64_t other = pl.kind == MILORA_KERNEL_TILES && pl.slice == M ? pl.tiles.time : INT64_MAX / 2;
-  return plan_tiles(M, d1, d2, false, true).time <= other + write_out_time(d1, d2);
+  return plan_tiles(M, d1, d2, false, true, false, kCutMx4).time <= other + write_out_time(d1, d2);
 }
 
 int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const bf16_t* bias,
@@ -407,14 +407,16 @@ int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* ro
   if (mx4_linear_direct(M, d1, d2, pl)) {
     GatedTileArgs a{};
     const int parts = shrink_parts(M, d1);
-    float* const t = (float*)workspace;
+    float* const t = (float*)((char*)workspace + kStreamCtrlBytes);
     int2* const looked_up = (int2*)((char*)t + align_up((size_t)M * ad.r_max * parts * sizeof(float), 256));
     a.X = X; a.M = M; a.d = d1; a.F = d2; a.row_to_req = row_to_req; a.Wg = (const bf16_t*)W; a.mx4 = true;
     a.row_lora = looked_up; a.lora_site = (size_t)M; a.halves = halves_of(nullptr, M, ad.r_max);
     a.halves.at = (bf16_t*)((char*)looked_up + align_up((size_t)M * sizeof(int2), 256));
     a.ad = ad; a.tenant_id = tenant_id; a.route = route; a.B = B; a.t = t; a.t_stride = (size_t)M * ad.r_max; a.t_site = a.t_stride * parts; a.parts = parts;
     a.Y = Y;
-    int rc = launch_shrink_sites(X, d1, M, d1, row_to_req, ad, site, 1, tenant_id, route, B, t, looked_up, nullptr, st);
+    a.cnt = (int*)((char*)workspace + kTileCtrlOffset);
+    a.partial = (float*)((char*)a.halves.at + align_up(a.halves.site * sizeof(bf16_t), 256));
+    int rc = launch_shrink_sites(X, d1, M, d1, row_to_req, ad, site, 1, tenant_id, route, B, t, looked_up, a.cnt, st);
     if (!rc) rc = launch_halves(t, parts, M, ad.r_max, looked_up, 1, a.halves, st);
     return rc ? rc : linear_prefill_mx4(a, bias, site, st);
   }
@@ -460,7 +462,7 @@ extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int
   const size_t few = mx4_rows_workspace_bytes(M < kMxMostFew ? M : kMxMostFew, d1, d2, r_max, 1);
   if (M <= kMxAlwaysFew) return few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
-  const size_t direct = align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256) + align_up((size_t)M * sizeof(int2), 256) +
+  const size_t direct = kStreamCtrlBytes + cut_bytes_bound(M, d2) + align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256) + align_up((size_t)M * sizeof(int2), 256) +
                         align_up(halves_of(nullptr, M, r_max).site * sizeof(bf16_t), 256);
   const size_t most = many > direct ? many : direct;
   return most > few ? most : few;

@@ -72,6 +72,12 @@ int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* r
 }
 
 
+// (2 F is below 2^31: the entry points refuse larger ones)
+static size_t gated_partial_bytes(int64_t M, int d, int F) {
+  const size_t parts = partial_bytes_bound(M, d, 2 * F), cut = cut_bytes_bound(M, 2 * (int64_t)((F + 127) / 128) * 128);
+  return parts > cut ? parts : cut;
+}
+
 size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
   size_t most = 0;
   if (dtype == MILORA_BF16) {  // control words, shrinks of both sites, look-ups, partial tiles, 4-bit weights in bf16
@@ -79,7 +85,7 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
     c.take<char>(kStreamCtrlBytes);
     c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
     c.take<int2>((size_t)M * 2);
-    c.take<char>(partial_bytes_bound(M, d, 2 * F));
+    c.take<char>(gated_partial_bytes(M, d, F));
     c.take<bf16_t>(halves_of(nullptr, M, r_max).site * 2);
     if (mx4 && M > kMxAlwaysFew) c.take<bf16_t>((size_t)d * F * 2);
     most = c.off;
@@ -119,14 +125,14 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     a.cnt = (int*)(ctrl + kTileCtrlOffset);
     float* const t = c.take<float>(shrink_rows_bound(M, g.d) * g.ad.r_max * 2);
     int2* const looked_up = c.take<int2>((size_t)M * 2);
-    a.partial = c.take<float>(partial_bytes_bound(M, g.d, 2 * g.F) / sizeof(float));
+    a.partial = c.take<float>(gated_partial_bytes(M, g.d, g.F) / sizeof(float));
     a.halves = halves_of(nullptr, M, g.ad.r_max);
     a.halves.at = c.take<bf16_t>(a.halves.site * 2);
     // slices of rows where the smaller tiles are the only ones and the call has more than a launch of them takes
     int64_t slice = large || M <= kTileMaxRows ? M : kTileMaxRows;
-    TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large, true);
+    TilePlan first = plan_tiles(slice, g.d, 2 * g.F, small, large, true, kCut);
     if (g.mx4 && mx4_prefill_supported(M, g.d, g.F)) {  // the codes themselves by 256 x 256 tiles, unless smaller ones make up for writing them out
-      const TilePlan direct = plan_tiles(M, g.d, 2 * g.F, false, true, true);
+      const TilePlan direct = plan_tiles(M, g.d, 2 * g.F, false, true, true, kCutMx4);
       if (direct.time <= first.time + 2 * write_out_time(g.d, g.F)) {
         first = direct;
         slice = M;
@@ -148,7 +154,7 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     const bool big = first.shape == kTiles256;
     int2* const row_lora = large && !big ? nullptr : looked_up;
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, t, row_lora,
-                             !big && (row_lora || first.S > 1) ? a.cnt : nullptr, st);
+                             big || row_lora || first.S > 1 ? a.cnt : nullptr, st);
     if (!rc && big) rc = launch_halves(t, parts, M, g.ad.r_max, looked_up, 2, a.halves, st);
     for (int64_t m0 = 0; m0 < M && !rc; m0 += slice) {
       a.M = M - m0 < slice ? M - m0 : slice;
@@ -160,7 +166,7 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
       a.row_to_req = g.row_to_req ? g.row_to_req + m0 : nullptr;
       a.t = t + (size_t)m0 * g.ad.r_max;
       a.row_lora = row_lora ? row_lora + m0 : nullptr;
-      const TilePlan pl = a.M == slice ? first : plan_tiles(a.M, g.d, 2 * g.F, small, large, true);
+      const TilePlan pl = a.M == slice ? first : plan_tiles(a.M, g.d, 2 * g.F, small, large, true, kCut);
       rc = pl.shape == kTiles256 ? gated_prefill(a, st) : gated_tiles(a, pl, st);
     }
     return rc;
@@ -245,7 +251,9 @@ int launch_dz(const void* dY, const float* gate, const float* up, int64_t M, int
 // Tenant and rank of every row at the two sites, [site][M], and the least and the largest tenant among 64 rows, [site][M / 64].
 __global__ void __launch_bounds__(kThreads) gated_rows_kernel(int64_t M, const int32_t* __restrict__ row_to_req, AdapterView ad,
                                                               const int32_t* __restrict__ tenant_id, const uint8_t* __restrict__ route, int B,
-                                                              int2* __restrict__ row_lora, int2* __restrict__ among) {
+                                                              int2* __restrict__ row_lora, int2* __restrict__ among, int* __restrict__ clear) {
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < kShrinkClear; i += kThreads) clear[i] = 0;
   const int64_t m = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t req = m < M ? (row_to_req ? (int64_t)row_to_req[m] : m) : -1;
   for (int s = 0; s < 2; ++s) {
@@ -611,6 +619,7 @@ struct BackWs {
   void* W;         // 4-bit weights in bf16
   Halves low_halves, t_halves;  // of the bf16 matrix cores
   float* partial;
+  int* cnt;        // of cut tiles
   size_t bytes;
 };
 
@@ -629,6 +638,7 @@ BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int 
   w.low_halves.at = c.take<bf16_t>(tiles ? w.low_halves.site * 2 : 0);
   w.t_halves.at = c.take<bf16_t>(tiles ? w.t_halves.site * 2 : 0);
   w.partial = c.take<float>(tiles ? back_partial_floats(M, d, F) : 0);
+  w.cnt = c.take<int>(kShrinkClear);
   w.bytes = c.off;
   return w;
 }
@@ -642,7 +652,7 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   int rc = launch_dz<T>(dY, gate, up, M, g.F, w.dz, st);
   if (rc) return rc;
   hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
-                     g.route, g.B, w.row_lora, w.among);
+                     g.route, g.B, w.row_lora, w.among, w.cnt);
   if ((rc = check_launch())) return rc;
   hipLaunchKernelGGL(gated_low_kernel<T>, dim3((unsigned)M, 2), dim3(kThreads), 0, st, (const T*)w.dz, M, g.F, w.row_lora, g.ad, w.low);
   if ((rc = check_launch())) return rc;
@@ -684,7 +694,7 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   if (!rc) rc = launch_low_sites(dz, M, g.F, g.row_to_req, g.ad, g.tenant_id, g.route, g.B, w.low, st);
   if (rc) return rc;
   hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
-                     g.route, g.B, w.row_lora, w.among);
+                     g.route, g.B, w.row_lora, w.among, w.cnt);
   if ((rc = check_launch())) return rc;
   const int low_parts = shrink_parts(M, g.F);
   const size_t row_floats = (size_t)M * r_max;
@@ -696,7 +706,7 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
     a.Wu = g.mx4 ? (const bf16_t*)w.W + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
     a.row_lora = w.row_lora; a.lora_site = (size_t)M; a.halves = w.low_halves;
     a.low = w.low; a.low_stride = row_floats; a.low_site = row_floats * low_parts; a.parts = low_parts;
-    a.partial = w.partial; a.dX = (bf16_t*)dX;
+    a.partial = w.partial; a.cnt = w.cnt; a.dX = (bf16_t*)dX;
     if ((rc = gated_dx_tiles(a, st))) return rc;
   }
   if (!dA && !dB) return rc;

@@ -64,6 +64,9 @@ struct PParams {
   float* partial;     // kBack, S > 1: [part][M][d2] sums of the parts of the reduction
   size_t partial_stride;
   int S, steps;       // kBack: parts, and k steps of a part
+  int whole, cut, cut_steps;  // (not kPlain on bf16) tiles behind the first `whole` are cut in `cut` parts of so many k steps
+  float* cut_sums;            // [tile behind those][part][65536]
+  int* cut_cnt;               // [tile behind those][2], zero between launches
   const float* t;     // `parts` partial shrinks [part][rows of the whole call][r_max], to be added in part order
   size_t t_stride;    // floats from one part to the next
   int parts;
@@ -130,12 +133,26 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   // workgroup -> tile: workgroup ids go round-robin over the 8 XCDs; each XCD takes a contiguous run of the
   // tile order, which walks kGroupM row tiles per column tile so that the XCD's L2 serves the re-reads
   // (the 32 workgroups resident on an XCD then cover 4 row tiles x 8 column tiles)
-  const int total = p.tilesM * p.tilesN * (BACK ? p.S : 1);
+  const int tiles = p.tilesM * p.tilesN;
+  const int uncut = HALVES ? p.whole : tiles, total = BACK && p.S > 1 ? tiles * p.S : uncut;
   const int per = (total + 7) / 8;
-  int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if (id >= total) return;
-  const int part = BACK ? id / (p.tilesM * p.tilesN) : 0;
-  if (BACK) id %= p.tilesM * p.tilesN;
+  int id = (int)(blockIdx.x >> 3), part = 0, cut_tile = -1;
+  if (id < per) {
+    id += (int)(blockIdx.x & 7) * per;
+    if (id >= total) return;
+    if (BACK && p.S > 1) {
+      part = id / tiles;
+      id %= tiles;
+    }
+  } else {  // parts of the tiles that would fill the compute units for less than a turn; the same part of all of them first
+    if (!HALVES) return;
+    const int rest = tiles - uncut, units = rest * p.cut;
+    id += (int)(blockIdx.x & 7) * ((units + 7) / 8) - per;
+    if (id >= units) return;
+    part = id / rest;
+    cut_tile = id % rest;
+    id = uncut + cut_tile;
+  }
   const int gspan = kGroupM * p.tilesN;
   const int first = id / gspan * kGroupM;
   const int gsz = p.tilesM - first < kGroupM ? p.tilesM - first : kGroupM;
@@ -143,8 +160,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const int64_t m0 = (int64_t)(first + in_group % gsz) * kTM;
   const int n0 = in_group / gsz * (GATED ? kTN / 2 : kTN);
 
-  const int kt0 = BACK ? part * p.steps : 0;
-  const int KT = BACK ? (p.d1 / kTK - kt0 < p.steps ? p.d1 / kTK - kt0 : p.steps) : p.d1 / kTK;
+  const int kt_of = HALVES ? (cut_tile >= 0 ? p.cut_steps : BACK && p.S > 1 ? p.steps : p.d1 / kTK) : p.d1 / kTK;
+  const int kt0 = HALVES ? part * kt_of : 0;
+  const int KT = HALVES && p.d1 / kTK - kt0 < kt_of ? p.d1 / kTK - kt0 : kt_of;
+  const bool last_part = !HALVES || kt0 + KT == p.d1 / kTK;  // adds the LoRA terms
   const uint32_t lds0 = lds_addr(lds);
 
   // copies.  A k step of 64 is brought in two halves: half 0 = X rows 0..127 and W rows 0..127 of the tile,
@@ -200,7 +219,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   const unsigned char* const codes = (const unsigned char*)(GATED && wave >= 2 ? p.W2 : p.W);  // (MX) of this wave's copies
   auto issue_one = [&](int kt, int hh, int slot, int j) __attribute__((always_inline)) {
     if constexpr (MX) {
-      const int kk = kt < KT ? kt : KT - 1;
+      const int kk = kt0 + (kt < KT ? kt : KT - 1);
       if (j < 4) copy_to_lds16((const unsigned char*)p.X + (size_t)kk * (kTK * 2), voff[hh][j], lds0 + slot * kHalfBytes + (wave * 4 + j) * 1024);
       else copy_to_lds16(codes + (size_t)kk * 32, voff[hh][4], lds0 + slot * kHalfBytes + (kBlocksM / 2) * kBlockBytes + wave * 1024);
       return;
@@ -228,7 +247,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   int2 lora[kSites];  // (HALVES) of row tid, at the sites
 #pragma unroll
   for (int s = 0; s < kSites; ++s) lora[s] = int2{-1, 0};
-  if (HALVES && m0 + tid < p.M && (!BACK || part == p.S - 1))
+  if (HALVES && m0 + tid < p.M && last_part)
 #pragma unroll
     for (int s = 0; s < kSites; ++s) lora[s] = p.row_lora[s * p.lora_site + p.row_base + m0 + tid];
 
@@ -335,7 +354,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
   };
 
-  if constexpr (MX) issue_scales(0);
+  if constexpr (MX) issue_scales(kt0 >> 3);  // (a part begins with a multiple of eight steps)
   issue(0, 0, 0);
   issue(0, 1, 1);
   issue(1, 0, 2);
@@ -361,7 +380,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     wait_vm<2 * kCopies>();         // all but the two halves issued last have landed: both halves of this step
     __builtin_amdgcn_s_barrier();   // for every wave
     asm volatile("" ::: "memory");
-    if (MX && (kt & 7) == 0 && kt + 8 < KT) issue_scales((kt >> 3) + 1);
+    if (MX && (kt & 7) == 0 && kt + 8 < KT) issue_scales(((kt0 + kt) >> 3) + 1);
     auto mid = [&]() __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's operand reads have returned
       __builtin_amdgcn_s_barrier();        // and every other wave's
@@ -376,9 +395,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       }
     };
     if constexpr (MX) {
-      const int gr = kt >> 3, from = gr * 16 < scale_bytes - 16 ? gr * 16 : scale_bytes - 16;
+      const int gr = (kt0 + kt) >> 3, from = gr * 16 < scale_bytes - 16 ? gr * 16 : scale_bytes - 16;
       mma64_mx(wm ? h1 : h0, wn ? h1 : h0,
-               lds + (gr & 1) * kHalfBytes + kScaleAt + (wn * 128 + rrow) * 16 + kt * 2 + (lane >> 5) - from, mid, copy);
+               lds + (gr & 1) * kHalfBytes + kScaleAt + (wn * 128 + rrow) * 16 + (kt0 + kt) * 2 + (lane >> 5) - from, mid, copy);
     } else {
       mma64(std::integral_constant<bool, BACK>{}, wm ? h1 : h0, wn ? h1 : h0, mid, copy);
     }
@@ -647,6 +666,71 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
   }
 
+  // ---- a cut tile: the workgroup that is done last adds the others' sums to its own, in part order, and goes on; it waits only for workgroups
+  // that are already writing theirs ----
+  if constexpr (HALVES) {
+    if (cut_tile >= 0) {
+      int* const cnt = p.cut_cnt + 2 * cut_tile;
+      __syncthreads();
+      if (tid == 0) ctl[2] = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      typedef unsigned long long two_floats;  // (stores and loads of eight bytes past the caches of an XCD)
+      two_floats* const sums = (two_floats*)p.cut_sums + (size_t)cut_tile * p.cut * (kTM * kTN / 2) + tid;
+      if (ctl[2] != p.cut - 1) {
+        two_floats* const to = sums + (size_t)part * (kTM * kTN / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const f32x2 v = {acc[i][j][2 * e], acc[i][j][2 * e + 1]};
+              __hip_atomic_store(to + ((i * 4 + j) * 8 + e) * kThreadsP, __builtin_bit_cast(two_floats, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (tid == 0) __hip_atomic_fetch_add(cnt + 1, ctl[1] ? 0x10001 : 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return;
+      }
+      if (tid == 0) {
+        int done;
+        while (((done = __hip_atomic_load(cnt + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) & 0xffff) != p.cut - 1) __builtin_amdgcn_s_sleep(2);
+        if (done >> 16) ctl[1] = 1;
+        __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+        __hip_atomic_store(cnt + 1, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j0 = 0; j0 < 4; j0 += 2) {
+          f32x2 sum[16];
+          for (int k = 0; k < p.cut; ++k) {
+            f32x2 v[16];
+            if (k == part) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = f32x2{acc[i][j0 + (e >> 3)][2 * (e & 7)], acc[i][j0 + (e >> 3)][2 * (e & 7) + 1]};
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                v[e] = __builtin_bit_cast(f32x2, __hip_atomic_load(sums + ((size_t)k * 128 + (i * 4 + j0) * 8 + e) * kThreadsP, __ATOMIC_RELAXED,
+                                                                   __HIP_MEMORY_SCOPE_AGENT));
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) sum[e][h] = k ? sum[e][h] + v[e][h] : v[e][h];
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            acc[i][j0 + (e >> 3)][2 * (e & 7)] = sum[e][0];
+            acc[i][j0 + (e >> 3)][2 * (e & 7) + 1] = sum[e][1];
+          }
+        }
+    }
+  }
+
   // ---- bias, one rounding, store: of a 32 x 32 tile a lane holds row l % 32 and, in registers 4 g .. 4 g + 3, the
   // columns 8 g + 4 (l / 32) .. + 3.  By way of the wave's own LDS, so that a store writes whole lines (256 bytes of four rows instead
   // of 16 bytes of 32 rows, lines that had to be read before they could be written: seven linears of 32768 rows 11.43 -> 10.79 ms), and
@@ -909,9 +993,15 @@ static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t st
     p.row_base = row_base + r0;
     p.tilesM = (int)((p.M + kTM - 1) / kTM);
     p.tilesN = tilesN;
-    const int total = p.tilesM * p.tilesN * (MODE == kBack ? p.S : 1);
-    const int per = (total + 7) / 8;
-    hipLaunchKernelGGL((prefill_kernel<MODE, MX>), dim3(8 * per), dim3(kThreadsP), kLdsBytesP, stream, p);
+    const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
+    int64_t total = tiles * (MODE == kBack && p.S > 1 ? p.S : 1), units = 0;
+    if ((MODE != kPlain || MX) && total == tiles) {
+      const CutPlan cut = cut_plan(tiles, p.d1 / kTK, MX);
+      p.whole = (int)cut.whole; p.cut = cut.parts; p.cut_steps = cut.steps;
+      total = cut.whole;
+      units = (tiles - cut.whole) * cut.parts;
+    }
+    hipLaunchKernelGGL((prefill_kernel<MODE, MX>), dim3((unsigned)(8 * ((total + 7) / 8 + (units + 7) / 8))), dim3(kThreadsP), kLdsBytesP, stream, p);
     const int rc = check_launch();
     if (rc) return rc;
   }
@@ -936,6 +1026,7 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t stream) {
   p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
   p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
+  p.cut_sums = g.partial; p.cut_cnt = g.cnt;
   p.d1 = g.d; p.d2 = g.F; p.site = 4; p.B = g.B;
   return g.mx4 ? launch_prefill<kGated, true>(p, g.M, g.row_base, stream) : launch_prefill<kGated, false>(p, g.M, g.row_base, stream);
 }
@@ -947,6 +1038,7 @@ int linear_prefill_mx4(const GatedTileArgs& g, const bf16_t* bias, int site, hip
   p.t = g.t; p.t_stride = g.t_stride; p.t_site = g.t_site; p.parts = g.parts;
   p.row_to_req = g.row_to_req; p.tenant_id = g.tenant_id; p.route = g.route; p.ad = g.ad;
   p.row_lora = g.row_lora; p.lora_site = g.lora_site; p.halves = g.halves.at; p.half_site = g.halves.site; p.half_chunk = g.halves.chunk;
+  p.cut_sums = g.partial; p.cut_cnt = g.cnt;
   p.d1 = g.d; p.d2 = g.F; p.site = site; p.B = g.B;
   return launch_prefill<kPlain, true>(p, g.M, g.row_base, stream);
 }
@@ -963,7 +1055,7 @@ static int back_parts(int64_t M, int d, int F, int* steps) {
   const int KT = 2 * F / kTK;
   int64_t S = 256 / tiles;
   if (S > KT / 8) S = KT / 8;
-  if (S < 1) S = 1;
+  if (S <= kCutParts) S = 1;  // (a cut of all tiles does without the launch behind)
   *steps = (int)((KT + S - 1) / S);
   return (KT + *steps - 1) / *steps;
 }
@@ -972,7 +1064,8 @@ static int back_parts(int64_t M, int d, int F, int* steps) {
 // less for a larger call, so that a workspace for the largest serves all.
 size_t back_partial_floats(int64_t M, int d, int F) {
   const size_t by_grid = (size_t)256 * kTM * kTN, by_steps = (size_t)(F / 256 + 1) * (size_t)M * d;
-  return by_steps < by_grid ? by_steps : by_grid;
+  const size_t all = by_steps < by_grid ? by_steps : by_grid, cut = cut_bytes_bound(M, d) / sizeof(float);
+  return all > cut ? all : cut;
 }
 
 bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX) {
@@ -1009,6 +1102,7 @@ int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
   p.d1 = 2 * g.F; p.d2 = g.d; p.site = 4; p.B = g.B;
   p.S = back_parts(g.M, g.d, g.F, &p.steps);
   p.partial = p.S > 1 ? g.partial : nullptr;
+  p.cut_sums = g.partial; p.cut_cnt = g.cnt;
   p.partial_stride = (size_t)g.M * g.d;
   const int rc = launch_prefill<kBack, false>(p, g.M, 0, stream);
   if (rc || p.S == 1) return rc;

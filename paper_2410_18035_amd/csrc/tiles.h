@@ -19,6 +19,33 @@ inline int64_t write_out_time(int d1, int d2) { return 300 + (int64_t)d1 * d2 / 
 constexpr int kStreamRows = 32;      // rows up to which a packed linear takes the weight-streaming kernel (decode.hip)
 constexpr int kMaxSplitUnits = 512;  // tiles x parts of a launch that cuts its reduction
 constexpr int kMaxParts = 8;         // of one reduction
+// 256 x 256 tiles run one a compute unit, whole turns of 256.  Those of a last turn that is not full are cut along the reduction where that is
+// faster: `parts` workgroups a tile, of `steps` k steps of 64 (a multiple of eight for 4-bit weights, whose scales come for eight), whose sums meet in
+// memory (prefill.hip).  A turn's step takes 1.6 us, the exchange some 15 us.
+struct CutPlan {
+  int64_t whole;  // tiles that are not cut, in front of the others
+  int parts, steps;
+};
+constexpr int kCutParts = 4, kCutCost = 1500;  // (10 ns)
+inline CutPlan cut_plan(int64_t tiles, int KT, bool mx4) {
+  const CutPlan none{tiles, 1, KT};
+  const int rest = (int)(tiles % 256);
+  if (rest == 0 || rest > 128) return none;
+  int parts = 256 / rest < kCutParts ? 256 / rest : kCutParts;
+  if (parts > KT / 8) parts = KT / 8;
+  if (parts < 2) return none;
+  int steps = (KT + parts - 1) / parts;
+  if (mx4) steps = (steps + 7) / 8 * 8;
+  parts = (KT + steps - 1) / steps;
+  if (parts < 2 || (KT - steps) * 163 <= kCutCost) return none;
+  return CutPlan{tiles - rest, parts, steps};
+}
+// What the sums of cut tiles take, at most; never less for larger sizes.  (columns: gate and up together)
+inline size_t cut_bytes_bound(int64_t M, int64_t columns) {
+  const int64_t tiles = ((M + 255) / 256) * ((columns + 255) / 256);
+  return (size_t)(tiles < 256 / kCutParts ? tiles * kCutParts : 256) * 65536 * sizeof(float);
+}
+
 // The first bytes of a routed linear's workspace belong to control words: those of the stream kernels (decode.hip), then the
 // part counters of the tile kernel, zeroed by the shrink launch in front of it.  Both keep their data behind them, so calls of
 // any sizes and either layout can follow one another on one workspace, and the status word can be asked for after either.
@@ -28,7 +55,9 @@ constexpr int kTileCtrlOffset = kStreamCtrlBytes - kTileCtrlBytes;
 
 // `small`: the tiles of tiles.hip are a choice up to kTileMaxRows rows (tiles_supported); `large`: the 256 x 256 kernel is one
 // (row-major weights, 64 rows or more).  At least one of them.
-TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated = false);
+// kCut: the 256 x 256 kernel cuts its last tiles, kCutMx4: and reads 4-bit weights.
+enum TileCut { kNoCut, kCut, kCutMx4 };
+TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated = false, TileCut cut = kNoCut);
 // The most partial_bytes over the plans of all calls of up to these sizes; never less for a larger size.
 size_t partial_bytes_bound(int64_t M, int d1, int d2);
 bool tiles_supported(int64_t M, int d1, int d2, bool packed, const void* X, const void* W, const void* Y);
@@ -100,6 +129,7 @@ struct GatedBackArgs {
   size_t low_stride, low_site;
   int parts;
   float* partial;  // back_partial_floats(M, d, F)
+  int* cnt;        // kShrinkClear words, zero
   bf16_t* dX;
 };
 bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX);

@@ -736,7 +736,7 @@ int launch_tiles(const TParams& p, hipStream_t st) {
 // The gated block (gate and up columns: twice its width): what a turn costs more with two terms and the activation, 10 us with 128 x 128
 // tiles, 12 with 256 x 256 (4096 x 11008, requests of three sites, ranks 8 to 64, 128 x 128 / 256 x 256 tiles: 300 rows 142 / 126 us, 500
 // 177 / 132, 777 267 / 228, 2000 585 / 359).
-TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated) {
+TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gated, TileCut cut) {
   const int KT = (d1 + 63) / 64;
   TilePlan best{};
   int64_t best_t = INT64_MAX;
@@ -759,7 +759,14 @@ TilePlan plan_tiles(int64_t M, int d1, int d2, bool small, bool large, bool gate
       offer(kTiles64, 64, 26, gated ? 700 : 200, S, 400 + 70 * S);
       offer(kTiles128, 128, 58, gated ? 1400 : 400, S, 250 + 220 * S);
     }
-  if (large) offer(kTiles256, 256, 163, gated ? 1975 : 775, 1, 0);
+  if (large) {
+    offer(kTiles256, 256, 163, gated ? 1975 : 775, 1, 0);
+    const int64_t tm = (M + 255) / 256, tn = (d2 + 255) / 256;
+    if (const CutPlan c = cut_plan(tm * tn, KT, cut == kCutMx4); cut != kNoCut && c.parts > 1) {
+      const int64_t t = (c.whole / 256 * KT + c.steps) * 163 + (c.whole / 256 + 1) * (gated ? 1975 : 775) + kCutCost;
+      if (t < best_t) best = TilePlan{kTiles256, (int)tm, (int)tn, 1, KT, 0, t};
+    }
+  }
   return best;
 }
 

@@ -176,7 +176,8 @@ def _table(c, dA, dB):
 
 SHAPES = [  # M, d, F, rows
     (1, 64, 16, "own"), (2, 64, 48, "mixed"), (17, 128, 80, "mixed"), (45, 192, 272, "mixed"), (63, 1024, 528, "own"), (64, 64, 64, "mixed"),
-    (130, 192, 272, "sorted"), (300, 512, 1040, "mixed"), (300, 2048, 2064, "sorted"), (1100, 256, 1040, "mixed"), (513, 4096, 336, "sorted")]
+    (130, 192, 272, "sorted"), (300, 512, 1040, "mixed"), (300, 2048, 2064, "sorted"), (1100, 256, 1040, "mixed"), (513, 4096, 336, "sorted"),
+    (1100, 2304, 1040, "mixed"), (2100, 1536, 4112, "sorted")]
 
 
 @gpu
@@ -196,7 +197,7 @@ def test_forward_bf16(M, d, F, rows, ranks):
 @gpu
 @pytest.mark.parametrize("M,d,F,rows", [(1, 96, 16, "own"), (5, 1056, 48, "mixed"), (16, 64, 528, "own"), (33, 160, 80, "mixed"), (128, 512, 272, "own"),
                                         (129, 96, 48, "mixed"), (200, 192, 272, "mixed"), (700, 512, 1040, "sorted"), (600, 1056, 304, "mixed"),
-                                                        (1100, 512, 2064, "mixed"), (2049, 640, 2064, "sorted"), (1300, 1152, 2048, "mixed")])
+                                                        (1100, 512, 2064, "mixed"), (2049, 640, 2064, "sorted"), (1300, 1152, 2048, "mixed"), (1100, 2304, 1040, "mixed")])
 @pytest.mark.parametrize("ranks", [(8,), (5, 33, 256)])
 def test_forward_quantised(M, d, F, rows, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 6), 3, d, F, ranks, M + d, torch.bfloat16, rows, mx4=True)
@@ -229,7 +230,7 @@ def test_any_shape_forward_and_backward(M, d, F, rows, dtype, ranks):
 @gpu
 @pytest.mark.parametrize("M,d,F,rows,mx4", [(1, 64, 64, "own", False), (5, 128, 192, "mixed", False), (64, 64, 128, "own", False), (100, 256, 704, "mixed", False),
                                             (257, 192, 320, "sorted", False), (600, 512, 1088, "mixed", False), (700, 1040, 448, "sorted", False),
-                                            (1500, 320, 1024, "sorted", False), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
+                                            (1500, 320, 1024, "sorted", False), (4200, 4128, 704, "sorted", False), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
 @pytest.mark.parametrize("ranks", [(8,), (16, 32), (5, 33, 256)])
 def test_backward_bf16(M, d, F, rows, mx4, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 6), 3, d, F, ranks, M + d, torch.bfloat16, rows, mx4)
@@ -278,7 +279,7 @@ def test_rows_without_a_tenant_and_tenants_without_rows():
 
 
 @gpu
-@pytest.mark.parametrize("M,d,F,dtype", [(20, 128, 96, torch.bfloat16), (130, 128, 192, torch.bfloat16), (1100, 256, 1040, torch.bfloat16), (40, 30, 50, torch.float32),
+@pytest.mark.parametrize("M,d,F,dtype", [(20, 128, 96, torch.bfloat16), (130, 128, 192, torch.bfloat16), (1100, 256, 1040, torch.bfloat16), (600, 1280, 1040, torch.bfloat16), (40, 30, 50, torch.float32),
                                          (9, 30, 50, torch.float32)])
 def test_infinities_and_nans_stay_in_their_tenants_rows(M, d, F, dtype):
     c, x, W, dense = _layer(M, 6, 3, d, F, (8, 16), 40 + M, dtype, "mixed")
@@ -327,7 +328,8 @@ def test_backward_keeps_a_tenants_infinities_to_its_rows():
 
 @gpu
 @pytest.mark.parametrize("M,d,F,mx4,dtype", [(40, 128, 96, False, torch.bfloat16), (300, 256, 320, False, torch.bfloat16), (24, 128, 96, True, torch.bfloat16),
-                                             (300, 256, 320, True, torch.bfloat16), (30, 50, 70, False, torch.float32)])
+                                             (300, 256, 320, True, torch.bfloat16), (1100, 1536, 1088, False, torch.bfloat16), (1100, 2304, 1088, True, torch.bfloat16),
+                                             (30, 50, 70, False, torch.float32)])
 def test_captured_step_replays(M, d, F, mx4, dtype):
     """A training step captured once and replayed with other inputs gives the bits of eager calls, whatever the workspaces hold."""
     c, x, W, dense = _layer(M, 5, 2, d, F, (8, 16), 60 + M, dtype, "mixed", mx4)
