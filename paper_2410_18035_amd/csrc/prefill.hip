@@ -704,26 +704,26 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j0 = 0; j0 < 4; j0 += 2) {
-          f32x2 sum[16];
+        for (int j0 = 0; j0 < 4; j0 += 4) {
+          f32x2 sum[32];
           for (int k = 0; k < p.cut; ++k) {
-            f32x2 v[16];
+            f32x2 v[32];
             if (k == part) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) v[e] = f32x2{acc[i][j0 + (e >> 3)][2 * (e & 7)], acc[i][j0 + (e >> 3)][2 * (e & 7) + 1]};
+              for (int e = 0; e < 32; ++e) v[e] = f32x2{acc[i][j0 + (e >> 3)][2 * (e & 7)], acc[i][j0 + (e >> 3)][2 * (e & 7) + 1]};
             } else {
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
+              for (int e = 0; e < 32; ++e)
                 v[e] = __builtin_bit_cast(f32x2, __hip_atomic_load(sums + ((size_t)k * 128 + (i * 4 + j0) * 8 + e) * kThreadsP, __ATOMIC_RELAXED,
                                                                    __HIP_MEMORY_SCOPE_AGENT));
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
+            for (int e = 0; e < 32; ++e)
 #pragma unroll
               for (int h = 0; h < 2; ++h) sum[e][h] = k ? sum[e][h] + v[e][h] : v[e][h];
           }
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
+          for (int e = 0; e < 32; ++e) {
             acc[i][j0 + (e >> 3)][2 * (e & 7)] = sum[e][0];
             acc[i][j0 + (e >> 3)][2 * (e & 7) + 1] = sum[e][1];
           }
