@@ -134,6 +134,12 @@ constexpr int kMxW = 8;
 constexpr int kMxT = kMxW * 64;
 constexpr int kMxCols = kMxW * 32;
 
+// What a row has at a site: W^B and rank, or rank 0.
+struct MxTerm {
+  const bf16_t* B;
+  int r, unused;
+};
+
 struct MxBase {
   const bf16_t* X;
   int64_t ldx;
@@ -143,6 +149,7 @@ struct MxBase {
   float* partial;  // [site][part][M][d2]
   int shrink_parts, shrink_z;  // the shrink: parts of a row, workgroups in all (a multiple of 8)
   ShrinkArgs shrink;
+  MxTerm* terms;  // [site][M]
 };
 
 constexpr int kMxShrinkK = 1024;
@@ -156,7 +163,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   const int64_t req = sh.row_to_req ? (int64_t)sh.row_to_req[m] : m;
   int ten = -1;
   const int r = req >= 0 && req < sh.B ? routed_rank(sh.ad, sh.tenant_id, sh.route, (int)req, sh.B, site, &ten) : 0;
-  if (part == 0 && tid == 0) sh.row_lora[s * sh.lora_site + m] = int2{r ? ten : -1, r};
+  if (part == 0 && tid == 0) g.terms[s * sh.lora_site + m] = MxTerm{r ? (const bf16_t*)sh.ad.B[ten * MILORA_NUM_SITES + site] : nullptr, r, 0};
   if (r == 0) return;
   gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
   const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
@@ -357,7 +364,7 @@ struct MxFinish {
   const float* t;  // [site][t_parts][M][r_max]
   size_t t_part, t_site;
   int t_parts;
-  const int2* row_lora;  // [site][M]
+  const MxTerm* terms;  // [site][M]
 };
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x2_a8 __attribute__((ext_vector_type(2)));
@@ -373,9 +380,9 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m = blockIdx.y, s0 = GATED ? 0 : blockIdx.z;
   const int n = blockIdx.x * kFinCols + lane * 4;
   const bool in = n < g.d2;
-  int2 tr[kSites];
+  MxTerm tr[kSites];
 #pragma unroll
-  for (int s = 0; s < kSites; ++s) tr[s] = f.row_lora[(size_t)(s0 + s) * g.M + m];
+  for (int s = 0; s < kSites; ++s) tr[s] = f.terms[(size_t)(s0 + s) * g.M + m];
   // ---- this wave's parts ----
   f32x4 v[kSites];
 #pragma unroll
@@ -418,15 +425,15 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
     if (lane == 0) ss[w] = sum;
   }
   // ---- LoRA: t of the row, this wave's ranks of W^B ----
-  const bool lora = tr[0].y || tr[kSites - 1].y;
+  const bool lora = tr[0].r || tr[kSites - 1].r;
   if (lora) {
     gbf16* b[kSites];
 #pragma unroll
     for (int s = 0; s < kSites; ++s)
-      b[s] = tr[s].y ? in_global(g.ad.B[tr[s].x * MILORA_NUM_SITES + g.site[s0] + s]) + (in ? n : 0) : nullptr;
+      b[s] = in_global(tr[s].B) + (in ? n : 0);
 #pragma unroll
     for (int s = 0; s < kSites; ++s)
-      if (tid < tr[s].y) {
+      if (tid < tr[s].r) {
         const float* const tp = f.t + (s0 + s) * f.t_site + (size_t)m * g.ad.r_max + tid;
         float x = 0.f;
         for (int p = 0; p < f.t_parts; p += 4) {
@@ -446,12 +453,12 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         const int c = w + 4 * u;
-        if (tr[s].y) first[s][u] = *(__attribute__((address_space(1))) const u32x2_a2*)(b[s] + (size_t)(c < tr[s].y ? c : 0) * g.d2);
+        if (tr[s].r) first[s][u] = *(__attribute__((address_space(1))) const u32x2_a2*)(b[s] + (size_t)(c < tr[s].r ? c : 0) * g.d2);
       }
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < kSites; ++s) {
-      const int r = tr[s].y;
+      const int r = tr[s].r;
       auto add = [&](int c, u32x2_a2 x) __attribute__((always_inline)) {
         if (c >= r) return;
         const float t = ts[s][c];
@@ -582,7 +589,7 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
 }
 
 size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites) {
-  return align_up((size_t)M * mx4_shrink_parts(d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(int2), 256) +
+  return align_up((size_t)M * mx4_shrink_parts(d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(MxTerm), 256) +
          align_up(mx4_partial_floats(M, d1, d2, sites) * sizeof(float), 256);
 }
 
@@ -590,16 +597,17 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   if (g.M > 65535) return MILORA_ERANGE;
   const int r_max = g.ad.r_max, t_parts = mx4_shrink_parts(g.d1);
   float* const t = (float*)workspace;
-  int2* const lora = (int2*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
-  float* const partial = (float*)((char*)lora + align_up((size_t)g.M * sites * sizeof(int2), 256));
+  MxTerm* const terms = (MxTerm*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
+  float* const partial = (float*)((char*)terms + align_up((size_t)g.M * sites * sizeof(MxTerm), 256));
   MxBase b{};
   b.X = g.X; b.ldx = g.ldx; b.M = g.M; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
   b.sites = sites;
   b.parts = mx4_parts(g.M, g.d1);
   b.partial = partial;
-  b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, lora, nullptr,
+  b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, nullptr, nullptr,
                         sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
+  b.terms = terms;
   b.shrink_parts = t_parts;
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
   const int kw = mx4_waves(g.M);
@@ -614,7 +622,7 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
                  : b.row_groups == 1 ? launch_base<2, kMxSteps, false, 8>(b, st)
                                      : launch_base<2, kMxSteps, true, 8>(b, st);
   if (rc) return rc;
-  MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, lora};
+  MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, terms};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
   if (gated) hipLaunchKernelGGL(mx4_finish_kernel<true>, grid, dim3(kFinT), 0, st, f);
   else hipLaunchKernelGGL(mx4_finish_kernel<false>, grid, dim3(kFinT), 0, st, f);
