@@ -271,76 +271,182 @@ __global__ void __launch_bounds__(kThreads) gated_rows_kernel(int64_t M, const i
   }
 }
 
-// low[site][m][c] = sum_j dz[m][site F + j] B[c][j] for the routed rows: a workgroup for a row and site, a wave for a rank.
+// low[site][m][c] = sum_j dz[m][site F + j] B[c][j] for the routed rows.  A workgroup takes four rows and four ranks of a site, a wave a quarter of
+// the columns, so that eight loads feed sixteen products; rows of different tenants one tenant after the other.  Bound: the caches, which send W^B
+// once for four rows (500 rows x 2730 columns, ranks 8 and 20: 15 us; a rank a wave, row by row, 62).
+constexpr int kLowU = 4;  // columns of a lane on their way
 template <typename T>
 __global__ void __launch_bounds__(kThreads) gated_low_kernel(const T* __restrict__ dz, int64_t M, int F, const int2* __restrict__ row_lora, AdapterView ad,
                                                              float* __restrict__ low) {
-  const int64_t m = blockIdx.x;
-  const int s = blockIdx.y, lane = threadIdx.x & 63;
-  const int2 tr = row_lora[s * M + m];
-  if (tr.y == 0) return;
-  const T* const z = dz + m * 2 * F + (int64_t)s * F;
-  const T* const B = (const T*)ad.B[tr.x * MILORA_NUM_SITES + kGate + s];
-  for (int c = threadIdx.x >> 6; c < tr.y; c += kThreads / 64) {
-    float sum = 0.f;
-    for (int j = lane; j < F; j += 64) sum += Elem<T>::load(z, j) * Elem<T>::load(B, (size_t)c * F + j);
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_down(sum, off, 64);
-    if (lane == 0) low[((size_t)s * M + m) * ad.r_max + c] = sum;
+  __shared__ float red[kThreads / 64][16];
+  const int64_t m0 = (int64_t)blockIdx.x * 4;
+  const int s = blockIdx.y, c0 = blockIdx.z * 4, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int2 tr[4];
+  const T* z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t m = m0 + i < M ? m0 + i : M - 1;
+    tr[i] = m0 + i < M ? row_lora[s * M + m] : int2{-1, 0};
+    z[i] = dz + m * 2 * F + (int64_t)s * F;
+  }
+  const int per = (F + 3) / 4, j_end = (w + 1) * per < F ? (w + 1) * per : F;
+#pragma unroll
+  for (int first = 0; first < 4; ++first) {
+    bool seen = tr[first].y <= c0;  // no such ranks, or done with a row in front
+    for (int i = 0; i < first; ++i) seen |= tr[i].x == tr[first].x;
+    if (seen) continue;
+    const T* const B = (const T*)ad.B[tr[first].x * MILORA_NUM_SITES + kGate + s];
+    const int r = tr[first].y;
+    const T* b[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) b[c] = B + (size_t)(c0 + c < r ? c0 + c : r - 1) * F;
+    float sum[4][4] = {};
+    for (int j = w * per + lane; j < j_end; j += 64 * kLowU) {
+      float zv[kLowU][4], bv[kLowU][4];
+#pragma unroll
+      for (int u = 0; u < kLowU; ++u) {
+        const int at = j + u * 64 < j_end ? j + u * 64 : j;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          zv[u][i] = Elem<T>::load(z[i], at);
+          bv[u][i] = Elem<T>::load(b[i], at);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kLowU; ++u)
+        if (j + u * 64 < j_end)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[i][c] += zv[u][i] * bv[u][c];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        for (int off = 32; off > 0; off >>= 1) sum[i][c] += __shfl_xor(sum[i][c], off, 64);
+        if (lane == 0) red[w][i * 4 + c] = sum[i][c];
+      }
+    __syncthreads();
+    if (threadIdx.x < 16) {
+      const int i = threadIdx.x >> 2, c = c0 + (threadIdx.x & 3);
+      int ten = -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k == i) ten = tr[k].x;
+      if (ten == tr[first].x && c < r)
+        low[((size_t)s * M + m0 + i) * ad.r_max + c] = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
+    }
+    __syncthreads();
   }
 }
 
-// dX of any shape and type: 64 x 64 tiles, 32 of the reduction (2 F) at a time through LDS, fp32 matrix instructions; the LoRA part of a
-// row after them.
-constexpr int kNnK = 32;
+// dX of any shape and type: 64 x 64 tiles, 32 of the reduction (2 F, cut into `parts`) at a time through LDS, the next 32 on their way, fp32 matrix
+// instructions; the LoRA part of a row after them, or after the parts' sums have been added by the launch behind.  Bound: the matrix instructions
+// (500 rows of 1000 x 2730 in fp32: 90 us and 18 for the sums; the whole reduction by one workgroup, one step at a time, 842; 11 rows of 989 x 3026: 16 and 8 against 715).
+constexpr int kNnK = 32, kDxUnits = 1024, kDxParts = 32;  // workgroups of a cut launch, parts of a reduction, at most
+__host__ __device__ inline int dx_steps(int F) { return (F + kNnK - 1) / kNnK; }  // of one weight
+inline int dx_parts(int64_t M, int d, int F) {
+  const int64_t tiles = ((M + 63) / 64) * ((d + 63) / 64), steps = 2 * (int64_t)dx_steps(F);
+  int64_t parts = kDxUnits / tiles;
+  if (parts > kDxParts) parts = kDxParts;
+  if (parts > steps / 4) parts = steps / 4;
+  if (parts < 2) return 1;
+  const int64_t each = (steps + parts - 1) / parts;
+  return (int)((steps + each - 1) / each);
+}
+// never less for larger sizes
+inline size_t dx_partial_floats(int64_t M, int d) {
+  const size_t by_units = (size_t)kDxUnits * 64 * 64, by_parts = (size_t)kDxParts * M * d;
+  return by_units < by_parts ? by_units : by_parts;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) gated_dx_kernel(const T* __restrict__ dz, int64_t M, int d, int F, const T* __restrict__ Wg,
-                                                            const T* __restrict__ Wu, const int2* __restrict__ row_lora, AdapterView ad,
-                                                            const float* __restrict__ low, T* __restrict__ dX) {
-  __shared__ float zs[64][kNnK + 1], ws[kNnK][64 + 4];
+__device__ __forceinline__ float dx_lora(int64_t m, int n, int64_t M, const int2* __restrict__ row_lora, const AdapterView& ad, const float* __restrict__ low,
+                                         float v) {
+  for (int s = 0; s < 2; ++s) {
+    const int2 tr = row_lora[s * M + m];
+    if (tr.y == 0) continue;
+    const T* const A = (const T*)ad.A[tr.x * MILORA_NUM_SITES + kGate + s] + (size_t)n * tr.y;
+    const float* const lw = low + ((size_t)s * M + m) * ad.r_max;
+    float sum = 0.f;
+    for (int c = 0; c < tr.y; ++c) sum += lw[c] * Elem<T>::load(A, c);
+    v += sum;
+  }
+  return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 4) gated_dx_kernel(const T* __restrict__ dz, int64_t M, int d, int F, const T* __restrict__ Wg,
+                                                               const T* __restrict__ Wu, const int2* __restrict__ row_lora, AdapterView ad,
+                                                               const float* __restrict__ low, float* __restrict__ partial, T* __restrict__ dX) {
+  __shared__ float zs[2][64][kNnK + 1], ws[2][kNnK][64 + 4];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l32 = lane & 31, lh = lane >> 5;
   const int64_t m0 = (int64_t)blockIdx.y * 64;
   const int n0 = blockIdx.x * 64, wm = w & 1, wn = w >> 1;
+  const int half = dx_steps(F), each = (2 * half + (int)gridDim.z - 1) / (int)gridDim.z;
+  const int from = blockIdx.z * each, end = from + each < 2 * half ? from + each : 2 * half;
+  constexpr int kN = 64 * kNnK / kThreads;
+  float z[kN], wv[kN];
+  auto ask = [&](int step) __attribute__((always_inline)) {
+    const bool up = step >= half;
+    const int k0 = (up ? step - half : step) * kNnK;
+    const T* const W = up ? Wu : Wg;
+    const T* const zr = dz + (up ? F : 0);
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      const int e = tid + u * kThreads, row = e / kNnK, k = k0 + e % kNnK, col = n0 + e % 64, kw = k0 + e / 64;
+      z[u] = m0 + row < M && k < F ? Elem<T>::load(zr, (m0 + row) * 2 * F + k) : 0.f;
+      wv[u] = col < d && kw < F ? Elem<T>::load(W, (size_t)kw * d + col) : 0.f;
+    }
+  };
   f32x16 acc;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  for (int half = 0; half < 2; ++half) {
-    const T* const W = half ? Wu : Wg;
-    for (int k0 = 0; k0 < F; k0 += kNnK) {
-      __syncthreads();
-      for (int e = tid; e < 64 * kNnK; e += kThreads) {
-        const int row = e / kNnK, k = k0 + e % kNnK;
-        zs[row][e % kNnK] = m0 + row < M && k < F ? Elem<T>::load(dz, (m0 + row) * 2 * F + (int64_t)half * F + k) : 0.f;
-        const int col = n0 + e % 64, kw = k0 + e / 64;
-        ws[e / 64][e % 64] = col < d && kw < F ? Elem<T>::load(W, (size_t)kw * d + col) : 0.f;
-      }
-      __syncthreads();
+  ask(from);
+  for (int step = from, buf = 0; step < end; ++step, buf ^= 1) {
 #pragma unroll
-      for (int k = 0; k < kNnK; k += 2)
-        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(ws[k + lh][wn * 32 + l32], zs[wm * 32 + l32][k + lh], acc, 0, 0, 0);
+    for (int u = 0; u < kN; ++u) {
+      const int e = tid + u * kThreads;
+      zs[buf][e / kNnK][e % kNnK] = z[u];
+      ws[buf][e / 64][e % 64] = wv[u];
     }
+    __syncthreads();  // (the buffer written next was read before this)
+    if (step + 1 < end) ask(step + 1);
+#pragma unroll
+    for (int k = 0; k < kNnK; k += 2)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(ws[buf][k + lh][wn * 32 + l32], zs[buf][wm * 32 + l32][k + lh], acc, 0, 0, 0);
   }
   // (lane: row l % 32, registers 4 g .. + 3: columns 8 g + 4 (l / 32) ..)
   const int64_t m = m0 + wm * 32 + l32;
   if (m >= M) return;
-  for (int s = 0; s < 2; ++s) {
-    const int2 tr = row_lora[s * M + m];
-    if (tr.y == 0) continue;
-    const T* const A = (const T*)ad.A[tr.x * MILORA_NUM_SITES + kGate + s];
-    const float* const lw = low + ((size_t)s * M + m) * ad.r_max;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int n = n0 + wn * 32 + (e >> 2) * 8 + lh * 4 + (e & 3);
-      if (n >= d) continue;
-      float v = 0.f;
-      for (int c = 0; c < tr.y; ++c) v += lw[c] * Elem<T>::load(A, (size_t)n * tr.y + c);
-      acc[e] += v;
-    }
-  }
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     const int n = n0 + wn * 32 + (e >> 2) * 8 + lh * 4 + (e & 3);
-    if (n < d) Elem<T>::store(dX, (size_t)m * d + n, acc[e]);
+    if (n >= d) continue;
+    if (gridDim.z > 1) partial[(blockIdx.z * (size_t)M + m) * d + n] = acc[e];
+    else Elem<T>::store(dX, (size_t)m * d + n, dx_lora<T>(m, n, M, row_lora, ad, low, acc[e]));
   }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) gated_dx_sum_kernel(const float* __restrict__ partial, int parts, int64_t M, int d, const int2* __restrict__ row_lora,
+                                                                AdapterView ad, const float* __restrict__ low, T* __restrict__ dX) {
+  const int64_t m = blockIdx.y;
+  const int n = blockIdx.x * kThreads + threadIdx.x;
+  if (n >= d) return;
+  const float* const q = partial + (size_t)m * d + n;
+  const size_t stride = (size_t)M * d;
+  float v = 0.f;
+  for (int p = 0; p < parts; p += 4) {
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = q[(p + u < parts ? p + u : p) * stride];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (p + u < parts) v += x[u];
+  }
+  Elem<T>::store(dX, (size_t)m * d + n, dx_lora<T>(m, n, M, row_lora, ad, low, v));
 }
 
 // Gradients of the tenants' matrices: out[col][c] = sum over the tenant's rows m of P[m][col] s[m][c], with (P, s) = (X, low) for dA and
@@ -637,7 +743,8 @@ BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int 
   w.low_halves = w.t_halves = halves_of(nullptr, M, r_max);
   w.low_halves.at = c.take<bf16_t>(tiles ? w.low_halves.site * 2 : 0);
   w.t_halves.at = c.take<bf16_t>(tiles ? w.t_halves.site * 2 : 0);
-  w.partial = c.take<float>(tiles ? back_partial_floats(M, d, F) : 0);
+  const size_t any = dx_partial_floats(M, d), by_tiles = tiles ? back_partial_floats(M, d, F) : 0;
+  w.partial = c.take<float>(any > by_tiles ? any : by_tiles);
   w.cnt = c.take<int>(kShrinkClear);
   w.bytes = c.off;
   return w;
@@ -654,7 +761,7 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
                      g.route, g.B, w.row_lora, w.among, w.cnt);
   if ((rc = check_launch())) return rc;
-  hipLaunchKernelGGL(gated_low_kernel<T>, dim3((unsigned)M, 2), dim3(kThreads), 0, st, (const T*)w.dz, M, g.F, w.row_lora, g.ad, w.low);
+  hipLaunchKernelGGL(gated_low_kernel<T>, dim3((unsigned)((M + 3) / 4), 2, (unsigned)((g.ad.r_max + 3) / 4)), dim3(kThreads), 0, st, (const T*)w.dz, M, g.F, w.row_lora, g.ad, w.low);
   if ((rc = check_launch())) return rc;
   const T *Wg = (const T*)g.Wg, *Wu = (const T*)g.Wu;
   if (g.mx4) {
@@ -662,9 +769,15 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
     Wu = Wg + (size_t)g.d * g.F;
   }
   if (dX) {
-    hipLaunchKernelGGL(gated_dx_kernel<T>, dim3((unsigned)((g.d + 63) / 64), (unsigned)((M + 63) / 64)), dim3(kThreads), 0, st, (const T*)w.dz, M, g.d,
-                       g.F, Wg, Wu, w.row_lora, g.ad, w.low, (T*)dX);
+    const int parts = dx_parts(M, g.d, g.F);  // (up to kDxUnits tiles where there are several: rows fit a grid's y)
+    hipLaunchKernelGGL(gated_dx_kernel<T>, dim3((unsigned)((g.d + 63) / 64), (unsigned)((M + 63) / 64), (unsigned)parts), dim3(kThreads), 0, st,
+                       (const T*)w.dz, M, g.d, g.F, Wg, Wu, w.row_lora, g.ad, w.low, w.partial, (T*)dX);
     if ((rc = check_launch())) return rc;
+    if (parts > 1) {
+      hipLaunchKernelGGL(gated_dx_sum_kernel<T>, dim3((unsigned)((g.d + kThreads - 1) / kThreads), (unsigned)M), dim3(kThreads), 0, st, w.partial, parts, M,
+                         g.d, w.row_lora, g.ad, w.low, (T*)dX);
+      if ((rc = check_launch())) return rc;
+    }
   }
   if (dA || dB) {
     GradArgs a{};
