@@ -797,7 +797,7 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   return rc;
 }
 
-// bf16 of whole 64 of F and 32 of d, 16-byte aligned: everything on the bf16 matrix cores.
+// bf16 of whole 32 of F and d, 16-byte aligned: everything on the bf16 matrix cores.
 int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB, const BackWs& w,
                    hipStream_t st) {
   const int64_t M = g.M;

@@ -208,9 +208,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         }
       }
   }
-  // (BACK: the second half of the reduction is the second weight's)
-  const int half_steps = p.d1 / kTK / 2, back_by = BACK && is_w ? half_steps : 0;
-  const unsigned char* const src2 = BACK && is_w ? (const unsigned char*)p.W2 : src;
+  // (BACK: the second half of the reduction is the second weight's; of a step's 64 rows wave 2 brings the first 32, wave 3 the others, and the
+  // halves meet at a multiple of 32)
+  const int second_at = BACK && is_w ? p.d1 / 2 - (wave & 1) * 32 : 0x7fffffff;
+  const unsigned char* const src2 = BACK && is_w ? (const unsigned char*)p.W2 - (size_t)(p.d1 / 2) * p.d2 * 2 : src;
   const size_t k_bytes = BACK && is_w ? (size_t)kTK * p.d2 * 2 : kTK * 2;
   const uint32_t dst_in_half = (uint32_t)((is_w ? 8 : 0) + (wave & 1) * 4) * kBlockBytes;
   // half H = 2 * (k step) + hh lives in ring slot H % kHalves
@@ -225,8 +226,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       return;
     }
     const int kk = kt0 + (kt < KT ? kt : KT - 1);  // past the end: re-read the last step into a slot nobody reads
-    const bool second = BACK && kk >= half_steps;
-    const unsigned char* b = (second ? src2 : src) + (size_t)(second ? kk - back_by : kk) * (BACK ? k_bytes : kTK * 2);
+    const unsigned char* b = (BACK && kk * kTK >= second_at ? src2 : src) + (size_t)kk * (BACK ? k_bytes : kTK * 2);
     const uint32_t dst = lds0 + slot * kHalfBytes + dst_in_half;
     copy_to_lds16(b, voff[hh][j], dst + j * 1024);
   };
@@ -1069,7 +1069,7 @@ size_t back_partial_floats(int64_t M, int d, int F) {
 }
 
 bool back_supported(int64_t M, int d, int F, const void* dz, const void* Wg, const void* Wu, const void* dX) {
-  if (F % kTK != 0 || d % 16 != 0 || M < 1 || M > kHalvesRows) return false;
+  if (F % (kTK / 2) != 0 || d % 16 != 0 || M < 1 || M > kHalvesRows) return false;
   if ((((uintptr_t)dz | (uintptr_t)Wg | (uintptr_t)Wu) & 15) != 0 || ((uintptr_t)dX & 7) != 0) return false;
   return (uint64_t)d * kTK * 2u < (1ull << 31) && (uint64_t)F * 4u * kTM < (1ull << 32) && (int64_t)((d + kTN - 1) / kTN) <= 1 << 16;
 }

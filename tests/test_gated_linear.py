@@ -212,7 +212,8 @@ def test_forward_quantised(M, d, F, rows, ranks):
 @pytest.mark.parametrize("M,d,F,rows,dtype", [
     (1, 1, 1, "own", torch.float32), (3, 3, 5, "mixed", torch.float32), (16, 100, 77, "own", torch.float32), (17, 33, 65, "mixed", torch.float32),
     (300, 250, 683, "mixed", torch.float32), (200, 1000, 130, "sorted", torch.float32), (7, 50, 31, "mixed", torch.bfloat16),
-    (100, 70, 90, "mixed", torch.bfloat16), (90, 64, 24, "mixed", torch.bfloat16)])
+    (100, 70, 90, "mixed", torch.bfloat16), (90, 64, 24, "mixed", torch.bfloat16), (11, 200, 1010, "mixed", torch.float32),
+    (70, 66, 700, "sorted", torch.float32), (2100, 1030, 100, "sorted", torch.float32), (130, 90, 650, "mixed", torch.bfloat16)])
 @pytest.mark.parametrize("ranks", [(4,), (3, 17, 40)])
 def test_any_shape_forward_and_backward(M, d, F, rows, dtype, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 5), 3, d, F, ranks, 3 * M + d, dtype, rows)
@@ -230,7 +231,8 @@ def test_any_shape_forward_and_backward(M, d, F, rows, dtype, ranks):
 @gpu
 @pytest.mark.parametrize("M,d,F,rows,mx4", [(1, 64, 64, "own", False), (5, 128, 192, "mixed", False), (64, 64, 128, "own", False), (100, 256, 704, "mixed", False),
                                             (257, 192, 320, "sorted", False), (600, 512, 1088, "mixed", False), (700, 1040, 448, "sorted", False),
-                                            (1500, 320, 1024, "sorted", False), (4200, 4128, 704, "sorted", False), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
+                                            (1500, 320, 1024, "sorted", False), (4200, 4128, 704, "sorted", False), (65, 96, 32, "mixed", False), (300, 288, 800, "mixed", True),
+                                            (1100, 1056, 1504, "sorted", False), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
 @pytest.mark.parametrize("ranks", [(8,), (16, 32), (5, 33, 256)])
 def test_backward_bf16(M, d, F, rows, mx4, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 6), 3, d, F, ranks, M + d, torch.bfloat16, rows, mx4)
