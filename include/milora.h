@@ -175,7 +175,7 @@ int milora_route(const void *H, int64_t M_tok, int d, int dtype, const int32_t *
  *               bf16 is part of it; what it holds before a call does not matter); the sizes never go down when an
  *               argument goes up, so one workspace sized for the largest call serves every smaller one
  * A row whose request index, tenant id or tenant rank is out of range gets the base term only.
- * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK), EUNSUPPORTED (packed or 4-bit layout with fp32, with
+ * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK; 4-bit layout with d1 >= 2^30), EUNSUPPORTED (packed or 4-bit layout with fp32, with
  * d1 % 32 != 0 or d2 % 16 != 0, or with X, W, bias or Y not 16-byte aligned), EWORKSPACE, EHIP.
  */
 size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max);
@@ -211,9 +211,9 @@ int milora_routed_linear(const void *X, int64_t M, int d1, int d2, int dtype,
  *   W_gate, W_up  device, math shape d x F in `w_layout`: MILORA_W_ROWMAJOR, or MILORA_W_MX4 (dtype bf16)
  *   Y          device [M][F], `dtype`; must not overlap any input
  *   gate_out, up_out  device [M][F] float or NULL: g and u, for milora_gated_linear_backward
- *   workspace  device, milora_gated_linear_workspace_bytes() bytes (the size never goes down when M, d, F or r_max go up by steps
- *              that keep the kind of call); what it holds before a call does not matter
- * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK, F >= 2^30, sizes beyond a launch), EUNSUPPORTED (MILORA_W_PACKED; 4-bit weights with fp32,
+ *   workspace  device, milora_gated_linear_workspace_bytes() bytes (never fewer when M, d, F or r_max goes up); what it
+ *              holds before a call does not matter
+ * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK, d or F >= 2^30, sizes beyond a launch), EUNSUPPORTED (MILORA_W_PACKED; 4-bit weights with fp32,
  * with d % 32 != 0 or F % 16 != 0, or with X, Y or a weight not 16-byte aligned), EWORKSPACE, EHIP.
  */
 size_t milora_gated_linear_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max);
@@ -235,8 +235,8 @@ typedef struct {
  *   dg = dY u s (1 + g (1 - s)),  du = dY g s
  *   dX = dg W_gate^T + du W_up^T + sum over both sites of [routed] (dz (W^B)^T) (W^A)^T,  dz = dg at site 4, du at site 5
  *   dW^A = sum over the tenant's routed rows of x^T (dz (W^B)^T),  dW^B = sum of (x W^A)^T dz
- * dg and du are rounded to `dtype` for the matrix products (bf16: half of what separates the results from exact ones, the other half
- * is their own rounding); sums are fp32, in an order that depends on the sizes and rows alone.
+ * dg and du are rounded to `dtype` for the matrix products (in bf16 that and the rounding of the results are what separates them from exact
+ * ones, about as much each); sums are fp32, in an order that depends on the sizes and rows alone.
  *
  *   dY         device [M][F], `dtype`;  X: as in the forward call
  *   gate, up   device [M][F] float: gate_out and up_out of the forward call
@@ -244,7 +244,8 @@ typedef struct {
  *   dX         device [M][d], `dtype`, or NULL: not wanted
  *   gradients  host struct or NULL: the wanted gradients of sites 4 and 5 are overwritten (zero for a tenant without rows); those of
  *              other sites and of a tenant whose rank is out of range are left as they are.  No two entries may overlap.
- *   workspace  device, milora_gated_linear_backward_workspace_bytes() bytes; what it holds before a call does not matter
+ *   workspace  device, milora_gated_linear_backward_workspace_bytes() bytes (never fewer when M, d, F or r_max goes up); what it holds before a
+ *              call does not matter
  * Errors: those of milora_gated_linear (X, dY and dX may have any alignment of their type); ERANGE also for more than 32767 tenants and more
  * than 4194240 rows.
  */

@@ -173,11 +173,12 @@ def _dev(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.4 us; the Stream object of the public call 2.7 us
 
 
-def _stream() -> int:
-    """The current stream of the current device."""
-    if _raw_stream is None:
-        return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+def _stream(on: Optional[torch.Tensor] = None) -> int:
+    """The current stream of the current device, which has to be the device of `on`."""
+    device = torch.cuda.current_device()
+    if on is not None and on.get_device() != device:
+        raise ValueError("tensors must be on the current device: call under torch.cuda.device(...)")
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -318,7 +319,7 @@ def milora_routed_linear(X: torch.Tensor, W: torch.Tensor, adapters: AdapterTabl
     rc = lib().milora_routed_linear(_dev(X), M, d1, d2, _dtype_code(X), _dev(row_to_req, torch.int32), _dev(W),
                                     w_layout, _dev(bias, X.dtype), ctypes.byref(ad), site,
                                     _dev(tenant_id, torch.int32), _dev(route, torch.uint8), B, _dev(out),
-                                    _dev(workspace), workspace.numel(), _stream())
+                                    _dev(workspace), workspace.numel(), _stream(X if w_layout == W_MX4 else None))
     if rc != 0:
         raise MiloraError(rc, "milora_routed_linear")
     return out
@@ -371,7 +372,7 @@ def milora_gated_linear(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tenso
     ad = adapters.c_struct()
     rc = lib().milora_gated_linear(_dev(X), M, d, F, _dtype_code(X), _dev(row_to_req, torch.int32), _dev(W_gate), _dev(W_up), w_layout,
                                    ctypes.byref(ad), _dev(tenant_id, torch.int32), _dev(route, torch.uint8), B, _dev(out, X.dtype),
-                                   _dev(gate_out, torch.float32), _dev(up_out, torch.float32), _dev(workspace), workspace.numel(), _stream())
+                                   _dev(gate_out, torch.float32), _dev(up_out, torch.float32), _dev(workspace), workspace.numel(), _stream(X))
     if rc != 0:
         raise MiloraError(rc, "milora_gated_linear")
     return out
@@ -397,6 +398,8 @@ class GradientTable:
             raise ValueError("no gradient wanted: pass grads=None")
         if any(g.dtype != every[0].dtype for g in every):
             raise TypeError("gradients must share a dtype")
+        if len({g.data_ptr() for g in every if g.numel()}) != sum(g.numel() > 0 for g in every):
+            raise ValueError("two gradients in one place")
         ptrs = lambda rows: torch.tensor([_dev(g) or 0 for row in rows for g in row], dtype=torch.int64, device=every[0].device)
         return GradientTable(ptrs(dA), ptrs(dB), len(dA), every[0].dtype, (dA, dB))
 
@@ -429,7 +432,7 @@ def milora_gated_linear_backward(dY: torch.Tensor, X: torch.Tensor, gate: torch.
     rc = lib().milora_gated_linear_backward(
         _dev(dY, X.dtype), _dev(X), _dev(gate, torch.float32), _dev(up, torch.float32), M, d, F, _dtype_code(X), _dev(row_to_req, torch.int32),
         _dev(W_gate), _dev(W_up), w_layout, ctypes.byref(ad), _dev(tenant_id, torch.int32), _dev(route, torch.uint8), B, _dev(dX, X.dtype),
-        ctypes.byref(gr) if gr is not None else None, _dev(workspace), workspace.numel(), _stream())
+        ctypes.byref(gr) if gr is not None else None, _dev(workspace), workspace.numel(), _stream(X))
     if rc != 0:
         raise MiloraError(rc, "milora_gated_linear_backward")
     return dX
@@ -470,7 +473,7 @@ def milora_layer_decode(x: torch.Tensor, weights: Sequence[torch.Tensor], adapte
     ad = adapters.c_struct()
     args = (_dev(x), B, d, F, _dtype_code(x), ctypes.byref(lw), ctypes.byref(ad), _dev(tenant_id, torch.int32),
             _dev(route, torch.uint8), LAYER_RMSNORM if rmsnorm else 0, _dev(attn_out, x.dtype), _dev(y),
-            _dev(qkv_out), _dev(workspace), workspace.numel(), _stream())
+            _dev(qkv_out), _dev(workspace), workspace.numel(), _stream(x if w_layout == W_MX4 else None))
     if profile_reps > 0:
         slots = (ctypes.c_float * PROFILE_SLOTS)()
         rc = lib().milora_layer_decode_profile(*args, profile_reps, slots)
@@ -552,7 +555,7 @@ def milora_quantize_weight(W: torch.Tensor, out: Optional[torch.Tensor] = None) 
         out = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
     elif out.dtype != torch.uint8 or out.numel() != nbytes:
         raise ValueError("out holds quantized_weight_bytes(d1, d2) bytes")
-    rc = lib().milora_quantize_weight(_dev(W), _dtype_code(W), _dev(out), d1, d2, _stream())
+    rc = lib().milora_quantize_weight(_dev(W), _dtype_code(W), _dev(out), d1, d2, _stream(W))
     if rc != 0:
         raise MiloraError(rc, "milora_quantize_weight")
     return out
@@ -566,7 +569,7 @@ def milora_dequantize_weight(Wq: torch.Tensor, d1: int, d2: int, dtype: torch.dt
         out = torch.empty(d2, d1, dtype=dtype, device=Wq.device)
     elif out.shape != (d2, d1):
         raise ValueError("out must be [d2, d1]")
-    rc = lib().milora_dequantize_weight(_dev(Wq), _dev(out), _dtype_code(out), d1, d2, _stream())
+    rc = lib().milora_dequantize_weight(_dev(Wq), _dev(out), _dtype_code(out), d1, d2, _stream(Wq))
     if rc != 0:
         raise MiloraError(rc, "milora_dequantize_weight")
     return out

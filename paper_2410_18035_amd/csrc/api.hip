@@ -458,7 +458,7 @@ extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2
 }
 
 extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
-  if (M < 1 || d1 < 1 || d2 < 1 || r_max < 1) return 0;
+  if (M < 1 || d1 < 1 || d2 < 1 || d1 > 0x3fffffff || r_max < 1) return 0;
   const size_t few = mx4_rows_workspace_bytes(M < kMxMostFew ? M : kMxMostFew, d1, d2, r_max, 1);
   if (M <= kMxAlwaysFew) return few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
@@ -506,6 +506,7 @@ extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, in
   if (rc) return rc;
   if (M > 0x7fffffffLL) return MILORA_ERANGE;
   const bool mx4 = w_layout == MILORA_W_MX4;
+  if (mx4 && d1 > 0x3fffffff) return MILORA_ERANGE;
   if (!workspace || workspace_bytes < (mx4 ? milora_quantized_linear_workspace_bytes(M, d1, d2, adapters->r_max)
                                            : milora_routed_linear_workspace_bytes(M, d1, d2, adapters->r_max)))
     return MILORA_EWORKSPACE;
@@ -532,14 +533,14 @@ static int check_gated(int64_t M, int d, int F, int dtype, const int32_t* row_to
   if (!row_to_req && M != B) return MILORA_EINVAL;
   const int rc = check_adapters(adapters);
   if (rc) return rc;
-  if (M > 0x7fffffffLL || F > 0x3fffffff) return MILORA_ERANGE;
+  if (M > 0x7fffffffLL || F > 0x3fffffff || d > 0x3fffffff) return MILORA_ERANGE;
   if (w_layout == MILORA_W_PACKED) return MILORA_EUNSUPPORTED;
   if (w_layout == MILORA_W_MX4 && (dtype != MILORA_BF16 || !packed_shape_ok(d, F) || !aligned16(Wg) || !aligned16(Wu))) return MILORA_EUNSUPPORTED;
   return MILORA_OK;
 }
 
 extern "C" size_t milora_gated_linear_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max) {
-  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
+  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || d > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
   return gated_workspace_bytes(M, d, F, dtype, w_layout == MILORA_W_MX4, r_max);
 }
 
@@ -557,7 +558,7 @@ extern "C" int milora_gated_linear(const void* X, int64_t M, int d, int F, int d
 }
 
 extern "C" size_t milora_gated_linear_backward_workspace_bytes(int64_t M, int d, int F, int dtype, int w_layout, int r_max) {
-  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
+  if (M < 1 || d < 1 || F < 1 || F > 0x3fffffff || d > 0x3fffffff || r_max < 1 || !valid_dtype(dtype) || !valid_layout(w_layout)) return 0;
   return gated_backward_workspace_bytes(M, d, F, dtype, w_layout == MILORA_W_MX4, r_max);
 }
 
@@ -618,6 +619,7 @@ static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, cons
       if (!aligned16(weights->W[m])) return MILORA_EUNSUPPORTED;
     if (weights->layout == MILORA_W_MX4) {
       if (marks) return MILORA_EUNSUPPORTED;
+      if (d > 0x3fffffff || F > 0x3fffffff) return MILORA_ERANGE;
       return layer_decode_mx4((const bf16_t*)x, B, d, F, weights, ad, tenant_id, route, flags, (const bf16_t*)attn_out, (bf16_t*)y,
                               (bf16_t*)qkv_out, workspace, st);
     }

@@ -39,6 +39,7 @@ def test_refusals():
         both(-1, **kw)
     both(-2, a=far)
     both(-2, F=1 << 30)
+    both(-2, d=1 << 30)
     for kw in (dict(lay=1), dict(lay=2, dt=1), dict(lay=2, d=48), dict(lay=2, F=40), dict(lay=2, Wg=off), dict(lay=2, Wu=off)):
         both(-3, **kw)
     both(-5, ws=n)
@@ -393,6 +394,26 @@ def test_unaligned_bf16_tensors(M):
     dA, dB = _room(c, d, F)
     dX = mb.milora_gated_linear_backward(dY, x, gate, up, *W, c.tab, tid, route, row_to_req=c.rows(), grads=_table(c, dA, dB))
     _assert_backward(c, x, dense, dY, dX, dA, dB)
+
+
+@gpu
+def test_refuses_another_device_and_gradients_in_one_place(monkeypatch):
+    c, x, W, _ = _layer(20, 4, 2, 64, 96, (8,), 90, torch.bfloat16, "mixed", True)
+    tid, route = c.requests()
+    kw = dict(row_to_req=c.rows(), w_layout=mb.W_MX4, F=96)
+    gate, up = (torch.empty(20, 96, device=DEV) for _ in range(2))
+    dA, dB = _room(c, 64, 96)
+    dA[1][0] = dA[0][0]
+    with pytest.raises(ValueError):
+        _table(c, dA, dB)
+    wide, dy, dx = c.rnd(64, 64), c.rnd(20, 96), torch.empty_like(x)
+    q = mb.milora_quantize_weight(wide)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: mb.milora_gated_linear(x, *W, c.tab, tid, route, **kw),
+                 lambda: mb.milora_gated_linear_backward(dy, x, gate, up, *W, c.tab, tid, route, dX=dx, **kw),
+                 lambda: mb.milora_quantize_weight(wide, out=q), lambda: mb.milora_dequantize_weight(q, 64, 64)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
 
 
 @gpu

@@ -48,6 +48,7 @@ def test_sizes_and_refusals():
     assert lin(4, 32, 16, 1, p, p, p, big) == -3  # fp32 activations
     assert lin(4, 48, 16, 0, p, p, p, big) == -3 and lin(4, 32, 24, 0, p, p, p, big) == -3
     assert lin(4, 32, 16, 0, off, p, p, big) == -3 and lin(4, 32, 16, 0, p, off, p, big) == -3
+    assert lin(4, 1 << 30, 16, 0, p, p, p, big) == -2
     assert lin(4, 32, 16, 0, p, p, n, 0) == -5 and lin(4, 32, 16, 0, p, p, p, 16) == -5
     assert L.milora_routed_linear(p, 4, 32, 16, 0, p, p, 3, n, ctypes.byref(ad), 0, p, p, 1, p, p, big, n) == -1  # no such layout
     lw = mb._LayerWeights()
@@ -58,6 +59,7 @@ def test_sizes_and_refusals():
     assert dec(48, 64, 0, p) == -3 and dec(64, 48, 0, p) == -3 and dec(64, 64, 1, p) == -3 and dec(64, 64, 0, off) == -3
     assert L.milora_layer_decode_noalloc(p, 4, 64, 64, 0, ctypes.byref(lw), ctypes.byref(ad), p, p, 0, n, p, n, n) == -3
     slots = (ctypes.c_float * mb.PROFILE_SLOTS)()
+    assert mb.quantized_linear_workspace_bytes(4, 1 << 30, 16, 8) == 0
     lw.layout = 3
     assert dec(64, 64, 0, p) == -1
     del slots
