@@ -1870,7 +1870,7 @@ __global__ void __launch_bounds__(kThreads) decode_wide_kernel(const Params p) {
       } else {
         spin_until([&]() { return ld_lds(&c.shr_ready) >= L + 1; });
       }
-      expand_items(L, sg);
+      if (!dead) expand_items(L, sg);  // (after a wait that ran out just above, the level's list may not be there: on the first level it is whatever the LDS held)
       TS(3);
     }
     // ===================================== all waves: sum, LoRA term, glue, store =====================================
