@@ -5,7 +5,10 @@
 //   dA = sum over the tenant's rows of x^T low,  dB = sum of (x A)^T dz
 //
 // Forward: bf16 takes the matrix-core tiles with gate and up columns side by side (tiles.hip, prefill.hip), 4-bit weights of few rows
-// mx4.hip, everything else the any-shape kernels of linear_generic.hip.
+// mx4.hip, of more the same tiles, on the codes or on the weights written out in bf16, whichever is reckoned shorter; everything else the
+// any-shape kernels of linear_generic.hip.  Backward: the 256 x 256 tiles of prefill.hip for dX (4-bit weights written out first: the product
+// runs along their columns, and a byte holds two inputs of one) and the bf16 matrix cores below for dA and dB; everything else the any-shape
+// kernels below, fp32 matrix instructions.
 #include "gated.h"
 #include "mx4.h"
 #include "tiles.h"
@@ -70,7 +73,6 @@ int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* r
   hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, v, (size_t)M * r_max, parts, M, r_max, row_lora, out);
   return check_launch();
 }
-
 
 // (2 F is below 2^31: the entry points refuse larger ones)
 static size_t gated_partial_bytes(int64_t M, int d, int F) {
@@ -728,7 +730,6 @@ struct BackWs {
   int* cnt;        // of cut tiles
   size_t bytes;
 };
-
 
 BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int r_max) {
   Carver c{(char*)base};

@@ -55,7 +55,7 @@ struct PParams {
   float* gate_out;    // kGated: [M][d2] each, or null
   float* up_out;
   size_t t_site;      // kGated, kBack: floats to the shrinks of the next site
-  // kGated, kBack: [site][M of the call] tenant and rank of each row, and the shrinks as two bf16 halves: [site][chunk of 32 ranks][1 + M] lines
+  // kGated, kBack, 4-bit weights: [site][M of the call] tenant and rank of each row, and the shrinks as two bf16 halves: [site][chunk of 32 ranks][1 + M] lines
   // of 64 values, 32 high halves and 32 low ones; the first line is zero
   const int2* row_lora;
   size_t lora_site;
@@ -101,7 +101,7 @@ __device__ __forceinline__ void wait_vm() {
 // projections, X = [dg | du].  A k step's W side is 64 rows of 256 columns, copied as they lie, 256 bytes of a row to a half; the transposing
 // LDS read (ds_read_b64_tr_b16: four rows x sixteen columns by sixteen lanes) makes operands of them.  A row's sixteen-column pieces are permuted
 // so that the four rows of two pieces that half a wave reads at once lie on all banks.  The LoRA steps take t = dz W^B^T against the rows of
-// W^A, which are contiguous along the ranks.  Few tiles: the reduction in S parts, their fp32 sums added in part order by a launch behind this one.
+// W^A, which are contiguous along the ranks.  Very few tiles: the reduction in S > 4 parts, their fp32 sums added in part order by a launch behind this one.
 __device__ __forceinline__ int swz_tr(int k) { return ((k & 3) << 1) | ((k >> 3) & 1); }  // of a row's eight pieces
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bf16x8 read_tr(uint32_t at) {  // rows k .. k + 3 and, 1024 bytes on, k + 4 .. k + 7
@@ -112,6 +112,9 @@ __device__ __forceinline__ bf16x8 read_tr(uint32_t at) {  // rows k .. k + 3 and
   return __builtin_bit_cast(bf16x8, v);
 }
 
+// Cut tiles (cut_plan; not kPlain on bf16): the tiles of a last turn that would not fill the compute units are dealt to up to four workgroups each.
+// What it gains, us of a call with / without (a turn of 4096 inputs 105 us): gated block of 4096 x 11008, 777 rows, 1.3 turns, 217 / 246; 600 rows,
+// 1.0, 193 / 324; 4096 rows, 5.4, 702 / 723; 5120 x 13824, 8192 rows, 13.5 turns, 2071 / 2070; 4-bit linear of 5120 x 13824, 1777 rows, 1.5, 237 / 264.
 //
 // MX: W (and W2) are 4-bit weights; a half's W side is 128 columns x 32 bytes of codes, four copies, and a wave brings four copies of X and one of
 // W.  A lane reads the 32 codes of one group of one column at once, so sub-step ks holds the inputs 32 (l / 32) + 8 ks .. + 7 on both sides, and
