@@ -397,6 +397,48 @@ def test_unaligned_bf16_tensors(M):
 
 
 @gpu
+def test_two_streams_at_once():
+    """Training steps and 4-bit linears on two streams at the same time, workspaces apart, give the bits of one after the other."""
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    steps = []
+    for k, (M, d, F, mx4) in enumerate([(1100, 2304, 1088, False), (1100, 1536, 1088, True)]):
+        c, x, W, _ = _layer(M, 5, 2, d, F, (8, 16), 95 + k, torch.bfloat16, "mixed", mx4)
+        tid, route, r2r = *c.requests(), c.rows()
+        lay = mb.W_MX4 if mx4 else mb.W_ROWMAJOR
+        dY, gate, up, Y, dX = c.rnd(M, F), *(torch.empty(M, F, device=DEV) for _ in range(2)), torch.empty(M, F, dtype=c.dtype, device=DEV), torch.empty_like(x)
+        dA, dB = _room(c, d, F)
+        q = mb.milora_quantize_weight(c.rnd(F, d, s=d ** -0.5))
+        Z = torch.empty_like(Y)
+        size = mb.gated_linear_workspace_bytes, mb.gated_linear_backward_workspace_bytes
+        ws = [torch.empty(f(M, d, F, c.dtype, lay, c.tab.r_max), dtype=torch.uint8, device=DEV) for f in size]
+        ws.append(torch.empty(mb.quantized_linear_workspace_bytes(M, d, F, c.tab.r_max), dtype=torch.uint8, device=DEV))
+        kw = dict(row_to_req=r2r, w_layout=lay, F=F)
+
+        def step(x=x, W=W, c=c, tid=tid, route=route, r2r=r2r, kw=kw, Y=Y, gate=gate, up=up, dY=dY, dX=dX, ws=ws, q=q, Z=Z, F=F, table=_table(c, dA, dB)):
+            mb.milora_gated_linear(x, *W, c.tab, tid, route, out=Y, gate_out=gate, up_out=up, workspace=ws[0], **kw)
+            mb.milora_gated_linear_backward(dY, x, gate, up, *W, c.tab, tid, route, dX=dX, grads=table, workspace=ws[1], **kw)
+            mb.milora_routed_linear(x, q, c.tab, 4, tid, route, row_to_req=r2r, w_layout=mb.W_MX4, d2=F, out=Z, workspace=ws[2])
+
+        steps.append((step, [Y, gate, up, dX, Z, *dA[0], *dA[1], *dB[0], *dB[1]]))
+    alone = []
+    for step, outs in steps:
+        step()
+        alone.append([o.clone() for o in outs])
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for _, outs in steps:
+            for o in outs:
+                o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for side, (step, _) in zip(sides, steps):
+            with torch.cuda.stream(side):
+                step()
+                step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for (_, outs), want in zip(steps, alone) for a, b in zip(outs, want))
+
+
+@gpu
 def test_refuses_another_device_and_gradients_in_one_place(monkeypatch):
     c, x, W, _ = _layer(20, 4, 2, 64, 96, (8,), 90, torch.bfloat16, "mixed", True)
     tid, route = c.requests()
