@@ -49,11 +49,20 @@ struct Carver {
 // The scales of the ranks (X W^A, dz W^B^T: fp32, [site][part][M][r_max]) as two bf16 halves, about 17 of their bits: zero past the rank and for
 // rows without a term.  A row's 32 ranks by 32 lanes.
 constexpr int kHalvesRowsWg = kThreads / 32;
-__global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __restrict__ v, size_t part, int parts, int64_t M, int r_max,
-                                                                const int2* __restrict__ row_lora, Halves out) {
+struct HalvesOf {
+  const float* v;
+  int parts;
+  Halves out;
+};
+__global__ void __launch_bounds__(kThreads) gated_halves_kernel(HalvesOf first, HalvesOf second, size_t part, int64_t M, int r_max,
+                                                                const int2* __restrict__ row_lora, int sites) {
   const int64_t i = (int64_t)blockIdx.x * kHalvesRowsWg + (threadIdx.x >> 5);  // line
   if (i > M) return;
-  const int chunk = blockIdx.y, s = blockIdx.z, c = chunk * 32 + (threadIdx.x & 31);
+  const bool other = (int)blockIdx.z >= sites;
+  const float* const v = other ? second.v : first.v;
+  const int parts = other ? second.parts : first.parts;
+  const Halves out = other ? second.out : first.out;
+  const int chunk = blockIdx.y, s = (int)blockIdx.z - (other ? sites : 0), c = chunk * 32 + (threadIdx.x & 31);
   float x = 0.f;
   if (i > 0 && c < row_lora[s * M + i - 1].y) {
     const float* const q = v + (size_t)s * part * parts + (size_t)(i - 1) * r_max + c;
@@ -68,10 +77,14 @@ __global__ void __launch_bounds__(kThreads) gated_halves_kernel(const float* __r
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 }  // namespace
 
-int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st) {
-  const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), (unsigned)sites);
-  hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, v, (size_t)M * r_max, parts, M, r_max, row_lora, out);
+static int launch_halves_of(const HalvesOf& first, const HalvesOf* second, int64_t M, int r_max, const int2* row_lora, int sites, hipStream_t st) {
+  const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), (unsigned)(second ? 2 * sites : sites));
+  hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, first, second ? *second : first, (size_t)M * r_max, M, r_max, row_lora, sites);
   return check_launch();
+}
+
+int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st) {
+  return launch_halves_of(HalvesOf{v, parts, out}, nullptr, M, r_max, row_lora, sites, st);
 }
 
 // (2 F is below 2^31: the entry points refuse larger ones)
@@ -559,11 +572,12 @@ __global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) 
 }
 
 // ---- the same on the bf16 matrix cores -------------------------------------------------------------------------------------
-// out[col][c] = sum over the tenant's rows of P[m][col] s[m][c]: a workgroup of eight waves takes 64 columns and 32 ranks of one of a
-// tenant's matrices, a wave every eighth 64 rows of the call.  A wave lists the tenant's rows among its own and takes 32 of them at a time: their 128 bytes
+// out[col][c] = sum over the tenant's rows of P[m][col] s[m][c]: a workgroup of kGradW waves takes 64 columns and 32 ranks of one of a
+// tenant's matrices, a wave every kGradW-th 64 rows of the call: two waves up to kGradFewRows, so that all workgroups are resident (a training step
+// of 4096 x 11008 with 16 / 534 / 1111 rows: 155 / 394 / 567 us, with eight 168 / 407 / 579), eight beyond (5120 x 13824, 8192 rows: 4422 us, with
+// two 4448).  A wave lists the tenant's rows among its own and takes 32 of them at a time: their 128 bytes
 // of P and of s go through registers (the next 32 rows' are on their way while these are multiplied) into the wave's LDS, and the
 // transposing read makes operands of both.  The waves' sums meet in LDS at the end.  Bound: the reads of P (HBM) and s (L2).
-constexpr int kGradW = 8;
 struct GradTileArgs {
   const bf16_t *X, *dz;
   int64_t M;
@@ -577,6 +591,8 @@ struct GradTileArgs {
 // 16-column pieces (32 bytes) of a 128-byte row k: permuted so that four rows of two pieces, which half a wave reads at once, hit all banks
 __device__ __forceinline__ int grad_swz(int k) { return ((k >> 1) & 1) * 2; }
 
+constexpr int64_t kGradFewRows = 2048;
+template <int kGradW>
 __global__ void __launch_bounds__(kGradW * 64, 4) gated_grad_tile_kernel(const GradTileArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[kGradW * 8192];
   __shared__ int lists[kGradW][128];
@@ -812,7 +828,12 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   if ((rc = check_launch())) return rc;
   const int low_parts = shrink_parts(M, g.F);
   const size_t row_floats = (size_t)M * r_max;
-  if ((rc = launch_halves(w.low, low_parts, M, r_max, w.row_lora, 2, w.low_halves, st))) return rc;
+  const HalvesOf low{w.low, low_parts, w.low_halves}, t{w.t, shrink_parts(M, g.d), w.t_halves};
+  if (dB) {
+    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
+    if (rc) return rc;
+  }
+  if ((rc = launch_halves_of(low, dB ? &t : nullptr, M, r_max, w.row_lora, 2, st))) return rc;
   if (dX) {
     GatedBackArgs a{};
     a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
@@ -824,18 +845,15 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
     if ((rc = gated_dx_tiles(a, st))) return rc;
   }
   if (!dA && !dB) return rc;
-  if (dB) {
-    rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
-    if (!rc) rc = launch_halves(w.t, shrink_parts(M, g.d), M, r_max, w.row_lora, 2, w.t_halves, st);
-    if (rc) return rc;
-  }
   const int chunks = (r_max + 31) / 32;
   GradTileArgs a{};
   a.X = (const bf16_t*)g.X; a.dz = dz; a.M = M; a.d = g.d; a.F = g.F;
   a.tiles_a = dA ? (g.d + 63) / 64 : 0;
   a.tiles_b = dB ? (g.F + 63) / 64 : 0;
   a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = w.low_halves; a.t = w.t_halves; a.dA = dA; a.dB = dB;
-  hipLaunchKernelGGL(gated_grad_tile_kernel, dim3((unsigned)((a.tiles_a + a.tiles_b) * chunks), (unsigned)(2 * tenants)), dim3(kGradW * 64), 0, st, a);
+  const dim3 grid((unsigned)((a.tiles_a + a.tiles_b) * chunks), (unsigned)(2 * tenants));
+  if (M <= kGradFewRows) hipLaunchKernelGGL(gated_grad_tile_kernel<2>, grid, dim3(2 * 64), 0, st, a);
+  else hipLaunchKernelGGL(gated_grad_tile_kernel<8>, grid, dim3(8 * 64), 0, st, a);
   return check_launch();
 }
 
