@@ -814,6 +814,9 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   return rc;
 }
 
+// (4-bit weights) Does the product behind both projections read the codes?  Scales of 128 inputs are copied four bytes at a time.
+bool direct_back(const GatedCall& g) { return g.d % 128 == 0; }
+
 // bf16 of whole 32 of F and d, 16-byte aligned: everything on the bf16 matrix cores.
 int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB, const BackWs& w,
                    hipStream_t st) {
@@ -837,8 +840,9 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   if (dX) {
     GatedBackArgs a{};
     a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
-    a.Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
-    a.Wu = g.mx4 ? (const bf16_t*)w.W + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
+    a.mx4 = g.mx4 && direct_back(g);
+    a.Wg = g.mx4 && !a.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
+    a.Wu = g.mx4 && !a.mx4 ? (const bf16_t*)w.W + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
     a.row_lora = w.row_lora; a.lora_site = (size_t)M; a.halves = w.low_halves;
     a.low = w.low; a.low_stride = row_floats; a.low_site = row_floats * low_parts; a.parts = low_parts;
     a.partial = w.partial; a.cnt = w.cnt; a.dX = (bf16_t*)dX;
@@ -866,15 +870,16 @@ size_t gated_backward_workspace_bytes(int64_t M, int d, int F, int dtype, bool m
 int run_gated_backward(const GatedCall& g, const void* dY, const float* gate, const float* up, void* dX, void* const* dA, void* const* dB,
                        void* workspace, hipStream_t st) {
   const BackWs w = carve_back(workspace, g.M, g.d, g.F, g.dtype, g.mx4, g.ad.r_max);
-  if (g.mx4 && dX) {
+  const bf16_t* const Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
+  const bf16_t* const Wu = g.mx4 ? Wg + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
+  const bool tiles = g.dtype == MILORA_BF16 && g.d % 32 == 0 && aligned16(g.X) && g.M <= (int64_t)65535 * 64 && g.ad.n_tenants <= 32767 &&
+                     back_supported(g.M, g.d, g.F, w.dz, Wg, Wu, dX);
+  if (g.mx4 && dX && !(tiles && direct_back(g))) {
     int rc = mx4_dequantize(g.Wg, w.W, MILORA_BF16, g.d, g.F, false, st);
     if (!rc) rc = mx4_dequantize(g.Wu, (bf16_t*)w.W + (size_t)g.d * g.F, MILORA_BF16, g.d, g.F, false, st);
     if (rc) return rc;
   }
-  const bf16_t* const Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
-  const bf16_t* const Wu = g.mx4 ? Wg + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
-  if (g.dtype == MILORA_BF16 && g.d % 32 == 0 && aligned16(g.X) && g.M <= (int64_t)65535 * 64 && g.ad.n_tenants <= 32767 &&
-      back_supported(g.M, g.d, g.F, w.dz, Wg, Wu, dX))
+  if (tiles)
     return backward_tiles(g, dY, gate, up, dX, dA, dB, w, st);
   return g.dtype == MILORA_BF16 ? backward_any<bf16_t>(g, dY, gate, up, dX, dA, dB, w, st) : backward_any<float>(g, dY, gate, up, dX, dA, dB, w, st);
 }

@@ -89,6 +89,14 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
+// copy_to_lds16 with four bytes a lane
+__device__ __forceinline__ void copy_to_lds4(const void* base, uint32_t voff, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(dst), "v"(voff), "s"(base)
+               : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
@@ -120,6 +128,8 @@ __device__ __forceinline__ bf16x8 read_tr(uint32_t at) {  // rows k .. k + 3 and
 // W.  A lane reads the 32 codes of one group of one column at once, so sub-step ks holds the inputs 32 (l / 32) + 8 ks .. + 7 on both sides, and
 // turns eight of them into an operand by four conversions between the matrix instructions of the sub-step before.  The scales come sixteen bytes
 // of a column at a time, for eight steps, into the ends of ring slots 0 and 1.  (A weight written out in bf16 first costs 20 us per 45 M values.)
+// kBack: the codes of a step's 64 rows come as they lie, and each thread turns 64 of them into rows of bf16 in LDS, between the matrix instructions
+// of the step before.
 constexpr int kScaleAt = 24 * 1024, kScaleBytes = kTN * 16;
 template <int MODE, bool MX>
 __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
@@ -127,7 +137,6 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   constexpr bool HALVES = MODE != kPlain || MX;  // LoRA terms from prepared halves
   constexpr int kSites = MODE == kPlain ? 1 : 2;
   constexpr int kCopies = MX ? 5 : 8;  // of a half by a wave
-  static_assert(!(BACK && MX), "the backward pass multiplies rows of W");
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -189,9 +198,15 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         r = r < p.M ? r : p.M - 1;
         voff[hh][j] = (uint32_t)((uint64_t)r * (uint32_t)p.d1 * 2u + (uint32_t)((lane & 7) ^ swz((i & 1) * 8 + rr)) * 16u);
       }
-      int n = GATED ? n0 + hh * 64 + (wave & 1) * 32 + (lane >> 1) : n0 + hh * 128 + wave * 32 + (lane >> 1);
-      n = n < p.d2 ? n : p.d2 - 1;
-      voff[hh][4] = (uint32_t)n * (uint32_t)(p.d1 >> 1) + (uint32_t)(lane & 1) * 16u;
+      if constexpr (BACK) {  // 32 inputs of one of the step's 64 rows
+        int n = n0 + hh * 128 + (tid & 3) * 32;
+        n = n < p.d2 ? n : p.d2 - 32;
+        voff[hh][4] = (uint32_t)(tid >> 2) * (uint32_t)(p.d2 >> 1) + (uint32_t)(n >> 1);
+      } else {
+        int n = GATED ? n0 + hh * 64 + (wave & 1) * 32 + (lane >> 1) : n0 + hh * 128 + wave * 32 + (lane >> 1);
+        n = n < p.d2 ? n : p.d2 - 1;
+        voff[hh][4] = (uint32_t)n * (uint32_t)(p.d1 >> 1) + (uint32_t)(lane & 1) * 16u;
+      }
     }
   } else {
 #pragma unroll
@@ -245,6 +260,37 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   auto issue = [&](int kt, int hh, int slot) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kCopies; ++j) issue_one(kt, hh, slot, j);
+  };
+
+  // (MX && BACK) the codes of a step as they lie, and their scales: a thread brings, and later turns into operands, 32 inputs of one row in
+  // each half; the scales of a wave's 16 rows, four bytes a half, by its first 32 lanes.  A wave's rows lie in one weight (F % 32 == 0).
+  constexpr int kRawAt = 4 * kHalfBytes, kRawScaleAt = kRawAt + 16 * 1024;
+  const uint32_t sv = (uint32_t)(wave * 16 + ((lane >> 1) & 15)) * (uint32_t)(p.d2 >> 5) + (uint32_t)(n0 >> 5) + (n0 + (lane & 1) * 128 < p.d2 ? (lane & 1) * 4u : 0u);
+  auto issue_raw = [&](int kt, int j) __attribute__((always_inline)) {
+    const int kk = kt0 + (kt < KT ? kt : KT - 1), F = p.d1 >> 1;
+    const bool second = kk * kTK + wave * 16 >= F;
+    const unsigned char* const w = (const unsigned char*)(second ? p.W2 : p.W);
+    const int64_t row = (int64_t)kk * kTK - (second ? F : 0);
+    if (j < 2) copy_to_lds16(w + row * (p.d2 >> 1), voff[j][kCopies - 1], lds0 + kRawAt + (kt & 1) * 8192 + j * 4096 + wave * 1024);
+    else copy_to_lds4(w + (size_t)F * p.d2 / 2 + row * (p.d2 >> 5), sv, lds0 + kRawScaleAt + (kt & 1) * 1024 + wave * 256);
+  };
+  u32x4 raw[2];
+  float raw_scale[2];
+  auto read_raw = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh) {
+      raw[hh] = *(const u32x4*)(lds + kRawAt + (kt & 1) * 8192 + hh * 4096 + tid * 16);
+      raw_scale[hh] = mx4_scale(lds[kRawScaleAt + (kt & 1) * 1024 + wave * 256 + ((lane >> 2) * 2 + hh) * 4 + (lane & 3)]);
+    }
+  };
+  // eight inputs (of group i = 4 half + u) of row tid / 4 to where a copied row has them; odd rows the other sixteen bytes of a piece first, so that
+  // the rows that a cycle writes lie on all banks
+  auto put_raw = [&](int kt, int i) __attribute__((always_inline)) {
+    const int k = tid >> 2, odd = k & 1, hh = i >> 2, v = (i >> 1) & 1, e = i & 1;
+    const uint32_t c = odd ? raw[hh][2 * v + 1 - e] : raw[hh][2 * v + e];
+    const int piece = (lane & 3) * 2 + v;
+    *(u32x4*)(lds + (2 * (kt & 1) + hh) * kHalfBytes + (kBlocksM / 2) * kBlockBytes + k * 256 + ((piece ^ swz_tr(k)) & 7) * 32 + (e ^ odd) * 16) =
+        mx4_bf16(c, raw_scale[hh]);
   };
 
   int2 lora[kSites];  // (HALVES) of row tid, at the sites
@@ -357,11 +403,26 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
   };
 
+  if constexpr (BACK && MX) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int j = 0; j < 3; ++j) issue_raw(kt, j);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) issue_one(kt, j >> 2, 2 * kt + (j >> 2), j & 3);
+    }
+    wait_vm<19>();  // codes and scales of the first step
+    asm volatile("" ::: "memory");
+    read_raw(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) put_raw(0, i);
+  } else {
   if constexpr (MX) issue_scales(kt0 >> 3);  // (a part begins with a multiple of eight steps)
   issue(0, 0, 0);
   issue(0, 1, 1);
   issue(1, 0, 2);
   issue(1, 1, 3);
+  }
   // 12 of the 16 accumulator tiles in the accumulation registers, 4 in ordinary ones: with all 256 in the
   // accumulation file the compiler has no spare tile there and shuffles tiles between the files in the loop
 #pragma unroll
@@ -371,6 +432,32 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
       if (i < kAccTilesRows) asm volatile("" : "+a"(acc[i][j]));
       else asm volatile("" : "+v"(acc[i][j]));
     }
+  if constexpr (BACK && MX) {
+    // Slots 2 b and 2 b + 1 hold a step of parity b, slot 4 codes and scales of two steps.  In step kt: codes of kt + 2 are asked for before its
+    // operands are out; behind that those of kt + 1, asked for a step ago, are turned into its W side, and X of kt + 2 is asked for.  Both waits
+    // leave the eleven copies issued since out.
+    for (int kt = 0; kt < KT; ++kt) {
+      wait_vm<11>();                       // X of this step (behind it: codes of kt + 1, X of kt + 1)
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // this wave's part of its W side
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      auto mid = [&]() __attribute__((always_inline)) {
+        wait_vm<11>();                       // codes of kt + 1 (behind them: X of kt + 1, codes of kt + 2)
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // operand reads have returned
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      };
+      auto copy = [&](int q) __attribute__((always_inline)) {
+        if (q < 15 && q % 5 == 0) issue_raw(kt + 2, q / 5);
+        if (q == 16) read_raw(kt + 1);
+        if (q >= 20 && q < 60 && q % 5 == 0) issue_one(kt + 2, (q - 20) / 20, 2 * (kt & 1) + (q - 20) / 20, (q - 20) / 5 % 4);
+        if (q >= 22 && q < 62 && q % 5 == 2) put_raw(kt + 1, (q - 22) / 5);
+      };
+      const int b = 2 * (kt & 1);
+      mma64(std::integral_constant<bool, BACK>{}, b + wm, b + wn, mid, copy);
+      asm volatile("" ::: "memory");
+    }
+  } else {
   // The ring: halves 2 kt and 2 kt + 1 (this step) are read, the two of the next step are on their way, the
   // fifth slot takes the first half of the step after next at once and the second half goes into this step's
   // first slot as soon as every wave has taken its operands out: a copy has between one and three quarters and
@@ -406,6 +493,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
     }
     asm volatile("" ::: "memory");
     h0 = h2;
+  }
   }
   wait_vm<0>();
   __syncthreads();
@@ -999,7 +1087,7 @@ static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t st
     const int64_t tiles = (int64_t)p.tilesM * p.tilesN;
     int64_t total = tiles * (MODE == kBack && p.S > 1 ? p.S : 1), units = 0;
     if ((MODE != kPlain || MX) && total == tiles) {
-      const CutPlan cut = cut_plan(tiles, p.d1 / kTK, MX);
+      const CutPlan cut = cut_plan(tiles, p.d1 / kTK, MX && MODE != kBack);
       p.whole = (int)cut.whole; p.cut = cut.parts; p.cut_steps = cut.steps;
       total = cut.whole;
       units = (tiles - cut.whole) * cut.parts;
@@ -1107,7 +1195,7 @@ int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
   p.partial = p.S > 1 ? g.partial : nullptr;
   p.cut_sums = g.partial; p.cut_cnt = g.cnt;
   p.partial_stride = (size_t)g.M * g.d;
-  const int rc = launch_prefill<kBack, false>(p, g.M, 0, stream);
+  const int rc = g.mx4 ? launch_prefill<kBack, true>(p, g.M, 0, stream) : launch_prefill<kBack, false>(p, g.M, 0, stream);
   if (rc || p.S == 1) return rc;
   const int64_t fours = g.M * g.d / 4;
   hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, stream, g.partial, p.S, p.partial_stride, fours, g.dX);

@@ -118,6 +118,7 @@ struct GatedBackArgs {
   int d, F;
   const int32_t* row_to_req;
   const bf16_t *Wg, *Wu;  // row-major [F][d]
+  bool mx4;               // 4-bit weights in their place, d % 128 == 0
   AdapterView ad;
   const int32_t* tenant_id;
   const uint8_t* route;

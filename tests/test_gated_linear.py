@@ -233,7 +233,8 @@ def test_any_shape_forward_and_backward(M, d, F, rows, dtype, ranks):
 @pytest.mark.parametrize("M,d,F,rows,mx4", [(1, 64, 64, "own", False), (5, 128, 192, "mixed", False), (64, 64, 128, "own", False), (100, 256, 704, "mixed", False),
                                             (257, 192, 320, "sorted", False), (600, 512, 1088, "mixed", False), (700, 1040, 448, "sorted", False),
                                             (1500, 320, 1024, "sorted", False), (4200, 4128, 704, "sorted", False), (65, 96, 32, "mixed", False), (300, 288, 800, "mixed", True),
-                                            (1100, 1056, 1504, "sorted", False), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
+                                            (1100, 1056, 1504, "sorted", False), (40, 384, 96, "mixed", True), (1100, 1152, 1504, "sorted", True), (7, 128, 32, "own", True),
+                                            (2100, 4352, 512, "sorted", True), (33, 96, 128, "mixed", True), (300, 256, 704, "mixed", True), (64, 160, 48, "mixed", True)])
 @pytest.mark.parametrize("ranks", [(8,), (16, 32), (5, 33, 256)])
 def test_backward_bf16(M, d, F, rows, mx4, ranks):
     c, x, W, dense = _layer(M, M if rows == "own" else min(M, 6), 3, d, F, ranks, M + d, torch.bfloat16, rows, mx4)
