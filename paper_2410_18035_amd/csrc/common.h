@@ -147,20 +147,26 @@ struct LaunchMarks {
 // eight waves are there and no wave is without a chunk.  The workspace holds one [M][r_max] fp32 array per part.
 constexpr int kShrinkChunkK = 128;
 constexpr int64_t kTileMaxRows = 4096;  // rows of one launch of the tile kernel
-inline int shrink_parts(int64_t M, int d1) {
+// Blocks x parts of a site, at most.  Two sites in one launch: more for long reductions (2500 rows, 11008 inputs, four or six parts 42 us, two 50), fewer
+// for many rows (8192 rows, two parts 114 us and with 5120 inputs 44, four 117 and 51).
+inline int shrink_units(int64_t M, int d1, int sites) {
+  if (sites == 1) return 512;
+  return M > kTileMaxRows ? 320 : d1 > 7 * 8 * kShrinkChunkK ? 1024 : 512;
+}
+inline int shrink_parts(int64_t M, int d1, int sites = 1) {
   const int64_t blocks = M <= kTileMaxRows ? (M + 15) / 16 : (M + 63) / 64;
   const int most = (d1 + 8 * kShrinkChunkK - 1) / (8 * kShrinkChunkK);
   int parts = 1;
-  while (parts < 8 && parts * 2 <= most && blocks * parts * 2 <= 512) parts *= 2;
+  while (parts < 8 && parts * 2 <= most && blocks * parts * 2 <= shrink_units(M, d1, sites)) parts *= 2;
   return parts;
 }
 
-// The most rows x parts over all calls of up to M rows and d1 inputs (a call of more than one part has at most 512 blocks x parts).
-inline size_t shrink_rows_bound(int64_t M, int d1) {
+// The most rows x parts over all calls of up to M rows and d1 inputs (what a call of more than one part has at most goes up with both).
+inline size_t shrink_rows_bound(int64_t M, int d1, int sites = 1) {
   const int most = (d1 + 8 * kShrinkChunkK - 1) / (8 * kShrinkChunkK);
   int parts = 1;
   while (parts < 8 && parts * 2 <= most) parts *= 2;
-  const int64_t cut = M * parts, cap = 512 * (M <= kTileMaxRows ? 16 : 64);
+  const int64_t cut = M * parts, cap = (int64_t)shrink_units(M, d1, sites) * (M <= kTileMaxRows ? 16 : 64);
   const int64_t n = parts > 1 && cut < cap ? cut : cap;
   return (size_t)(parts == 1 || n < M ? M : n);
 }

@@ -98,7 +98,7 @@ size_t gated_workspace_bytes(int64_t M, int d, int F, int dtype, bool mx4, int r
   if (dtype == MILORA_BF16) {  // control words, shrinks of both sites, look-ups, partial tiles, 4-bit weights in bf16
     Carver c{nullptr};
     c.take<char>(kStreamCtrlBytes);
-    c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
+    c.take<float>(shrink_rows_bound(M, d, 2) * r_max * 2);
     c.take<int2>((size_t)M * 2);
     c.take<char>(gated_partial_bytes(M, d, F));
     c.take<bf16_t>(halves_of(nullptr, M, r_max).site * 2);
@@ -133,12 +133,12 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
   if (small || large) {
     Carver c{(char*)workspace};
     char* const ctrl = c.take<char>(kStreamCtrlBytes);
-    const int parts = shrink_parts(M, g.d);
+    const int parts = shrink_parts(M, g.d, 2);
     GatedTileArgs a{};
     a.d = g.d; a.F = g.F; a.packed = packed; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;
     a.t_stride = (size_t)M * g.ad.r_max; a.t_site = a.t_stride * parts; a.parts = parts; a.lora_site = (size_t)M;
     a.cnt = (int*)(ctrl + kTileCtrlOffset);
-    float* const t = c.take<float>(shrink_rows_bound(M, g.d) * g.ad.r_max * 2);
+    float* const t = c.take<float>(shrink_rows_bound(M, g.d, 2) * g.ad.r_max * 2);
     int2* const looked_up = c.take<int2>((size_t)M * 2);
     a.partial = c.take<float>(gated_partial_bytes(M, g.d, g.F) / sizeof(float));
     a.halves = halves_of(nullptr, M, g.ad.r_max);
@@ -751,8 +751,8 @@ BackWs carve_back(void* base, int64_t M, int d, int F, int dtype, bool mx4, int 
   Carver c{(char*)base};
   BackWs w;
   w.dz = c.take<char>((size_t)M * F * 2 * dtype_size(dtype));
-  w.low = c.take<float>(shrink_rows_bound(M, F) * r_max * 2);
-  w.t = c.take<float>(shrink_rows_bound(M, d) * r_max * 2);
+  w.low = c.take<float>(shrink_rows_bound(M, F, 2) * r_max * 2);
+  w.t = c.take<float>(shrink_rows_bound(M, d, 2) * r_max * 2);
   w.row_lora = c.take<int2>((size_t)M * 2);
   w.among = c.take<int2>((size_t)((M + 63) / 64) * 2);
   w.W = c.take<bf16_t>(mx4 ? (size_t)d * F * 2 : 0);
@@ -829,9 +829,9 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
   hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
                      g.route, g.B, w.row_lora, w.among, w.cnt);
   if ((rc = check_launch())) return rc;
-  const int low_parts = shrink_parts(M, g.F);
+  const int low_parts = shrink_parts(M, g.F, 2);
   const size_t row_floats = (size_t)M * r_max;
-  const HalvesOf low{w.low, low_parts, w.low_halves}, t{w.t, shrink_parts(M, g.d), w.t_halves};
+  const HalvesOf low{w.low, low_parts, w.low_halves}, t{w.t, shrink_parts(M, g.d, 2), w.t_halves};
   if (dB) {
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
     if (rc) return rc;

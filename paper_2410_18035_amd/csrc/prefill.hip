@@ -1205,7 +1205,7 @@ int gated_dx_tiles(const GatedBackArgs& g, hipStream_t stream) {
 static int launch_shrinks(ShrinkArgs g, bool trans, hipStream_t stream) {
   const ShrinkArgs all = g;
   const int64_t M = g.M;
-  const int parts = shrink_parts(M, g.d1);
+  const int parts = shrink_parts(M, g.d1, g.sites);
   const int64_t slice = (int64_t)1 << 28;  // rows per launch: 512 threads for 64 rows, a grid has to stay below 2^32 threads
   for (int64_t r0 = 0; r0 < M; r0 += slice) {
     g.X = all.X + (size_t)r0 * g.ldx;
@@ -1228,22 +1228,22 @@ static int launch_shrinks(ShrinkArgs g, bool trans, hipStream_t stream) {
 }
 
 // LoRA shrink of the rows the tile kernel serves (same conditions as prefill_supported) at `sites` consecutive sites: t receives
-// shrink_parts(M, d1) partial results [site][part][M][r_max], to be added in part order, row_lora (or null) [site][M] what the
+// shrink_parts(M, d1, sites) partial results [site][part][M][r_max], to be added in part order, row_lora (or null) [site][M] what the
 // look-ups found of each row; `clear` (or null) is zeroed.
 int launch_shrink_sites(const bf16_t* X, int64_t ldx, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site, int sites,
                         const int32_t* tenant_id, const uint8_t* route, int B, float* t, int2* row_lora, int* clear, hipStream_t stream) {
   const size_t t_stride = (size_t)M * ad.r_max;
   return launch_shrinks(ShrinkArgs{X, ldx, M, 0, d1, site, B, row_to_req, tenant_id, route, ad, t, t_stride, row_lora, clear, sites,
-                                   t_stride * shrink_parts(M, d1), (size_t)M, 0}, true, stream);
+                                   t_stride * shrink_parts(M, d1, sites), (size_t)M, 0}, true, stream);
 }
 
 // low[site][part][m][0..r) = dz[m] (of the site) . (W^B)^T for the rows routed to the gate (site 4) and the up projection; dz [M][2 F],
-// F % 32 == 0, shrink_parts(M, F) parts.
+// F % 32 == 0, shrink_parts(M, F, 2) parts.
 int launch_low_sites(const bf16_t* dz, int64_t M, int F, const int32_t* row_to_req, const AdapterView& ad, const int32_t* tenant_id,
                      const uint8_t* route, int B, float* low, hipStream_t stream) {
   const size_t stride = (size_t)M * ad.r_max;
   return launch_shrinks(ShrinkArgs{dz, 2 * (int64_t)F, M, 0, F, 4, B, row_to_req, tenant_id, route, ad, low, stride, nullptr, nullptr, 2,
-                                   stride * shrink_parts(M, F), (size_t)M, F}, false, stream);
+                                   stride * shrink_parts(M, F, 2), (size_t)M, F}, false, stream);
 }
 
 int launch_shrink_tiles(const bf16_t* X, int64_t M, int d1, const int32_t* row_to_req, const AdapterView& ad, int site,
