@@ -6,8 +6,8 @@
 //
 // Forward: bf16 takes the matrix-core tiles with gate and up columns side by side (tiles.hip, prefill.hip), 4-bit weights of few rows
 // mx4.hip, of more the same tiles, on the codes or on the weights written out in bf16, whichever is reckoned shorter; everything else the
-// any-shape kernels of linear_generic.hip.  Backward: the 256 x 256 tiles of prefill.hip for dX (4-bit weights written out first: the product
-// runs along their columns, and a byte holds two inputs of one) and the bf16 matrix cores below for dA and dB; everything else the any-shape
+// any-shape kernels of linear_generic.hip.  Backward: the 256 x 256 tiles of prefill.hip for dX, on the codes of 4-bit weights too
+// (d % 128 == 0; others are written out first), and the bf16 matrix cores below for dA and dB; everything else the any-shape
 // kernels below, fp32 matrix instructions.
 #include "gated.h"
 #include "mx4.h"
