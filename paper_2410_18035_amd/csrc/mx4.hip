@@ -212,8 +212,8 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   }
 }
 
-// MORE: more than 32 rows.  XM: pieces of X a thread brings; with four (rows below five) the registers allow three workgroups a compute unit
-// (gated, one row of 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3).
+// MORE: more than 32 rows.  XM: pieces of X a thread brings; with four the registers allow three workgroups a compute unit (gated, one row of
+// 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3).
 template <int KW, int NL, bool MORE, int XM>
 __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_ker
   if (MORE) id = (id & 7) * per + (id >> 3);
   if (id >= total) return;
   constexpr int kCols = kMxCols / KW, kPart = KW * NL * 64;  // columns and inputs of the workgroup
+  constexpr int kScalePitch = KW * NL * 2 + 16, kScaleArea = kCols * kScalePitch;  // scales in LDS, [column][..], in front of X
   constexpr int kPitch = kPart * 2 + 16;                     // a row of X in LDS: 16 bytes past a multiple of all banks
   // Up to 16 rows: matrix instructions of 16 x 16, 32 inputs.  A lane's group g of a column: inputs 32 g of every kG x 32, kH columns a lane
   constexpr bool k16 = KW >= 4;
@@ -253,35 +254,42 @@ __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_ker
       if (e < 32 * kPieces && m < g.M && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(g.X + (size_t)m * g.ldx + k_part + p * 8);
     }
   };
+  // ---- scales: whole lines of the workgroup's columns, into LDS with the first rows of X ----
+  constexpr int kScales = KW * NL * 2, kScalePieces = kScales / 16;  // bytes of a column, and pieces
+  u32x4 scales = u32x4{0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+  const int scale_col = tid / kScalePieces, scale_piece = tid % kScalePieces;
+  if (scale_col < kCols) {
+    int col = cg * kCols + scale_col;
+    col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
+    const int from = (k_part >> 5) + scale_piece * 16, left = (d1 >> 5) - from;
+    const uint8_t* const sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5) + from;
+    typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
+    if (left >= 16) {
+      scales = *reinterpret_cast<const u32x4_a1*>(sp);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < left) scales[e >> 2] = (scales[e >> 2] & ~(255u << (8 * (e & 3)))) | ((uint32_t)sp[e] << (8 * (e & 3)));
+    }
+  }
   ask_x(rg * 32);
   __builtin_amdgcn_sched_barrier(0);
-  // ---- codes and scales: NL steps ----
+  // ---- codes: NL steps ----
   u32x4 c[kH][kS];
-  typedef typename std::conditional<k16, uint32_t, uint16_t>::type scales_t;  // of a step: kG bytes
-  typedef scales_t scales_a1 __attribute__((ext_vector_type(4), aligned(1)));
-  scales_a1 sc[kH][kS / 4];
 #pragma unroll
   for (int h = 0; h < kH; ++h) {
     int col = n0 + h * kSide + ln;
     col = col < g.d2 ? col : g.d2 - 1;  // (columns past the end: results dropped)
     const unsigned char* const wp = g.W[site] + (size_t)col * (d1 >> 1) + lg * 16 + (k0 >> 1);
-    const uint8_t* const sp = g.W[site] + (size_t)d1 * g.d2 / 2 + (size_t)col * (d1 >> 5) + (k0 >> 5);
     if (k0 + NL * 64 <= d1) {
 #pragma unroll
       for (int i = 0; i < kS; ++i) c[h][i] = *reinterpret_cast<const u32x4*>(wp + i * kG * 16);
-#pragma unroll
-      for (int i = 0; i < kS / 4; ++i) sc[h][i] = *reinterpret_cast<const scales_a1*>(sp + i * 4 * kG);
     } else {  // zeros past the end of the reduction
 #pragma unroll
       for (int i = 0; i < kS; ++i) {
         const int at = k0 + (i * kG + lg) * 32;
         c[h][i] = u32x4{0u, 0u, 0u, 0u};
-        scales_t one = 127;
-        if (at < d1) {
-          c[h][i] = *reinterpret_cast<const u32x4*>(wp + i * kG * 16);
-          one = sp[i * kG + lg];
-        }
-        sc[h][i / 4][i & 3] = (scales_t)(one << (8 * lg));
+        if (at < d1) c[h][i] = *reinterpret_cast<const u32x4*>(wp + i * kG * 16);
       }
     }
   }
@@ -292,13 +300,15 @@ __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_ker
     asm volatile("" ::: "memory");
   };
   constexpr int Ld = kMxCols + 4;  // a row of all waves' columns: [row][wave][32]
-  float* const red = reinterpret_cast<float*>(lds);
+  float* const red = reinterpret_cast<float*>(lds + kScaleArea);
+  if (scale_col < kCols) *reinterpret_cast<u32x4*>(lds + scale_col * kScalePitch + scale_piece * 16) = scales;
+  typedef typename std::conditional<k16, uint32_t, uint16_t>::type scales_t;  // of a step: kG bytes
   for (;;) {
     const int m0 = rg * 32, rows = g.M - m0 < 32 ? g.M - m0 : 32;
 #pragma unroll
     for (int u = 0; u < kXMost; ++u) {
       const int e = tid + u * kMxT, r = e / kPieces, p = e % kPieces;
-      if (r < rows) *reinterpret_cast<u32x4*>(lds + r * kPitch + p * 16) = x[u];
+      if (r < rows) *reinterpret_cast<u32x4*>(lds + kScaleArea + r * kPitch + p * 16) = x[u];
     }
     barrier();
     rg += row_split;
@@ -311,12 +321,13 @@ __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_ker
       for (int e = 0; e < (k16 ? 4 : 16); ++e) acc[h][e] = 0.f;
     if (n0 < g.d2 && k0 < d1) {
       const int row = ln < rows ? ln : rows - 1;  // (rows past the end: results dropped)
-      const unsigned char* const xr = lds + row * kPitch + kw * NL * 128 + lg * 64;
+      const unsigned char* const xr = lds + kScaleArea + row * kPitch + kw * NL * 128 + lg * 64;
+      const scales_t* const sr = reinterpret_cast<const scales_t*>(lds + (cw * 32 + ln) * kScalePitch + kw * NL * 2);
 #pragma unroll
       for (int i = 0; i < kS; ++i) {
         float scale[kH];
 #pragma unroll
-        for (int h = 0; h < kH; ++h) scale[h] = mx4_scale(((uint32_t)sc[h][i / 4][i & 3] >> (8 * lg)) & 255u);
+        for (int h = 0; h < kH; ++h) scale[h] = mx4_scale(((uint32_t)sr[h * kSide * (kScalePitch / (int)sizeof(scales_t)) + i] >> (8 * lg)) & 255u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const bf16x8 xv = *reinterpret_cast<const bf16x8*>(xr + i * kG * 64 + e * 16);
@@ -519,12 +530,14 @@ int launch_base(const MxBase& b, hipStream_t st) {
   constexpr int kPart = KW * NL * 64, kRed = 32 * (kMxCols + 4) * 4;
   const int rows = b.M < 32 ? b.M : 32, x = rows * (kPart * 2 + 16), red = rows * (kMxCols + 4) * 4;
   int bytes = x > red ? x : red;
+  constexpr int kScaleArea = kMxCols / KW * (KW * NL * 2 + 16);
+  bytes += kScaleArea;
   if (bytes < kMxW * 256 * 4) bytes = kMxW * 256 * 4;  // (the shrink's sums)
   static thread_local int lds_set_for = -1;
   int dev = 0;
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
-    const int most = 32 * (kPart * 2 + 16) > kRed ? 32 * (kPart * 2 + 16) : kRed;
+    const int most = (32 * (kPart * 2 + 16) > kRed ? 32 * (kPart * 2 + 16) : kRed) + kScaleArea;
     MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE, XM>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
     lds_set_for = dev;
   }
@@ -535,12 +548,19 @@ int launch_base(const MxBase& b, hipStream_t st) {
 }
 
 // How the first launch cuts a call; functions of the sizes alone, shared by the launch and the workspace's sizing.  Waves that share columns:
-// X of a row group is rows x KW x NL x 128 bytes, 64 KB of LDS at most (two workgroups a compute unit), and as few parts as that allows.
+// X of a row group is rows x KW x NL x 128 bytes, 64 KB of LDS at most (two workgroups a compute unit), and few parts.  Up to eight rows parts of
+// half the length where they let more workgroups run at once: one and two rows (us a call, one row, 4096 x 4096 8.0 for 8.8, 4096 x 12288 11.1 for
+// 12.0, gated 4096 x 11008 14.7 for 14.9), five to eight (gated, 8 rows, 18.4 for 22.6); three and four rows not (4 rows, 4096 x 12288, 14.5 for 13.9).
 constexpr int kMxSteps = 8;
 int mx4_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
-int mx4_parts(int64_t M, int d1) { return (d1 + mx4_waves(M) * kMxSteps * 64 - 1) / (mx4_waves(M) * kMxSteps * 64); }
-// (parts grow with the rows: no size lowers it)
-size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) { return (size_t)M * d2 * sites * mx4_parts(M, d1); }
+bool mx4_short(int64_t M) { return M <= 2 || (M >= 5 && M <= 8); }
+int mx4_part(int64_t M) { return mx4_waves(M) * (mx4_short(M) ? kMxSteps / 2 : kMxSteps) * 64; }  // inputs
+int mx4_parts(int64_t M, int d1) { return (d1 + mx4_part(M) - 1) / mx4_part(M); }
+// (the most parts of up to M rows: no size lowers it)
+size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
+  const int part = M <= 16 ? mx4_part(1) : mx4_part(17);
+  return (size_t)M * d2 * sites * ((d1 + part - 1) / part);
+}
 int mx4_shrink_parts(int d1) { return (d1 + kMxShrinkK - 1) / kMxShrinkK; }
 
 // Groups of eight of one launch: a grid has to stay below 2^32 threads.
@@ -616,8 +636,8 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.row_groups = (g.M + 31) / 32;
   const int64_t units = (int64_t)sites * b.col_groups * b.parts;
   b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
-  const int rc = kw == 8 && g.M <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
-                 : kw == 8 ? launch_base<8, kMxSteps, false, 8>(b, st)
+  const int rc = kw == 8 && g.M <= 2 ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
+                 : kw == 8 ? (mx4_short(g.M) ? launch_base<8, kMxSteps / 2, false, 4>(b, st) : launch_base<8, kMxSteps, false, 4>(b, st))
                  : kw == 4 ? launch_base<4, kMxSteps, false, 8>(b, st)
                  : b.row_groups == 1 ? launch_base<2, kMxSteps, false, 8>(b, st)
                                      : launch_base<2, kMxSteps, true, 8>(b, st);
