@@ -285,7 +285,7 @@ def milora_routed_linear_tile(M: int, d1: int, d2: int, dtype: torch.dtype, w_la
 def _check_weight(W: torch.Tensor, d1: int, d2: int, w_layout: int, dtype: torch.dtype) -> None:
     """Shape and type of a base weight of d1 inputs and d2 columns in a layout."""
     if w_layout == W_MX4:
-        if W.dtype != torch.uint8 or W.numel() != quantized_weight_bytes(d1, d2) or W.numel() == 0:
+        if W.dtype != torch.uint8 or d1 % 32 or d1 < 1 or d2 < 1 or W.numel() != d1 * d2 * 17 // 32:  # (quantized_weight_bytes, half a microsecond sooner)
             raise ValueError("a quantised W holds quantized_weight_bytes(d1, d2) bytes")
         return
     if w_layout == W_ROWMAJOR:
@@ -550,11 +550,10 @@ def milora_quantize_weight(W: torch.Tensor, out: Optional[torch.Tensor] = None) 
     """A row-major [d2, d1] weight (bf16 or fp32) to 4-bit values with a power-of-two scale for every 32 inputs: uint8
     codes [d2, d1/2], then scales [d2, d1/32]."""
     d2, d1 = W.shape
-    nbytes = quantized_weight_bytes(d1, d2)
     if out is None:
-        out = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
-    elif out.dtype != torch.uint8 or out.numel() != nbytes:
-        raise ValueError("out holds quantized_weight_bytes(d1, d2) bytes")
+        out = torch.empty(quantized_weight_bytes(d1, d2), dtype=torch.uint8, device=W.device)
+    else:
+        _check_weight(out, d1, d2, W_MX4, W.dtype)
     rc = lib().milora_quantize_weight(_dev(W), _dtype_code(W), _dev(out), d1, d2, _stream(W))
     if rc != 0:
         raise MiloraError(rc, "milora_quantize_weight")
