@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_ker
       f32x4 v = *reinterpret_cast<const f32x4*>(q);
 #pragma unroll
       for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4*>(q + k * 32);
-      *reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n) = v;
+      st_through(reinterpret_cast<f32x4*>(out + (size_t)r * g.d2 + n), v);  // (left in the L2, the launch ends by writing it back: 96 rows 33 us a call, so 31)
     }
     if (!more) return;
     barrier();
