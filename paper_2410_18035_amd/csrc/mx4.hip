@@ -215,7 +215,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
 // MORE: more than 32 rows.  XM: pieces of X a thread brings; with four the registers allow three workgroups a compute unit (gated, one row of
 // 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3).
 template <int KW, int NL, bool MORE, int XM>
-__global__ void __launch_bounds__(kMxT, KW == 8 && XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
+__global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -547,18 +547,20 @@ int launch_base(const MxBase& b, hipStream_t st) {
   return check_launch();
 }
 
-// How the first launch cuts a call; functions of the sizes alone, shared by the launch and the workspace's sizing.  Waves that share columns:
-// X of a row group is rows x KW x NL x 128 bytes, 64 KB of LDS at most (two workgroups a compute unit), and few parts.  Up to eight rows parts of
-// half the length where they let more workgroups run at once: one and two rows (us a call, one row, 4096 x 4096 8.0 for 8.8, 4096 x 12288 11.1 for
-// 12.0, gated 4096 x 11008 14.7 for 14.9), five to eight (gated, 8 rows, 18.4 for 22.6); three and four rows not (4 rows, 4096 x 12288, 14.5 for 13.9).
+// How the first launch cuts a call; functions of the sizes alone.  Waves that share columns: X of a row group is rows x KW x NL x 128 bytes, 64 KB
+// of LDS at most (two workgroups a compute unit), and few parts.  Up to 16 rows parts of half the length where they let more workgroups run at once:
+// one and two rows always (us a call, one row, 4096 x 4096 8.0 for 8.8, 4096 x 12288 11.1 for 12.0, gated 4096 x 11008 14.7 for 14.9), the
+// others where whole ones are more than two for each compute unit (gated 4096 x 11008, 8 rows 18.4 for 22.6, 16 rows 21.9 for 24.0; where they
+// are not: 4096 x 12288, 4 rows 14.5 for 13.9, 16 rows 16.0 for 15.4).
 constexpr int kMxSteps = 8;
 int mx4_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
-bool mx4_short(int64_t M) { return M <= 2 || (M >= 5 && M <= 8); }
-int mx4_part(int64_t M) { return mx4_waves(M) * (mx4_short(M) ? kMxSteps / 2 : kMxSteps) * 64; }  // inputs
-int mx4_parts(int64_t M, int d1) { return (d1 + mx4_part(M) - 1) / mx4_part(M); }
-// (the most parts of up to M rows: no size lowers it)
+bool mx4_short(int64_t M, int d1, int d2, int sites) {
+  const int kw = mx4_waves(M), cols = kMxCols / kw, part = kw * kMxSteps * 64;
+  return M <= 2 || (M <= 16 && (int64_t)sites * ((d2 + cols - 1) / cols) * ((d1 + part - 1) / part) > 512);
+}
+// (with the shorter parts where they can be: no size lowers it)
 size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
-  const int part = M <= 16 ? mx4_part(1) : mx4_part(17);
+  const int part = mx4_waves(M) * kMxSteps * 64 / (M <= 16 ? 2 : 1);
   return (size_t)M * d2 * sites * ((d1 + part - 1) / part);
 }
 int mx4_shrink_parts(int d1) { return (d1 + kMxShrinkK - 1) / kMxShrinkK; }
@@ -623,24 +625,29 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.X = g.X; b.ldx = g.ldx; b.M = g.M; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
   b.sites = sites;
-  b.parts = mx4_parts(g.M, g.d1);
+  const int kw = mx4_waves(g.M);
+  const bool half = mx4_short(g.M, g.d1, g.d2, sites);
+  const int part = kw * kMxSteps * 64 / (half ? 2 : 1);
+  b.parts = (g.d1 + part - 1) / part;
   b.partial = partial;
   b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, nullptr, nullptr,
                         sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
   b.terms = terms;
   b.shrink_parts = t_parts;
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
-  const int kw = mx4_waves(g.M);
   b.col_groups = (g.d2 + kMxCols / kw - 1) / (kMxCols / kw);
   // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
   b.row_groups = (g.M + 31) / 32;
   const int64_t units = (int64_t)sites * b.col_groups * b.parts;
   b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
-  const int rc = kw == 8 && g.M <= 2 ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
-                 : kw == 8 ? (mx4_short(g.M) ? launch_base<8, kMxSteps / 2, false, 4>(b, st) : launch_base<8, kMxSteps, false, 4>(b, st))
-                 : kw == 4 ? launch_base<4, kMxSteps, false, 8>(b, st)
-                 : b.row_groups == 1 ? launch_base<2, kMxSteps, false, 8>(b, st)
-                                     : launch_base<2, kMxSteps, true, 8>(b, st);
+  const int rc = g.M <= 2              ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
+                 : kw == 8 && half    ? launch_base<8, kMxSteps / 2, false, 4>(b, st)
+                 : kw == 8 && g.M <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
+                 : kw == 8            ? launch_base<8, kMxSteps, false, 8>(b, st)
+                 : kw == 4 && half    ? launch_base<4, kMxSteps / 2, false, 4>(b, st)
+                 : kw == 4            ? launch_base<4, kMxSteps, false, 8>(b, st)
+                 : b.row_groups == 1  ? launch_base<2, kMxSteps, false, 8>(b, st)
+                                      : launch_base<2, kMxSteps, true, 8>(b, st);
   if (rc) return rc;
   MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, terms};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
