@@ -31,6 +31,7 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
 struct MxArgs {
   const bf16_t* X;  // M rows of ldx elements
   int64_t ldx;
+  bool second;      // behind them M rows with what their rounding left, which the products take in as well (the shrinks do not)
   int M, d1, d2;
   const unsigned char* W[3];  // of the sites; gated: W[0] gate, W[1] up
   const bf16_t* bias;
@@ -40,6 +41,7 @@ struct MxArgs {
   float* up_out;
   const bf16_t* res;   // [M][d2] or null: h_out = res + linear, in fp32, and Y that rounded
   float* h_out;
+  bf16_t* left_out;    // [M][d2] or null: what the rounding of Y left of h_out
   const float* h_in;   // [M][d2] or null: Y = h_in + linear
   const bf16_t* norm_x;  // [M][d1] or null: the products are of the rows divided by the root of their mean square (plus 1e-5)
   const float* norm_h;   // the same, rows in fp32

@@ -158,8 +158,9 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   const ShrinkArgs& sh = g.shrink;
   const int tid = threadIdx.x, lane = tid & 63, d1 = g.d1;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (id >= g.M * g.sites * g.shrink_parts) return;
-  const int part = id % g.shrink_parts, m = id / g.shrink_parts % g.M, s = id / (g.shrink_parts * g.M), site = sh.site + s;
+  const int M = (int)sh.M;
+  if (id >= M * g.sites * g.shrink_parts) return;
+  const int part = id % g.shrink_parts, m = id / g.shrink_parts % M, s = id / (g.shrink_parts * M), site = sh.site + s;
   const int64_t req = sh.row_to_req ? (int64_t)sh.row_to_req[m] : m;
   int ten = -1;
   const int r = req >= 0 && req < sh.B ? routed_rank(sh.ad, sh.tenant_id, sh.route, (int)req, sh.B, site, &ten) : 0;
@@ -370,7 +371,7 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
 constexpr int kFinT = 256, kFinCols = 256;
 struct MxFinish {
   MxArgs a;
-  int parts;
+  int parts, rows;  // rows of a part: a.M, or twice that
   const float* partial;
   const float* t;  // [site][t_parts][M][r_max]
   size_t t_part, t_site;
@@ -399,8 +400,8 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
 #pragma unroll
   for (int s = 0; s < kSites; ++s) {
     v[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const size_t stride = (size_t)g.M * g.d2;
-    const float* const q = f.partial + ((size_t)(s0 + s) * f.parts * g.M + m) * g.d2 + (in ? n : 0);
+    const size_t stride = (size_t)f.rows * g.d2;
+    const float* const q = f.partial + ((size_t)(s0 + s) * f.parts * f.rows + m) * g.d2 + (in ? n : 0);
     for (int p = w; p < f.parts; p += 16) {
       f32x4 x[4];
 #pragma unroll
@@ -408,6 +409,13 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (p + 4 * u < f.parts) v[s] += x[u];
+      if (g.second) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const f32x4*>(q + (size_t)g.M * g.d2 + (p + 4 * u < f.parts ? p + 4 * u : p) * stride);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (p + 4 * u < f.parts) v[s] += x[u];
+      }
     }
   }
   // ---- normalisation of the level's input: a factor of the row, applied to its products ----
@@ -523,6 +531,13 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
   o[0] = pack_bf16x2(y[0], y[1]);
   o[1] = pack_bf16x2(y[2], y[3]);
   *reinterpret_cast<u32x2_a8*>(g.Y[s0] + (size_t)m * g.ldy + n) = o;
+  if (!GATED && g.left_out) {
+    u32x2_a8 left;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      left[e] = pack_bf16x2(y[2 * e] - __uint_as_float(o[e] << 16), y[2 * e + 1] - __uint_as_float(o[e] & 0xffff0000u));
+    *reinterpret_cast<u32x2_a8*>(g.left_out + at) = left;
+  }
 }
 
 template <int KW, int NL, bool MORE, int XM>
@@ -621,12 +636,13 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   float* const t = (float*)workspace;
   MxTerm* const terms = (MxTerm*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
   float* const partial = (float*)((char*)terms + align_up((size_t)g.M * sites * sizeof(MxTerm), 256));
+  const int rows = g.second ? 2 * g.M : g.M;
   MxBase b{};
-  b.X = g.X; b.ldx = g.ldx; b.M = g.M; b.d1 = g.d1; b.d2 = g.d2;
+  b.X = g.X; b.ldx = g.ldx; b.M = rows; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
   b.sites = sites;
-  const int kw = mx4_waves(g.M);
-  const bool half = mx4_short(g.M, g.d1, g.d2, sites);
+  const int kw = mx4_waves(rows);
+  const bool half = mx4_short(rows, g.d1, g.d2, sites);
   const int part = kw * kMxSteps * 64 / (half ? 2 : 1);
   b.parts = (g.d1 + part - 1) / part;
   b.partial = partial;
@@ -637,19 +653,19 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
   b.col_groups = (g.d2 + kMxCols / kw - 1) / (kMxCols / kw);
   // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
-  b.row_groups = (g.M + 31) / 32;
+  b.row_groups = (rows + 31) / 32;
   const int64_t units = (int64_t)sites * b.col_groups * b.parts;
   b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
-  const int rc = g.M <= 2              ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
+  const int rc = rows <= 2             ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
                  : kw == 8 && half    ? launch_base<8, kMxSteps / 2, false, 4>(b, st)
-                 : kw == 8 && g.M <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
+                 : kw == 8 && rows <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
                  : kw == 8            ? launch_base<8, kMxSteps, false, 8>(b, st)
                  : kw == 4 && half    ? launch_base<4, kMxSteps / 2, false, 4>(b, st)
                  : kw == 4            ? launch_base<4, kMxSteps, false, 8>(b, st)
                  : b.row_groups == 1  ? launch_base<2, kMxSteps, false, 8>(b, st)
                                       : launch_base<2, kMxSteps, true, 8>(b, st);
   if (rc) return rc;
-  MxFinish f{g, b.parts, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, terms};
+  MxFinish f{g, b.parts, rows, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, terms};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);
   if (gated) hipLaunchKernelGGL(mx4_finish_kernel<true>, grid, dim3(kFinT), 0, st, f);
   else hipLaunchKernelGGL(mx4_finish_kernel<false>, grid, dim3(kFinT), 0, st, f);
