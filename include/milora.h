@@ -276,7 +276,8 @@ int milora_gated_linear_backward(const void *dY, const void *X, const float *gat
  *   attn_out  device [B][d] `dtype` or NULL
  *   qkv_out   device [B][3d] `dtype` or NULL: q | k | v of every request, for the caller's attention
  *   workspace device, milora_layer_decode_workspace_bytes(B, d, F, r_max) bytes (packed weights and B > 32:
- *             this includes the tables of fp32 partial tiles of the wide-batch kernel, tens of MB)
+ *             this includes the tables of fp32 partial tiles of the wide-batch kernel, tens of MB); never fewer when an
+ *             argument goes up
  * Errors: EINVAL, ERANGE (B > MILORA_MAX_DECODE_BATCH, r_max > MILORA_MAX_RANK), EUNSUPPORTED
  * (packed or 4-bit layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
  * weight not 16-byte aligned), EWORKSPACE, EHIP.

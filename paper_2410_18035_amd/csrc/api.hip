@@ -256,12 +256,14 @@ MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
   MxLayerWs w;
   w.h = (float*)(b + take((size_t)B * d * 4));
   w.qkv = (bf16_t*)(b + take((size_t)B * d * 6));
-  w.hn = (bf16_t*)(b + take((size_t)(B <= kMxSecond ? 2 * B : B) * d * 2));
+  // (room for the largest need of up to B requests: the size never falls with B, so that one workspace serves every smaller batch)
+  const int rows = B <= kMxSecond ? 2 * B : B > 2 * kMxSecond ? B : 2 * kMxSecond;
+  w.hn = (bf16_t*)(b + take((size_t)rows * d * 2));
   w.mm = (bf16_t*)(b + take((size_t)B * F * 2));
   size_t level = 0;
   const struct { int d1, d2, sites; } levels[4] = {{d, d, 3}, {d, d, 1}, {d, F, 2}, {F, d, 1}};
   for (const auto& l : levels) {
-    const size_t n = mx4_rows_workspace_bytes(l.sites == 2 && B <= kMxSecond ? 2 * B : B, l.d1, l.d2, r_max, l.sites);
+    const size_t n = mx4_rows_workspace_bytes(l.sites == 2 ? rows : B, l.d1, l.d2, r_max, l.sites);
     level = n > level ? n : level;
   }
   w.level = b + take(level);

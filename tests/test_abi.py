@@ -58,6 +58,17 @@ def test_workspace_sizes_are_monotone_and_reject_bad_sizes():
     assert mb.routed_linear_workspace_bytes(32768, 4096, 4096, 32) >= 32768 * 32 * 4
 
 
+@pytest.mark.parametrize("d,F", [(32, 32), (256, 704), (1000, 2730), (2080, 4128), (4096, 11008), (5120, 13824), (8192, 28672)])
+def test_decode_workspace_never_falls(d, F):
+    """A workspace for the largest batch serves every smaller one, at any layout."""
+    size = mb.layer_decode_workspace_bytes
+    for r in (1, 8, 32, 256):
+        sizes = [size(B, d, F, r) for B in range(1, 129)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+        for B in (1, 8, 9, 16, 17, 33, 128):
+            assert sizes[B - 1] <= min(size(B, d + 32, F, r), size(B, d, F + 32, r), size(B, d, F, min(r + 1, 256)))
+
+
 def test_kernel_choice_of_the_routed_linear():
     import torch
 
