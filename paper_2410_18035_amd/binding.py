@@ -196,6 +196,13 @@ class AdapterTable:
     n_tenants: int
     keep: tuple
 
+    def __post_init__(self) -> None:
+        """Extents of the matrices, read once: (d1, d2) of each site (None where tenants differ) and the tenants' ranks."""
+        A, B = self.keep
+        sizes = [{(a[m].shape[0], b[m].shape[1]) for a, b in zip(A, B)} for m in range(NUM_SITES)]
+        self.extents = [v.pop() if len(v) == 1 else None for v in sizes]
+        self.ranks = [a[0].shape[1] for a in A]
+
     @staticmethod
     def from_tensors(A: Sequence[Sequence[torch.Tensor]], B: Sequence[Sequence[torch.Tensor]],
                      rank: Sequence[int], r_max: Optional[int] = None) -> "AdapterTable":
@@ -341,7 +348,10 @@ def _shaped(t: Optional[torch.Tensor], shape, what: str) -> None:
         raise ValueError(f"{what} must be {list(shape)}")
 
 
-def _gated_sizes(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, w_layout: int, F: Optional[int],
+_GATE, _UP = 4, 5  # sites of the gated block
+
+
+def _gated_sizes(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, adapters: AdapterTable, w_layout: int, F: Optional[int],
                  row_to_req: Optional[torch.Tensor], route: torch.Tensor, B: int):
     M, d = X.shape
     if w_layout == W_ROWMAJOR:
@@ -352,6 +362,8 @@ def _gated_sizes(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, w_la
     _check_weight(W_up, d, F, w_layout, X.dtype)
     _shaped(row_to_req, (M,), "row_to_req")
     _shaped(route, (B,), "route")
+    if adapters.extents[_GATE] != (d, F) or adapters.extents[_UP] != (d, F):
+        raise ValueError("adapter matrices of sites 4 and 5 must be [d, r_t] and [r_t, F]")
     return M, d, F
 
 
@@ -362,7 +374,7 @@ def milora_gated_linear(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tenso
     """Y = silu(X W_gate + its LoRA term) * (X W_up + its LoRA term).  Weights [F, d] row-major, or W_MX4 (then pass F);
     gate_out and up_out, float32 [M, F], receive both projections for the backward pass."""
     B = tenant_id.numel()
-    M, d, F = _gated_sizes(X, W_gate, W_up, w_layout, F, row_to_req, route, B)
+    M, d, F = _gated_sizes(X, W_gate, W_up, adapters, w_layout, F, row_to_req, route, B)
     if out is None:
         out = torch.empty(M, F, dtype=X.dtype, device=X.device)
     for t, what in ((out, "out"), (gate_out, "gate_out"), (up_out, "up_out")):
@@ -388,6 +400,26 @@ class GradientTable:
     dtype: torch.dtype
     keep: tuple
 
+    def __post_init__(self) -> None:
+        """What the adapters have to look like: (d, F) of the gated block and each tenant's rank, as sets of what the gradients say."""
+        dA, dB = self.keep
+        every = [g for rows in (dA, dB) for row in rows for g in row if g is not None and g.numel()]
+        spans = sorted((g.data_ptr(), g.data_ptr() + g.numel() * g.element_size()) for g in every)
+        if any(after[0] < before[1] for before, after in zip(spans, spans[1:])):
+            raise ValueError("two gradients in one place")
+        here = lambda rows, t: [rows[t][s] for s in (_GATE, _UP) if rows[t][s] is not None]
+        tenants = range(len(dA))
+        if any(g.dim() != 2 for t in tenants for g in here(dA, t) + here(dB, t)):
+            raise ValueError("dA must be [d, r_t] and dB must be [r_t, F]")
+        self.ranks = [{a.shape[1] for a in here(dA, t)} | {b.shape[0] for b in here(dB, t)} for t in tenants]
+        self.inputs = {a.shape[0] for t in tenants for a in here(dA, t)}
+        self.columns = {b.shape[1] for t in tenants for b in here(dB, t)}
+
+    def fits(self, adapters: AdapterTable, d: int, F: int) -> bool:
+        """Is every gradient of sites 4 and 5 of the extents of its matrix?"""
+        return (self.n_tenants == adapters.n_tenants and self.inputs <= {d} and self.columns <= {F}
+                and all(mine <= {r} for mine, r in zip(self.ranks, adapters.ranks)))
+
     @staticmethod
     def from_tensors(dA: Sequence[Sequence[Optional[torch.Tensor]]], dB: Sequence[Sequence[Optional[torch.Tensor]]]) -> "GradientTable":
         """dA[t][m], dB[t][m] as the matrices of AdapterTable, or None where no gradient is wanted."""
@@ -398,8 +430,6 @@ class GradientTable:
             raise ValueError("no gradient wanted: pass grads=None")
         if any(g.dtype != every[0].dtype for g in every):
             raise TypeError("gradients must share a dtype")
-        if len({g.data_ptr() for g in every if g.numel()}) != sum(g.numel() > 0 for g in every):
-            raise ValueError("two gradients in one place")
         ptrs = lambda rows: torch.tensor([_dev(g) or 0 for row in rows for g in row], dtype=torch.int64, device=every[0].device)
         return GradientTable(ptrs(dA), ptrs(dB), len(dA), every[0].dtype, (dA, dB))
 
@@ -415,7 +445,7 @@ def milora_gated_linear_backward(dY: torch.Tensor, X: torch.Tensor, gate: torch.
     """Gradients behind milora_gated_linear, whose gate_out and up_out are gate and up: returns dX (None without want_dx) and
     overwrites the LoRA gradients of sites 4 and 5 that `grads` names."""
     B = tenant_id.numel()
-    M, d, F = _gated_sizes(X, W_gate, W_up, w_layout, F, row_to_req, route, B)
+    M, d, F = _gated_sizes(X, W_gate, W_up, adapters, w_layout, F, row_to_req, route, B)
     if dX is None and want_dx:
         dX = torch.empty_like(X)
     if not want_dx:
@@ -423,8 +453,8 @@ def milora_gated_linear_backward(dY: torch.Tensor, X: torch.Tensor, gate: torch.
     for t, what in ((dY, "dY"), (gate, "gate"), (up, "up")):
         _shaped(t, (M, F), what)
     _shaped(dX, (M, d), "dX")
-    if grads is not None and (grads.n_tenants != adapters.n_tenants or grads.dtype != X.dtype):
-        raise ValueError("gradients must cover the adapters' tenants in the dtype of X")
+    if grads is not None and (grads.dtype != X.dtype or not grads.fits(adapters, d, F)):
+        raise ValueError("gradients must be those of the adapters' tenants, dA [d, r_t] and dB [r_t, F], in the dtype of X")
     if workspace is None:
         workspace = _workspace(gated_linear_backward_workspace_bytes(M, d, F, X.dtype, w_layout, adapters.r_max), X.device)
     ad = adapters.c_struct()

@@ -74,6 +74,49 @@ def test_gradient_table_refusals():
         mb.GradientTable.from_tensors([[torch.zeros(2)] + [None] * 6], [[None] * 7])  # host memory
 
 
+def _host_tables(dA, dB, ranks=(4, 6), d=64, F=96):
+    """Tables over host memory: what the binding reads of them before any device work."""
+    z = torch.zeros(7 * len(ranks), dtype=torch.int64)
+    A, B = [[torch.zeros(d, r)] * 7 for r in ranks], [[torch.zeros(r, F)] * 7 for r in ranks]
+    return mb.AdapterTable(torch.tensor(ranks, dtype=torch.int32), z, z, max(ranks), len(ranks), (A, B)), mb.GradientTable(z, z, len(dA), torch.float32, (dA, dB))
+
+
+def test_gradients_have_the_extents_of_their_matrices():
+    """A buffer that is smaller than its matrix would be written past its end."""
+    row = lambda **kw: [kw.get(f"s{s}") for s in range(7)]
+    z = torch.zeros
+    fits = lambda dA, dB: (lambda tabs: tabs[1].fits(tabs[0], 64, 96))(_host_tables(dA, dB))
+    assert fits([row(s4=z(64, 4)), row(s5=z(64, 6))], [row(s5=z(4, 96)), row()])
+    assert fits([row(), row(s4=z(64, 6), s0=z(1, 1))], [row(), row()])  # other sites' are not written
+    for a, b in ((z(64, 3), None), (z(63, 4), None), (None, z(4, 95)), (None, z(3, 96)), (z(4, 96), z(64, 4)), (z(64, 6), None), (None, z(6, 96))):
+        for s in ("s4", "s5"):
+            assert not fits([row(**{s: a}), row()], [row(**{s: b}), row()])
+    assert not fits([row(s4=z(64, 4))], [row()])  # a tenant short
+    with pytest.raises(ValueError, match="dA must be"):
+        _host_tables([row(s4=z(256)), row()], [row(), row()])
+    x, w, ids = z(8, 64), z(96, 64), (z(2, dtype=torch.int32), z(2, dtype=torch.uint8))
+    tab, short = _host_tables([row(s4=z(64, 2)), row()], [row(), row()])
+    m, r2r = z(8, 96), z(8, dtype=torch.int32)
+    with pytest.raises(ValueError, match="gradients must be those"):
+        mb.milora_gated_linear_backward(m, x, m, m, w, w, tab, *ids, row_to_req=r2r, grads=short)
+    narrow, _ = _host_tables([row(), row()], [row(), row()], F=95)
+    for call in (lambda: mb.milora_gated_linear(x, w, w, narrow, *ids, row_to_req=r2r),
+                 lambda: mb.milora_gated_linear_backward(m, x, m, m, w, w, narrow, *ids, row_to_req=r2r)):
+        with pytest.raises(ValueError, match="adapter matrices"):
+            call()
+
+
+def test_gradients_may_not_overlap():
+    room = torch.zeros(64 * 8 + 64 * 8)
+    row = lambda v: [None] * 4 + [v, None, None]
+    at = lambda k: room[k:k + 64 * 4].reshape(64, 4)
+    _host_tables([row(at(0)), row(None)], [[None] * 7] * 2)
+    _host_tables([row(at(0)), row(at(256))], [[None] * 7] * 2, ranks=(4, 4))  # one behind the other
+    for k in (0, 1, 255):
+        with pytest.raises(ValueError, match="one place"):
+            _host_tables([row(at(k)), row(at(256 if k else 0))], [[None] * 7] * 2, ranks=(4, 4))
+
+
 def test_plain_gradients_against_differences():
     """The formulas of the oracle against central differences in 64 bits (step 1e-6: error about 1e-9 relative)."""
     g = torch.Generator().manual_seed(2)
