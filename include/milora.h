@@ -175,7 +175,8 @@ int milora_route(const void *H, int64_t M_tok, int d, int dtype, const int32_t *
  *               bf16 is part of it; what it holds before a call does not matter); the sizes never go down when an
  *               argument goes up, so one workspace sized for the largest call serves every smaller one
  * A row whose request index, tenant id or tenant rank is out of range gets the base term only.
- * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK; 4-bit layout with d1 >= 2^30), EUNSUPPORTED (packed or 4-bit layout with fp32, with
+ * Errors: EINVAL, ERANGE (r_max > MILORA_MAX_RANK; 4-bit layout with d1 >= 2^30 or sizes beyond a launch:
+ * millions of columns or inputs), EUNSUPPORTED (packed or 4-bit layout with fp32, with
  * d1 % 32 != 0 or d2 % 16 != 0, or with X, W, bias or Y not 16-byte aligned), EWORKSPACE, EHIP.
  */
 size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max);
@@ -278,8 +279,8 @@ int milora_gated_linear_backward(const void *dY, const void *X, const float *gat
  *   workspace device, milora_layer_decode_workspace_bytes(B, d, F, r_max) bytes (packed weights and B > 32:
  *             this includes the tables of fp32 partial tiles of the wide-batch kernel, tens of MB); never fewer when an
  *             argument goes up
- * Errors: EINVAL, ERANGE (B > MILORA_MAX_DECODE_BATCH, r_max > MILORA_MAX_RANK), EUNSUPPORTED
- * (packed or 4-bit layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
+ * Errors: EINVAL, ERANGE (B > MILORA_MAX_DECODE_BATCH, r_max > MILORA_MAX_RANK; 4-bit layout with d or F >= 2^30 or sizes beyond
+ * a launch), EUNSUPPORTED (packed or 4-bit layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
  * weight not 16-byte aligned), EWORKSPACE, EHIP.
  * MILORA_W_MX4: eight launches; the outputs of o, gate, up and down stay in fp32 up to the glue's rounding, and n(u) W is formed as
  * (u W) / sqrt(mean(u^2) + 1e-5), u rounded to bf16 in the place of n(u) (up to 8 requests the gate and up projections take h as the sum of two bf16 values).  No wait inside a launch, and what the workspace holds before a

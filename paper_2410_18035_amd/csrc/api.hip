@@ -404,6 +404,16 @@ bool mx4_linear_direct(int64_t M, int d1, int d2, const LinearPlan& pl) {
   return plan_tiles(M, d1, d2, false, true, false, kCutMx4).time <= other + write_out_time(d1, d2);
 }
 
+// Is there a kernel for these sizes?  Not where only the weight-streaming kernel would be left for the weight written out (packed, reductions too long
+// or columns too many for the tiles): its hand-over words have to be zero before their first use, which a workspace of any contents does not
+// promise.  Nor where the rows of one large tile are beyond the offsets.
+bool mx4_linear_fits(int64_t M, int d1, int d2) {
+  if (mx4_few_rows(M, d1, d2)) return mx4_rows_fit(M, d1, d2, 1);
+  const void* aligned = (const void*)(uintptr_t)256;
+  const LinearPlan pl = plan_linear(M, d1, d2, MILORA_BF16, !mx4_rowmajor(d1), aligned, aligned, aligned);
+  return mx4_linear_direct(M, d1, d2, pl) || (pl.kind != MILORA_KERNEL_STREAM && !(pl.large && !pl.small && (uint64_t)d1 * 512u >= (1ull << 32)));
+}
+
 int run_linear_mx4(const bf16_t* X, int64_t M, int d1, int d2, const int32_t* row_to_req, const void* W, const bf16_t* bias,
                    const AdapterView& ad, int site, const int32_t* tenant_id, const uint8_t* route, int B, bf16_t* Y, void* workspace,
                    hipStream_t st) {
@@ -484,6 +494,7 @@ extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype,
   if (!valid_layout(w_layout)) return MILORA_EINVAL;
   if (w_layout != MILORA_W_ROWMAJOR) {
     if (dtype != MILORA_BF16 || !packed_shape_ok(d1, d2)) return MILORA_EUNSUPPORTED;
+    if (w_layout == MILORA_W_MX4 && (d1 > 0x3fffffff || M > 0x7fffffffLL || !mx4_linear_fits(M, d1, d2))) return MILORA_ERANGE;
     if (w_layout == MILORA_W_PACKED || mx4_few_rows(M, d1, d2)) return MILORA_KERNEL_STREAM;
     return MILORA_KERNEL_TILES;
   }
@@ -530,6 +541,7 @@ extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, in
       return MILORA_EUNSUPPORTED;
     if (packed && !row_to_req && M > MILORA_MAX_DECODE_BATCH) return MILORA_ERANGE;
   }
+  if (mx4 && !mx4_linear_fits(M, d1, d2)) return MILORA_ERANGE;
   if (mx4)
     return run_linear_mx4((const bf16_t*)X, M, d1, d2, row_to_req, W, (const bf16_t*)bias, ad, site, tenant_id, route, B, (bf16_t*)Y,
                           workspace, st);
@@ -631,6 +643,7 @@ static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, cons
     if (weights->layout == MILORA_W_MX4) {
       if (marks) return MILORA_EUNSUPPORTED;
       if (d > 0x3fffffff || F > 0x3fffffff) return MILORA_ERANGE;
+      if (!mx4_rows_fit(B, d, d, 3) || !mx4_rows_fit(B, d, d, 1) || !mx4_rows_fit(B, d, F, 2, B <= kMxSecond) || !mx4_rows_fit(B, F, d, 1)) return MILORA_ERANGE;
       return layer_decode_mx4((const bf16_t*)x, B, d, F, weights, ad, tenant_id, route, flags, (const bf16_t*)attn_out, (bf16_t*)y,
                               (bf16_t*)qkv_out, workspace, st);
     }

@@ -60,6 +60,8 @@ inline bool mx4_few_rows(int64_t M, int d1, int64_t columns) {
   return M <= kMxAlwaysFew || (M <= kMxMostFew && (double)M * d1 * columns <= 24e9);
 }
 size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites);
+// Does a launch take these sizes?
+bool mx4_rows_fit(int64_t M, int d1, int d2, int sites, bool second = false);
 // gated: sites = 2
 int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st);
 

@@ -557,7 +557,6 @@ int launch_base(const MxBase& b, hipStream_t st) {
     lds_set_for = dev;
   }
   const int64_t total = (int64_t)b.sites * b.col_groups * b.row_split * b.parts, grid = b.shrink_z + (total + 7) / 8 * 8;
-  if (grid > 1 << 22) return MILORA_ERANGE;  // (a grid has to stay below 2^32 threads)
   hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE, XM>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
   return check_launch();
 }
@@ -579,6 +578,26 @@ size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
   return (size_t)M * d2 * sites * ((d1 + part - 1) / part);
 }
 int mx4_shrink_parts(int d1) { return (d1 + kMxShrinkK - 1) / kMxShrinkK; }
+
+struct MxCut {
+  int kw;     // waves that share columns
+  bool half;  // parts of half the length
+  int parts, col_groups, row_groups, row_split;
+};
+// rows: of X, the second ones among them
+MxCut mx4_cut(int64_t rows, int d1, int d2, int sites) {
+  MxCut c;
+  c.kw = mx4_waves(rows);
+  c.half = mx4_short(rows, d1, d2, sites);
+  const int part = c.kw * kMxSteps * 64 / (c.half ? 2 : 1);
+  c.parts = (d1 + part - 1) / part;
+  c.col_groups = (d2 + kMxCols / c.kw - 1) / (kMxCols / c.kw);
+  // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
+  c.row_groups = (int)((rows + 31) / 32);
+  const int64_t units = (int64_t)sites * c.col_groups * c.parts;
+  c.row_split = (int)(512 / units < 1 ? 1 : 512 / units < c.row_groups ? 512 / units : c.row_groups);
+  return c;
+}
 
 // Groups of eight of one launch: a grid has to stay below 2^32 threads.
 constexpr int64_t kQuantSlice = (int64_t)1 << 30;
@@ -630,8 +649,13 @@ size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites)
          align_up(mx4_partial_floats(M, d1, d2, sites) * sizeof(float), 256);
 }
 
+bool mx4_rows_fit(int64_t M, int d1, int d2, int sites, bool second) {
+  const MxCut c = mx4_cut(second ? 2 * M : M, d1, d2, sites);
+  const int64_t shrinks = M * sites * mx4_shrink_parts(d1), tiles = (int64_t)sites * c.col_groups * c.row_split * c.parts;
+  return shrinks + tiles <= ((int64_t)1 << 22) - 16;  // (a grid has to stay below 2^32 threads)
+}
+
 int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hipStream_t st) {
-  if (g.M > 65535) return MILORA_ERANGE;
   const int r_max = g.ad.r_max, t_parts = mx4_shrink_parts(g.d1);
   float* const t = (float*)workspace;
   MxTerm* const terms = (MxTerm*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
@@ -641,21 +665,16 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.X = g.X; b.ldx = g.ldx; b.M = rows; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
   b.sites = sites;
-  const int kw = mx4_waves(rows);
-  const bool half = mx4_short(rows, g.d1, g.d2, sites);
-  const int part = kw * kMxSteps * 64 / (half ? 2 : 1);
-  b.parts = (g.d1 + part - 1) / part;
+  const MxCut cut = mx4_cut(rows, g.d1, g.d2, sites);
+  const int kw = cut.kw;
+  const bool half = cut.half;
+  b.parts = cut.parts; b.col_groups = cut.col_groups; b.row_groups = cut.row_groups; b.row_split = cut.row_split;
   b.partial = partial;
   b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, nullptr, nullptr,
                         sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
   b.terms = terms;
   b.shrink_parts = t_parts;
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
-  b.col_groups = (g.d2 + kMxCols / kw - 1) / (kMxCols / kw);
-  // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
-  b.row_groups = (rows + 31) / 32;
-  const int64_t units = (int64_t)sites * b.col_groups * b.parts;
-  b.row_split = (int)(512 / units < 1 ? 1 : 512 / units < b.row_groups ? 512 / units : b.row_groups);
   const int rc = rows <= 2             ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
                  : kw == 8 && half    ? launch_base<8, kMxSteps / 2, false, 4>(b, st)
                  : kw == 8 && rows <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)

@@ -83,6 +83,32 @@ def test_kernel_family_and_workspace():
     assert size(0, 32, 16, 1) == 0 and size(4, 32, 16, 0) == 0
 
 
+def test_sizes_beyond_a_launch_are_refused_before_any_work():
+    """What would be left for these is a kernel whose hand-over words a workspace of any contents does not hold, or no launch at all."""
+    L, n, p = mb.lib(), ctypes.c_void_p(None), ctypes.c_void_p(0x1000)
+    ad = mb._Adapters(1, 8, 0x1000, 0x1000, 0x1000)
+    k, t = mb.milora_routed_linear_kernel, mb.milora_routed_linear_tile
+    lin = lambda M, d1, d2: L.milora_routed_linear(p, M, d1, d2, 0, p, p, 2, n, ctypes.byref(ad), 0, p, p, 1, p, p, 1 << 60, n)
+    for M, d1, d2 in [(600, 8388640, 16), (4096, 96, 4200000), (1, 32, 1 << 28), (128, 1 << 26, 16), (600, 8388608, 16)]:
+        assert lin(M, d1, d2) == -2, (M, d1, d2)
+        assert k(M, d1, d2, torch.bfloat16, mb.W_MX4) == -2 and t(M, d1, d2, torch.bfloat16, mb.W_MX4) == -2
+    assert k(4, 1 << 30, 16, torch.bfloat16, mb.W_MX4) == -2
+    for M, d1, d2 in [(600, 8388512, 16), (4000, 96, 4190000), (1, 32, 1 << 26), (700, 48 * 2, 528)]:  # the last ones that fit keep their kernels
+        assert k(M, d1, d2, torch.bfloat16, mb.W_MX4) == (mb.KERNEL_STREAM if M == 1 else mb.KERNEL_TILES)
+        assert t(M, d1, d2, torch.bfloat16, mb.W_MX4) == 0 if M == 1 else t(M, d1, d2, torch.bfloat16, mb.W_MX4) in (64, 128)
+    # whatever a call is told about its kernel, it is never the streaming one on a weight written out
+    for M in (129, 513, 600, 4096, 5000, 100000):
+        for d1 in (32, 96, 4128, 8388576, 8388640):
+            for d2 in (16, 4096, 4194304, 4200000):
+                if k(M, d1, d2, torch.bfloat16, mb.W_MX4) == mb.KERNEL_TILES:
+                    assert t(M, d1, d2, torch.bfloat16, mb.W_MX4) in (64, 128)
+    lw = mb._LayerWeights()
+    for m in range(7):
+        lw.W[m] = 0x1000
+    lw.layout = 2
+    assert L.milora_layer_decode(p, 1, 32, 1 << 29, 0, ctypes.byref(lw), ctypes.byref(ad), p, p, 0, n, p, n, p, 1 << 60, n) == -2
+
+
 def test_binding_checks_quantised_weights():
     with pytest.raises(ValueError):
         mb._check_weight(torch.zeros(16, dtype=torch.uint8), 32, 1, mb.W_MX4, torch.bfloat16)
