@@ -118,6 +118,7 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
   const int64_t M = g.M;
   int rc;
   if (g.mx4 && mx4_few_rows(M, g.d, 2 * (int64_t)g.F)) {
+    if (!mx4_rows_fit(M, g.d, g.F, 2)) return MILORA_ERANGE;
     MxArgs a{};
     a.X = (const bf16_t*)g.X; a.ldx = g.d; a.M = (int)M; a.d1 = g.d; a.d2 = g.F;
     a.W[0] = (const unsigned char*)g.Wg; a.W[1] = (const unsigned char*)g.Wu; a.Y[0] = (bf16_t*)Y; a.ldy = g.F;
@@ -129,7 +130,8 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
   const void* const like = g.mx4 ? (const void*)(uintptr_t)256 : nullptr;  // (in the workspace: aligned)
   const void *Wg = like ? like : g.Wg, *Wu = like ? like : g.Wu;
   const bool small = g.dtype == MILORA_BF16 && g.F < 1 << 30 && tiles_supported(M, g.d, 2 * g.F, packed, g.X, Wg, Y) && aligned16(Wu) && g.F % 16 == 0;
-  const bool large = g.dtype == MILORA_BF16 && !packed && M <= kHalvesRows && prefill_supported(M, g.d, g.F, g.X, Wg, Y) && aligned16(Wu);
+  const bool large = g.dtype == MILORA_BF16 && !packed && M <= kHalvesRows && (uint64_t)g.d * 512u < (1ull << 32) &&  // (offsets of a tile's 256 rows)
+                     prefill_supported(M, g.d, g.F, g.X, Wg, Y) && aligned16(Wu);
   if (small || large) {
     Carver c{(char*)workspace};
     char* const ctrl = c.take<char>(kStreamCtrlBytes);
@@ -187,7 +189,7 @@ int run_gated(const GatedCall& g, void* Y, float* gate_out, float* up_out, void*
     return rc;
   }
   // any shape and type
-  if (g.mx4) return MILORA_EUNSUPPORTED;
+  if (g.mx4) return MILORA_ERANGE;
   return launch_gated_generic(g.X, M, g.d, g.F, g.dtype, g.row_to_req, g.Wg, g.Wu, g.ad, kGate, g.tenant_id, g.route, g.B, (float*)workspace, Y,
                               gate_out, up_out, st);
 }
@@ -772,7 +774,6 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
                  hipStream_t st) {
   const int64_t M = g.M;
   const int tenants = g.ad.n_tenants;
-  if ((M + 63) / 64 > 65535 || tenants > 32767) return MILORA_ERANGE;
   int rc = launch_dz<T>(dY, gate, up, M, g.F, w.dz, st);
   if (rc) return rc;
   hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((M + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, M, g.row_to_req, g.ad, g.tenant_id,
@@ -872,7 +873,8 @@ int run_gated_backward(const GatedCall& g, const void* dY, const float* gate, co
   const BackWs w = carve_back(workspace, g.M, g.d, g.F, g.dtype, g.mx4, g.ad.r_max);
   const bf16_t* const Wg = g.mx4 ? (const bf16_t*)w.W : (const bf16_t*)g.Wg;
   const bf16_t* const Wu = g.mx4 ? Wg + (size_t)g.d * g.F : (const bf16_t*)g.Wu;
-  const bool tiles = g.dtype == MILORA_BF16 && g.d % 32 == 0 && aligned16(g.X) && g.M <= (int64_t)65535 * 64 && g.ad.n_tenants <= 32767 &&
+  if (g.M > (int64_t)65535 * 64 || g.ad.n_tenants > 32767) return MILORA_ERANGE;
+  const bool tiles = g.dtype == MILORA_BF16 && g.d % 32 == 0 && aligned16(g.X) &&
                      back_supported(g.M, g.d, g.F, w.dz, Wg, Wu, dX);
   if (g.mx4 && dX && !(tiles && direct_back(g))) {
     int rc = mx4_dequantize(g.Wg, w.W, MILORA_BF16, g.d, g.F, false, st);

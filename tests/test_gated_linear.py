@@ -53,6 +53,20 @@ def test_refusals():
     assert L.milora_gated_linear_backward(p, p, p, p, 4, 64, 64, 0, p, p, p, 0, ctypes.byref(many), p, p, 2, p, None, p, big, n) == -2
 
 
+def test_sizes_beyond_a_launch_are_refused_before_any_work():
+    """On a machine without a GPU anything that is enqueued comes back as a failed HIP call."""
+    L, n, p, huge = mb.lib(), ctypes.c_void_p(None), ctypes.c_void_p(0x1000), 1 << 60
+    ad, many = (mb._Adapters(t, 8, 0x1000, 0x1000, 0x1000) for t in (1, 32768))
+    fwd = lambda M, d, F, lay, dt=0: L.milora_gated_linear(p, M, d, F, dt, p, p, p, lay, ctypes.byref(ad), p, p, 2, p, n, n, p, huge, n)
+    bwd = lambda M, d, F, lay, dt=0, a=ad: L.milora_gated_linear_backward(p, p, p, p, M, d, F, dt, p, p, p, lay, ctypes.byref(a), p, p, 2, p, None, p, huge, n)
+    assert fwd(4096, 32, 1 << 21, 2) == -2 and fwd(600, 8388640, 16, 2) == -2 and fwd(600, 8388608, 16, 2) == -2
+    assert fwd(1, 32, 1 << 28, 2) == -2 and fwd(128, 1 << 26, 16, 2) == -2
+    for lay, dt in ((0, 0), (0, 1), (2, 0)):
+        assert bwd(4194241, 32, 32, lay, dt) == -2
+        assert bwd(4, 32, 32, lay, dt, many) == -2
+    assert fwd(4194241, 1, 1, 0, 1) == -2
+
+
 def test_workspaces_never_shrink():
     rows = [1, 16, 17, 64, 100, 128, 129, 300, 1000, 4096, 4097, 8192, 20000]
     for size in (mb.gated_linear_workspace_bytes, mb.gated_linear_backward_workspace_bytes):
