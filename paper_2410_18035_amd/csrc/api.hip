@@ -481,12 +481,12 @@ extern "C" size_t milora_routed_linear_workspace_bytes(int64_t M, int d1, int d2
 extern "C" size_t milora_quantized_linear_workspace_bytes(int64_t M, int d1, int d2, int r_max) {
   if (M < 1 || d1 < 1 || d2 < 1 || d1 > 0x3fffffff || r_max < 1) return 0;
   const size_t few = mx4_rows_workspace_bytes(M < kMxMostFew ? M : kMxMostFew, d1, d2, r_max, 1);
-  if (M <= kMxAlwaysFew) return few;
+  if (M <= kMxAlwaysFew) return kStreamCtrlBytes + few;
   const size_t many = align_up((size_t)d1 * d2 * 2, 256) + milora_routed_linear_workspace_bytes(M, d1, d2, r_max);
   const size_t direct = kStreamCtrlBytes + cut_bytes_bound(M, d2) + align_up(shrink_rows_bound(M, d1) * r_max * sizeof(float), 256) + align_up((size_t)M * sizeof(int2), 256) +
                         align_up(halves_of(nullptr, M, r_max).site * sizeof(bf16_t), 256);
   const size_t most = many > direct ? many : direct;
-  return most > few ? most : few;
+  return kStreamCtrlBytes + (most > few ? most : few);  // (behind the words of the stream kernels: packed and 4-bit weights in turn)
 }
 
 extern "C" int milora_routed_linear_kernel(int64_t M, int d1, int d2, int dtype, int w_layout) {
@@ -544,7 +544,7 @@ extern "C" int milora_routed_linear(const void* X, int64_t M, int d1, int d2, in
   if (mx4 && !mx4_linear_fits(M, d1, d2)) return MILORA_ERANGE;
   if (mx4)
     return run_linear_mx4((const bf16_t*)X, M, d1, d2, row_to_req, W, (const bf16_t*)bias, ad, site, tenant_id, route, B, (bf16_t*)Y,
-                          workspace, st);
+                          (char*)workspace + kStreamCtrlBytes, st);
   return run_linear(X, M, d1, d2, dtype, row_to_req, W, packed, bias, ad, site, tenant_id, route, B, Y, workspace, st);
 }
 

@@ -48,7 +48,7 @@ inline size_t cut_bytes_bound(int64_t M, int64_t columns) {
 
 // The first bytes of a routed linear's workspace belong to control words: those of the stream kernels (decode.hip), then the
 // part counters of the tile kernel, zeroed by the shrink launch in front of it.  Both keep their data behind them, so calls of
-// any sizes and either layout can follow one another on one workspace, and the status word can be asked for after either.
+// any sizes and any layout can follow one another on one workspace (those of 4-bit weights leave all of it alone), and the status word can be asked for after either.
 constexpr int kStreamCtrlBytes = 16384;
 constexpr int kTileCtrlBytes = kMaxSplitUnits * (int)sizeof(int);
 constexpr int kTileCtrlOffset = kStreamCtrlBytes - kTileCtrlBytes;

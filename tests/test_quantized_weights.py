@@ -312,6 +312,29 @@ def test_linear_skips_foreign_ids():
 
 
 @gpu
+def test_packed_and_quantised_calls_share_a_workspace():
+    """The stream kernel's hand-over words stay as they are over calls on 4-bit weights of every kind."""
+    M, d1, d2, site = 8, 128, 64, 2
+    c = plain.Case(M, 4, 2, {site: (d1, d2)}, (8, 16), 91, DEV, rows="mixed", sites=[site])
+    x, w = c.rnd(M, d1), c.rnd(d2, d1)
+    wp, (tid, route), r2r = mb.milora_pack_weight(w), c.requests(), c.rows()
+    others = [(3, 96, 48), (129, 96, 48), (700, 96, 528), (1100, 512, 1040), (2100, 640, 4112)]
+    need = [mb.routed_linear_workspace_bytes(M, d1, d2, 16)] + [mb.quantized_linear_workspace_bytes(m, a, b, 16) for m, a, b in others]
+    ws = torch.zeros(max(need), dtype=torch.uint8, device=DEV)
+    packed = lambda: mb.milora_routed_linear(x, wp, c.tab, site, tid, route, row_to_req=r2r, w_layout=mb.W_PACKED, d2=d2, workspace=ws)
+    first = packed()
+    words = ws[:16384].clone()
+    for m, a, b in others:
+        o = plain.Case(m, 4, 2, {site: (a, b)}, (8, 16), m, DEV, rows="mixed", sites=[site])
+        xo, q, ids = o.rnd(m, a), mb.milora_quantize_weight(o.rnd(b, a, s=a ** -0.5)), o.requests()
+        Y = mb.milora_routed_linear(xo, q, o.tab, site, *ids, row_to_req=o.rows(), w_layout=mb.W_MX4, d2=b, workspace=ws)
+        _assert_linear(Y, xo, plain.dequantize(q, a, b), o, site)
+        assert torch.equal(ws[:16384], words), (m, a, b)
+    assert torch.equal(packed(), first)
+    assert mb.milora_packed_workspace_status(ws) == 0
+
+
+@gpu
 @pytest.mark.parametrize("M", [3, 64, 200])
 def test_linear_in_a_graph_and_on_another_stream(M):
     d1, d2, site = 256, 96, 5
