@@ -390,3 +390,62 @@ def test_layer_decode(B, d, F, ranks, norm, attn):
     again, _ = mb.milora_layer_decode(x, q, tab, tid.to(DEV), route.to(DEV), F, w_layout=mb.W_MX4, rmsnorm=norm, attn_out=a, want_qkv=False,
                                       y=x, workspace=ws)  # y may alias x
     assert torch.equal(again, y)
+
+
+@gpu
+@pytest.mark.parametrize("B,d,F", [(1, 2080, 1056), (3, 4128, 352), (8, 2080, 352), (8, 4128, 1056), (9, 4128, 352), (1, 4128, 96), (33, 2080, 352)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_layer_decode_of_real_width(B, d, F, norm):
+    """Several parts of every level's reduction, several trips of the sums of squares."""
+    test_layer_decode(B, d, F, (8, 20), norm, B == 8)
+
+
+def _remainder_layer(B, d, F, seed, sites):
+    """A layer whose gate and up projections see only what bf16 cannot hold of h: h is 1 + e with |e| < 2^-9, and inputs 2 k and 2 k + 1 have
+    opposite weights (in the adapters too), so that all ones cancel, exactly in the base weights, whose values are small multiples of a power
+    of two."""
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    pairs = lambda w: torch.stack([w, -w], -1).reshape(w.shape[0], -1)
+    W = [rnd(d, d) * 0.02 for _ in range(4)] + [pairs(rnd(F, d // 2)) * 64 for _ in range(2)] + [rnd(d, F)]
+    q = [mb.milora_quantize_weight(w.to(DEV)) for w in W]
+    W = [mb.milora_dequantize_weight(v, *synth.site_dims(m, d, F), torch.float32).double() for m, v in enumerate(q)]
+    x = torch.ones(B, d, dtype=torch.bfloat16, device=DEV)
+    a = rnd(B, d).to(torch.bfloat16).to(DEV)
+    a = (a.double() * 2.0 ** torch.floor(torch.log2(2.0 ** -9 / (a.double() @ W[3].t()).abs().max())).item()).to(torch.bfloat16)
+    r, T = 8, 2
+    A = [[(pairs(rnd(r, d // 2)).t() * 64 if m in (4, 5) else rnd(synth.site_dims(m, d, F)[0], r)).contiguous().to(torch.bfloat16).to(DEV) for m in range(7)]
+         for _ in range(T)]
+    Bm = [[(rnd(r, synth.site_dims(m, d, F)[1]) * 0.5).to(torch.bfloat16).to(DEV) for m in range(7)] for _ in range(T)]
+    tid = torch.arange(B) % T
+    route = torch.full((B,), 0x80 | sum(1 << s for s in sites) if sites else mb.ROUTE_NONE, dtype=torch.uint8)
+    return q, W, x, a, A, Bm, tid.to(torch.int32).to(DEV), route.to(DEV)
+
+
+def _remainder_step(B, d, F, norm, sites):
+    q, W, x, a, A, Bm, tid, route = _remainder_layer(B, d, F, B + d, sites)
+    tab = mb.AdapterTable.from_tensors(A, Bm, [8] * len(A))
+    ws = torch.full((mb.layer_decode_workspace_bytes(B, d, F, 8),), 255, dtype=torch.uint8, device=DEV)
+    y, _ = mb.milora_layer_decode(x, q, tab, tid, route, F, w_layout=mb.W_MX4, rmsnorm=norm, attn_out=a, want_qkv=False, workspace=ws)
+    e = a.double() @ W[3].t()
+    assert e.abs().max() <= 2.0 ** -9
+    h = 1 + e
+    n = h / torch.sqrt(h.square().mean(1, keepdim=True) + 1e-5) if norm else h
+    z = []
+    for s in (4, 5):
+        term = torch.stack([(n[b] @ A[int(tid[b])][s].double()) @ Bm[int(tid[b])][s].double() for b in range(B)])
+        z.append(n @ W[s].t() + (term if s in sites else 0.0))
+    ref = h + plain.gated(*z) @ W[6].t()
+    # Independent roundings, each uniform and at most 2^-8 of its value, 2^-8 / sqrt(3) = 2.26e-3 of a norm: the second row of h in g (silu's
+    # logarithmic slope: up to 2) and in u, m, y: sqrt(4 + 1 + 1 + 1) 2.26e-3 = 6e-3, 7e-3 with the sums.  Without the second rows z is
+    # zero and y is h, at least a tenth of the norm away: that shows.
+    assert (ref - h).norm() > 0.1 * ref.norm()
+    far = (y.double() - ref).norm(dim=1) / ref.norm(dim=1)
+    assert far.max() <= 7e-3, far.tolist()
+
+
+@gpu
+@pytest.mark.parametrize("B,d,F", [(1, 128, 96), (1, 4128, 352), (3, 2080, 352), (4, 4128, 1056), (8, 4128, 352), (8, 4128, 3104)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_layer_decode_takes_h_beyond_its_first_bf16(B, d, F, norm):
+    _remainder_step(B, d, F, norm, ())
