@@ -31,7 +31,7 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
 struct MxArgs {
   const bf16_t* X;  // M rows of ldx elements
   int64_t ldx;
-  bool second;      // behind them M rows with what their rounding left, which the products take in as well (the shrinks do not)
+  bool second;      // behind them M rows with what their rounding left, which the products take in as well
   int M, d1, d2;
   const unsigned char* W[3];  // of the sites; gated: W[0] gate, W[1] up
   const bf16_t* bias;

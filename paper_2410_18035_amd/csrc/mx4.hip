@@ -149,6 +149,7 @@ struct MxBase {
   float* partial;  // [site][part][M][d2]
   int shrink_parts, shrink_z;  // the shrink: parts of a row, workgroups in all (a multiple of 8)
   ShrinkArgs shrink;
+  const bf16_t* second;  // second rows of the shrink's X, or null
   MxTerm* terms;  // [site][M]
 };
 
@@ -168,6 +169,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   if (r == 0) return;
   gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
   const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
+  const bf16_t* const x2 = g.second ? g.second + (size_t)m * sh.ldx : nullptr;
   // lane: eight ranks (piece) of every kpl-th input of the wave's 128
   const int pieces = (r + 7) >> 3;
   int p2 = 1;
@@ -188,6 +190,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
         if (left >= 8) a[u] = *(gu32x4_any*)q;
         else a[u] = load8(q, left, false);
         xv[u] = bf16_to_f32(x[kk]);
+        if (x2) xv[u] += bf16_to_f32(x2[kk]);  // (16 bits of h, exact in fp32)
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
@@ -672,6 +675,7 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.partial = partial;
   b.shrink = ShrinkArgs{g.X, g.ldx, g.M, 0, g.d1, g.site[0], g.B, g.row_to_req, g.tenant_id, g.route, g.ad, t, (size_t)g.M * r_max, nullptr, nullptr,
                         sites, (size_t)g.M * r_max * t_parts, (size_t)g.M, 0};
+  b.second = g.second ? g.X + (size_t)g.M * g.ldx : nullptr;
   b.terms = terms;
   b.shrink_parts = t_parts;
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;

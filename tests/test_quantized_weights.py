@@ -449,3 +449,10 @@ def _remainder_step(B, d, F, norm, sites):
 @pytest.mark.parametrize("norm", [False, True])
 def test_layer_decode_takes_h_beyond_its_first_bf16(B, d, F, norm):
     _remainder_step(B, d, F, norm, ())
+
+
+@gpu
+@pytest.mark.parametrize("B,d,F,sites", [(1, 4128, 352, (4,)), (3, 2080, 352, (5,)), (8, 4128, 1056, (4, 5)), (5, 1056, 352, (4, 5))])
+@pytest.mark.parametrize("norm", [False, True])
+def test_low_rank_terms_take_h_beyond_its_first_bf16(B, d, F, sites, norm):
+    _remainder_step(B, d, F, norm, sites)
