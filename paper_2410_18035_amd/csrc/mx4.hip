@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
     u32x2_a8 left;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      left[e] = pack_bf16x2(y[2 * e] - __uint_as_float(o[e] << 16), y[2 * e + 1] - __uint_as_float(o[e] & 0xffff0000u));
+      left[e] = pack_bf16x2(rest_of(y[2 * e], __uint_as_float(o[e] << 16)), rest_of(y[2 * e + 1], __uint_as_float(o[e] & 0xffff0000u)));
     *reinterpret_cast<u32x2_a8*>(g.left_out + at) = left;
   }
 }

@@ -456,3 +456,26 @@ def test_layer_decode_takes_h_beyond_its_first_bf16(B, d, F, norm):
 @pytest.mark.parametrize("norm", [False, True])
 def test_low_rank_terms_take_h_beyond_its_first_bf16(B, d, F, sites, norm):
     _remainder_step(B, d, F, norm, sites)
+
+
+@gpu
+@pytest.mark.parametrize("B", [2, 8, 9])
+def test_an_infinite_input_stays_infinite_through_a_step(B):
+    """h + Inf W is Inf where the weights say so: request 1 has an Inf, all weights it meets are positive."""
+    d, F = 128, 96
+    g = torch.Generator().manual_seed(B)
+    W = [torch.rand(*synth.site_dims(m, d, F)[::-1], generator=g) + 0.5 for m in range(7)]
+    q = [mb.milora_quantize_weight(w.to(DEV)) for w in W]
+    A = [[torch.zeros(synth.site_dims(m, d, F)[0], 8, dtype=torch.bfloat16, device=DEV) for m in range(7)]]
+    Bm = [[torch.zeros(8, synth.site_dims(m, d, F)[1], dtype=torch.bfloat16, device=DEV) for m in range(7)]]
+    tab = mb.AdapterTable.from_tensors(A, Bm, [8])
+    x, a = (torch.rand(B, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    tid, route = torch.zeros(B, dtype=torch.int32, device=DEV), torch.full((B,), 255, dtype=torch.uint8, device=DEV)
+    run = lambda: mb.milora_layer_decode(x, q, tab, tid, route, F, w_layout=mb.W_MX4, attn_out=a)
+    clean, qkv = run()
+    assert torch.isfinite(clean).all()
+    x[1, 70] = float("inf")
+    y, qkv2 = run()
+    keep = torch.arange(B, device=DEV) != 1
+    assert torch.equal(y[keep], clean[keep]) and torch.equal(qkv2[keep], qkv[keep])
+    assert (y[1] == float("inf")).all() and (qkv2[1] == float("inf")).all()
