@@ -97,8 +97,9 @@ template <> struct Elem<bf16_t> {
   __device__ static __forceinline__ void store(bf16_t* p, size_t i, float v) { p[i] = f32_to_bf16(v); }
 };
 
+__device__ __forceinline__ bool finite_f32(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 // What the rounding of v to hi left: nothing where hi is Inf or NaN (Inf - Inf would make a NaN of an Inf).
-__device__ __forceinline__ float rest_of(float v, float hi) { return (__float_as_uint(hi) & 0x7f800000u) == 0x7f800000u ? 0.f : v - hi; }
+__device__ __forceinline__ float rest_of(float v, float hi) { return finite_f32(hi) ? v - hi : 0.f; }
 
 inline size_t dtype_size(int dtype) { return dtype == MILORA_BF16 ? 2 : 4; }
 

@@ -47,15 +47,17 @@ struct Carver {
 };
 
 // The scales of the ranks (X W^A, dz W^B^T: fp32, [site][part][M][r_max]) as two bf16 halves, about 17 of their bits: zero past the rank and for
-// rows without a term.  A row's 32 ranks by 32 lanes.
+// rows without a term.  A row's 32 ranks by 32 lanes.  An Inf or NaN is a high half by itself (its low half would be Inf - Inf); LATER: it becomes zero
+// and marks its row, whose products with it the tiles then form in fp32 (where zero columns stand beside those of the site, it would reach them).
 constexpr int kHalvesRowsWg = kThreads / 32;
 struct HalvesOf {
   const float* v;
   int parts;
   Halves out;
 };
-__global__ void __launch_bounds__(kThreads) gated_halves_kernel(HalvesOf first, HalvesOf second, size_t part, int64_t M, int r_max,
-                                                                const int2* __restrict__ row_lora, int sites) {
+template <bool LATER>
+__global__ void __launch_bounds__(kThreads) gated_halves_kernel(HalvesOf first, HalvesOf second, size_t part, int64_t M, int r_max, int2* row_lora,
+                                                                int sites) {
   const int64_t i = (int64_t)blockIdx.x * kHalvesRowsWg + (threadIdx.x >> 5);  // line
   if (i > M) return;
   const bool other = (int)blockIdx.z >= sites;
@@ -64,27 +66,33 @@ __global__ void __launch_bounds__(kThreads) gated_halves_kernel(HalvesOf first, 
   const Halves out = other ? second.out : first.out;
   const int chunk = blockIdx.y, s = (int)blockIdx.z - (other ? sites : 0), c = chunk * 32 + (threadIdx.x & 31);
   float x = 0.f;
-  if (i > 0 && c < row_lora[s * M + i - 1].y) {
+  if (i > 0 && c < (row_lora[s * M + i - 1].y & (kLaterBit - 1))) {
     const float* const q = v + (size_t)s * part * parts + (size_t)(i - 1) * r_max + c;
     for (int p = 0; p < parts; ++p) x += q[p * part];
+  }
+  if (LATER && !finite_f32(x)) {
+    x = 0.f;
+    atomicOr(&row_lora[s * M + i - 1].y, kLaterBit);
   }
   const bf16_t hi = f32_to_bf16(x);
   bf16_t* const line = out.at + s * out.site + chunk * out.chunk + (size_t)i * 64 + (threadIdx.x & 31);
   line[0] = hi;
-  line[32] = f32_to_bf16(x - bf16_to_f32(hi));
+  line[32] = f32_to_bf16(rest_of(x, bf16_to_f32(hi)));
 }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 }  // namespace
 
-static int launch_halves_of(const HalvesOf& first, const HalvesOf* second, int64_t M, int r_max, const int2* row_lora, int sites, hipStream_t st) {
+static int launch_halves_of(const HalvesOf& first, const HalvesOf* second, int64_t M, int r_max, int2* row_lora, int sites, bool later, hipStream_t st) {
   const dim3 grid((unsigned)((M + kHalvesRowsWg) / kHalvesRowsWg), (unsigned)((r_max + 31) / 32), (unsigned)(second ? 2 * sites : sites));
-  hipLaunchKernelGGL(gated_halves_kernel, grid, dim3(kThreads), 0, st, first, second ? *second : first, (size_t)M * r_max, M, r_max, row_lora, sites);
+  const HalvesOf& other = second ? *second : first;
+  if (later) hipLaunchKernelGGL(gated_halves_kernel<true>, grid, dim3(kThreads), 0, st, first, other, (size_t)M * r_max, M, r_max, row_lora, sites);
+  else hipLaunchKernelGGL(gated_halves_kernel<false>, grid, dim3(kThreads), 0, st, first, other, (size_t)M * r_max, M, r_max, row_lora, sites);
   return check_launch();
 }
 
-int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st) {
-  return launch_halves_of(HalvesOf{v, parts, out}, nullptr, M, r_max, row_lora, sites, st);
+int launch_halves(const float* v, int parts, int64_t M, int r_max, int2* row_lora, int sites, const Halves& out, hipStream_t st) {
+  return launch_halves_of(HalvesOf{v, parts, out}, nullptr, M, r_max, row_lora, sites, true, st);
 }
 
 // (2 F is below 2^31: the entry points refuse larger ones)
@@ -837,7 +845,7 @@ int backward_tiles(const GatedCall& g, const void* dY, const float* gate, const 
     rc = launch_shrink_sites((const bf16_t*)g.X, g.d, M, g.d, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, nullptr, nullptr, st);
     if (rc) return rc;
   }
-  if ((rc = launch_halves_of(low, dB ? &t : nullptr, M, r_max, w.row_lora, 2, st))) return rc;
+  if ((rc = launch_halves_of(low, dB ? &t : nullptr, M, r_max, w.row_lora, 2, false, st))) return rc;
   if (dX) {
     GatedBackArgs a{};
     a.dz = dz; a.M = M; a.d = g.d; a.F = g.F; a.row_to_req = g.row_to_req; a.ad = g.ad; a.tenant_id = g.tenant_id; a.route = g.route; a.B = g.B;

@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               hi[h] = pack_bf16x2(tv[2 * h], tv[2 * h + 1]);
-              lo[h] = pack_bf16x2(tv[2 * h] - __uint_as_float(hi[h] << 16), tv[2 * h + 1] - __uint_as_float(hi[h] & 0xffff0000u));
+              lo[h] = pack_bf16x2(rest_of(tv[2 * h], __uint_as_float(hi[h] << 16)), rest_of(tv[2 * h + 1], __uint_as_float(hi[h] & 0xffff0000u)));
             }
             unsigned char* const x = lds + (2 * st + (row >> 7)) * kHalfBytes + ((row >> 4) & 7) * kBlockBytes + (row & 15) * 128 + (rq & 1) * 8;
             *(u32x2*)(x + (((rq >> 1) ^ swz(row & 15)) << 4)) = hi;
@@ -646,11 +646,13 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
 #pragma unroll 1
     for (int s = 0; s < kSites; ++s) {
       const int my_ten = lora[s].y ? lora[s].x : -1;
+      const bool later = (lora[s].y & kLaterBit) != 0;
       row_ten[tid] = my_ten;  // (of the site before: read for the last time in front of a barrier)
       int last = -1;
       for (;;) {
         if (tid == 0) ctl[0] = 0x7fffffff;
         __syncthreads();
+        if (later) ctl[1] = 1;
         int cand = my_ten > last ? my_ten : 0x7fffffff;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -833,7 +835,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   __syncthreads();
   unsigned char* const mine = lds + wave * (128 * kOutPitch);
   if constexpr (GATED) {
-    // What the stages could not take (products with the tenant's own Inf and NaN) has to be in g and u before the activation: formed
+    // What the stages could not take (products of the tenant's own Inf and NaN) has to be in g and u before the activation: formed
     // row by row in the wave's LDS, 64 columns at a time, and added.
     if (bad) {
 #pragma unroll 1
@@ -852,7 +854,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
             for (int k = 0; k < p.parts; ++k) t += p.t[s * p.t_site + k * p.t_stride + (size_t)m * p.ad.r_max + c];
             for (int q = 0; q < 64; ++q) {
               const int n = n0 + wn * 64 + q;
-              if (n < p.d2 && (b[n] & 0x7f80u) == 0x7f80u) more[q] += t * bf16_to_f32(b[n]);
+              if (n < p.d2 && ((b[n] & 0x7f80u) == 0x7f80u || !finite_f32(t))) more[q] += t * bf16_to_f32(b[n]);
             }
           }
         }
@@ -997,7 +999,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
           const int n = n0 + wn * 128 + (q >> 4) * 32 + ((q >> 2) & 3) * 8 + (lane >> 5) * 4 + (q & 3);
           if (n >= p.d2) continue;
           const bf16_t bv = b[BACK ? (size_t)n * r : (size_t)n];
-          if ((bv & 0x7f80u) != 0x7f80u) continue;
+          // (MX forward: Inf and NaN of t are left for here too; a high half by itself otherwise)
+          if ((bv & 0x7f80u) != 0x7f80u && !(HALVES && !BACK && !finite_f32(t))) continue;
           if (whole) {
             bf16_t* const y = p.Y + (size_t)m * p.d2 + n;
             *y = f32_to_bf16(bf16_to_f32(*y) + t * bf16_to_f32(bv));

@@ -108,8 +108,9 @@ int gated_prefill(const GatedTileArgs& g, hipStream_t st);
 bool mx4_prefill_supported(int64_t M, int d1, int d2);
 // A linear on 4-bit weights (g.Wg, g.d inputs, g.F columns), [1][..] shrinks, look-ups and halves.
 int linear_prefill_mx4(const GatedTileArgs& g, const bf16_t* bias, int site, hipStream_t st);
-// (gated.hip) v [site][part][M][r_max] to `sites` sites' halves.
-int launch_halves(const float* v, int parts, int64_t M, int r_max, const int2* row_lora, int sites, const Halves& out, hipStream_t st);
+// (gated.hip) v [site][part][M][r_max] to `sites` sites' halves.  Inf and NaN become zeros there and set kLaterBit of the row's rank.
+constexpr int kLaterBit = 1 << 16;
+int launch_halves(const float* v, int parts, int64_t M, int r_max, int2* row_lora, int sites, const Halves& out, hipStream_t st);
 
 // dX = [dg | du] [W_gate; W_up] + sum over the two sites of low A^T on 256 x 256 tiles (prefill.hip).
 struct GatedBackArgs {

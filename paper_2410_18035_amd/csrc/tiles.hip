@@ -371,13 +371,23 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
                 for (int k = 0; k < p.parts; ++k) tv[e] += tp[k * p.t_stride + e];
           }
         };
-        auto put_t = [&](int group, const float (&tv)[8]) __attribute__((always_inline)) {  // group of the batch
+        auto put_t = [&](int group, float (&tv)[8]) __attribute__((always_inline)) {  // group of the batch
+          if constexpr (GATED) {  // (zero columns of the other projection beside it: Inf and NaN are left for the end, as those of W^B)
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += tv[e] - tv[e];
+            if (!(sum == 0.f)) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) tv[e] = finite_f32(tv[e]) ? tv[e] : 0.f;
+              ctl[kCtlBad] = 1;
+            }
+          }
           u32x4 hi, lo;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bf16_t h0 = f32_to_bf16(tv[2 * e]), h1 = f32_to_bf16(tv[2 * e + 1]);
             hi[e] = (uint32_t)h0 | ((uint32_t)h1 << 16);
-            lo[e] = pack_bf16x2(tv[2 * e] - bf16_to_f32(h0), tv[2 * e + 1] - bf16_to_f32(h1));
+            lo[e] = pack_bf16x2(rest_of(tv[2 * e], bf16_to_f32(h0)), rest_of(tv[2 * e + 1], bf16_to_f32(h1)));
           }
           unsigned char* const row = ring + (group >> 2) * C::StageBytes + xr * 128;
           *reinterpret_cast<u32x4*>(row + (((group & 3) ^ swz(xr & 15)) << 4)) = hi;
@@ -572,8 +582,9 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
         for (int it = 0; it < C::Items; ++it)
 #pragma unroll
           for (int u = 0; u < kU; ++u) {
-            const float t = ts[(r0 + it * kRowStep) * kTs + c0 + u];
             const bool in = c0 + u < cnt[it];
+            float t = ts[(r0 + it * kRowStep) * kTs + c0 + u];
+            if (GATED) t = in ? t : 0.f;  // (of the other site's ranks, for columns that do not take them)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t x = in ? b[it][u][e] : 0u;
@@ -599,12 +610,12 @@ __global__ void __launch_bounds__(kT, 2 * C::OCC) tile_kernel(const TParams p) {
       const float* const t_of = p.t + (GATED ? my_site * p.t_site : 0);
       for (int c = 0; c < r; ++c) {
         const u32x4 b = *(gu32x4_a2*)(in_global(p.ad.B[ten * MILORA_NUM_SITES + p.site + my_site]) + (size_t)c * p.d2 + n0 + my_col);
-        if (!(nonfinite2(b[0]) | nonfinite2(b[1]) | nonfinite2(b[2]) | nonfinite2(b[3]))) continue;
+        if (!GATED && !(nonfinite2(b[0]) | nonfinite2(b[1]) | nonfinite2(b[2]) | nonfinite2(b[3]))) continue;
         float t = 0.f;
         for (int k = 0; k < p.parts; ++k) t += t_of[k * p.t_stride + (size_t)(m0 + row) * p.ad.r_max + c];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t bad = nonfinite2(b[e]);
+          const uint32_t bad = GATED && !finite_f32(t) ? ~0u : nonfinite2(b[e]);
           if (bad & 0x8000u) val[it][e >> 1][2 * (e & 1)] += t * __uint_as_float(b[e] << 16);
           if (bad & 0x80000000u) val[it][e >> 1][2 * (e & 1) + 1] += t * __uint_as_float(b[e] & 0xffff0000u);
         }

@@ -537,3 +537,68 @@ def test_the_block_is_the_middle_of_a_layer():
     for m, y in outs:
         assert (m.cpu().double() - ref).norm() <= 2.5e-3 * ref.norm()  # one rounding
         assert (y.cpu().double() - out).norm() <= 4e-3 * out.norm()    # two
+
+
+# Kernels: few rows in fp32 arithmetic, tiles of 64 and 128 (terms row by row, and by the matrix cores), 256 x 256 (cut too), 4-bit weights of few rows,
+# on the codes and written out, any shape.
+@gpu
+@pytest.mark.parametrize("M,d,F,dtype,mx4", [
+    (9, 70, 96, torch.bfloat16, False), (20, 128, 96, torch.bfloat16, False), (63, 1024, 528, torch.bfloat16, False), (130, 128, 192, torch.bfloat16, False),
+    (300, 512, 1040, torch.bfloat16, False), (600, 1280, 1040, torch.bfloat16, False), (2100, 1536, 4112, torch.bfloat16, False), (9, 128, 96, torch.bfloat16, True),
+    (100, 512, 272, torch.bfloat16, True), (600, 1056, 304, torch.bfloat16, True), (1100, 512, 2064, torch.bfloat16, True), (2049, 640, 2064, torch.bfloat16, True),
+    (12, 30, 50, torch.float32, False), (40, 30, 50, torch.float32, False), (300, 250, 683, torch.float32, False)])
+def test_an_infinite_scale_stays_infinite_and_in_its_projection(M, d, F, dtype, mx4):
+    """x W^A_4 of one rank is Inf for a tenant's rows: g is Inf by the signs of the factors, u is what it was."""
+    c, x, W, dense = _layer(M, 6, 3, d, F, (8, 16), 40 + M, dtype, "mixed", mx4)
+    c.route[:] = 0x80 | 0x30
+    c.tid[:] = torch.tensor([0, 1, 2, 0, 1, 2])
+    tid, route = c.requests()
+    gate, up = (torch.empty(M, F, device=DEV) for _ in range(2))
+    run = lambda: mb.milora_gated_linear(x, *W, c.tab, tid, route, row_to_req=c.rows(), w_layout=mb.W_MX4 if mx4 else mb.W_ROWMAJOR, F=F, gate_out=gate, up_out=up)
+    clean, u = run(), up.clone()
+    assert torch.isfinite(clean).all()
+    c.A[4][1][3, 2] = float("inf")
+    assert (x[:, 3] != 0).all() and (c.Bm[4][1][2] != 0).all()
+    Y = run()
+    mine = (torch.tensor(c.tenants(4)) == 1).to(DEV)
+    assert mine.any() and torch.equal(Y[~mine], clean[~mine])
+    sign = torch.sign(x[mine, 3].float())[:, None] * torch.sign(c.Bm[4][1][2].float())
+    assert torch.equal(gate[mine], sign * float("inf"))
+    assert torch.equal(up, u)
+    pos = sign > 0
+    assert torch.isnan(Y[mine][~pos]).all()  # silu(-Inf) is -Inf / Inf
+    assert torch.equal(Y[mine][pos].float(), (torch.sign(u[mine]) * float("inf"))[pos])
+
+
+@gpu
+@pytest.mark.parametrize("M,d,F,mx4", [(40, 128, 96, False), (300, 192, 320, False), (1100, 1536, 1088, False), (300, 256, 704, True), (64, 160, 48, True), (40, 30, 50, False)])
+def test_backward_of_an_infinite_scale(M, d, F, mx4):
+    """dz (W^B)^T of one rank is Inf for a tenant's rows: dX is Inf by the signs of the factors, other gradients are what they were."""
+    dtype = torch.bfloat16 if d % 32 == 0 else torch.float32
+    c, x, W, dense = _layer(M, 6, 3, d, F, (8, 16), 41, dtype, "mixed", mx4)
+    c.route[:] = 0x80 | 0x30
+    c.tid[:] = torch.tensor([0, 1, 2, 0, 1, 2])
+    tid, route = c.requests()
+    kw = dict(row_to_req=c.rows(), w_layout=mb.W_MX4 if mx4 else mb.W_ROWMAJOR, F=F)
+    gate, up = (torch.empty(M, F, device=DEV) for _ in range(2))
+    mb.milora_gated_linear(x, *W, c.tab, tid, route, gate_out=gate, up_out=up, **kw)
+    dY = c.rnd(M, F)
+
+    def run():
+        dA, dB = _room(c, d, F)
+        return mb.milora_gated_linear_backward(dY, x, gate, up, *W, c.tab, tid, route, grads=_table(c, dA, dB), **kw), dA, dB
+
+    dX, dA, dB = run()
+    c.Bm[5][1][2, 7] = float("inf")
+    got, dA2, dB2 = run()
+    mine = (torch.tensor(c.tenants(5)) == 1).to(DEV)
+    du = dY[:, 7].float() * gate[:, 7] * torch.sigmoid(gate[:, 7])
+    assert mine.any() and (du != 0).all() and (c.A[5][1][:, 2] != 0).all()
+    assert torch.equal(got[~mine], dX[~mine])
+    assert torch.equal(got[mine].float(), torch.sign(du[mine])[:, None] * torch.sign(c.A[5][1][:, 2].float()) * float("inf"))
+    for s in range(2):
+        for t in range(3):
+            assert torch.equal(dB2[s][t], dB[s][t])
+            keep = [k for k in range(c.rank[t]) if (s, t, k) != (1, 1, 2)]
+            assert torch.equal(dA2[s][t][:, keep], dA[s][t][:, keep])
+    assert not torch.isfinite(dA2[1][1][:, 2]).any()

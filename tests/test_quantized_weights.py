@@ -479,3 +479,26 @@ def test_an_infinite_input_stays_infinite_through_a_step(B):
     keep = torch.arange(B, device=DEV) != 1
     assert torch.equal(y[keep], clean[keep]) and torch.equal(qkv2[keep], qkv[keep])
     assert (y[1] == float("inf")).all() and (qkv2[1] == float("inf")).all()
+
+
+@gpu
+@pytest.mark.parametrize("layout,M,d1,d2", [(mb.W_MX4, 5, 192, 80), (mb.W_MX4, 200, 192, 80), (mb.W_MX4, 700, 1056, 304), (mb.W_MX4, 2100, 640, 4112),
+                                            (mb.W_ROWMAJOR, 20, 192, 80), (mb.W_ROWMAJOR, 200, 192, 80), (mb.W_ROWMAJOR, 2100, 640, 4112), (mb.W_PACKED, 8, 192, 80),
+                                            (mb.W_PACKED, 200, 192, 80)])
+def test_linear_keeps_an_infinite_scale_infinite(layout, M, d1, d2):
+    site = 2
+    c = plain.Case(M, 4, 3, {site: (d1, d2)}, (8, 40), 50 + M, DEV, rows="mixed", sites=[site])
+    c.route[:] = site
+    c.tid[:] = torch.tensor([0, 1, 2, 1])
+    x, w = c.rnd(M, d1), c.rnd(d2, d1)
+    w = mb.milora_quantize_weight(w) if layout == mb.W_MX4 else mb.milora_pack_weight(w) if layout == mb.W_PACKED else w
+    tid, route = c.requests()
+    run = lambda: mb.milora_routed_linear(x, w, c.tab, site, tid, route, row_to_req=c.rows(), w_layout=layout, d2=d2)
+    clean = run()
+    c.A[site][1][3, 33] = float("inf")
+    assert (x[:, 3] != 0).all() and (c.Bm[site][1][33] != 0).all()
+    Y = run()
+    mine = (torch.tensor(c.tenants(site)) == 1).to(DEV)
+    assert mine.any() and torch.equal(Y[~mine], clean[~mine])
+    want = torch.sign(x[mine, 3].float())[:, None] * torch.sign(c.Bm[site][1][33].float()) * float("inf")
+    assert torch.equal(Y[mine].float(), want)
