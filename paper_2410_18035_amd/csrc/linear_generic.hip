@@ -317,16 +317,26 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = w / (C::WM * C::WN), wm = w % (C::WM * C::WN) % C::WM, wn = w % (C::WM * C::WN) / C::WM;
-  // workgroup -> tile: ids go round-robin over the 8 XCDs; each XCD takes a contiguous run of an order that walks kGroupM row tiles of one column
+  // workgroup -> tile: ids go round-robin over the 8 XCDs; each XCD takes a contiguous run of an order that walks kGenGroupM row tiles of one column
   // tile before the next column tile, so that its L2 serves the re-reads of W (gated block, 300 rows of 1000 x 2730, columns first: 52 us without
-  // LoRA rows)
+  // LoRA rows).  The small tiles of a linear, a turn or so of them, go columns first: rows of a high rank then do not meet on one compute unit (300
+  // rows of 1000 x 1000, a quarter of them of rank 64: 26 us a call, in the other order 32).
   const int total = tiles_m * tiles_n, per = (total + 7) >> 3;
-  const int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
-  const int first = id / (kGenGroupM * tiles_n) * kGenGroupM, in_group = id % (kGenGroupM * tiles_n);
-  const int gsz = tiles_m - first < kGenGroupM ? tiles_m - first : kGenGroupM;
-  const int64_t m0 = (int64_t)(first + in_group % gsz) * C::BM;
-  const int n0 = col0 + in_group / gsz * kOutN;
+  int row_tile, col_tile;
+  if constexpr (GATED || C::Outs > 2) {
+    const int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+    const int first = id / (kGenGroupM * tiles_n) * kGenGroupM, in_group = id % (kGenGroupM * tiles_n);
+    const int gsz = tiles_m - first < kGenGroupM ? tiles_m - first : kGenGroupM;
+    row_tile = first + in_group % gsz;
+    col_tile = in_group / gsz;
+  } else {
+    row_tile = (int)blockIdx.x / tiles_n;
+    col_tile = (int)blockIdx.x % tiles_n;
+    if (row_tile >= tiles_m) return;
+  }
+  const int64_t m0 = (int64_t)row_tile * C::BM;
+  const int n0 = col0 + col_tile * kOutN;
 
   const T* src[C::Items];
   const int kq = tid % (C::SK / 4) * 4;
@@ -431,19 +441,60 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
   }
 
   // LoRA expand, 32 ranks at a time: t of the rows by way of LDS; a thread's rows follow one another, so that they mostly belong to one tenant, whose
-  // sixteen rows of W^B it reads once for all of its outputs (eight rows of W^B for each output on their way together: 43.4 us a call of 300
-  // rows on 1000 x 2730 against 37.8 us; gated block of the same 82 us against 70)
+  // sixteen rows of W^B it reads once for all of its outputs, tenant by tenant.  Where the rows of some thread belong to more than a few tenants, and for
+  // two rows a thread: eight rows of W^B for each output, all outputs' on their way together (`apart`).  300 rows of 1000 x 2730 in fp32, every row
+  // routed, us a call tenant by tenant / apart: one tenant, rank 8 33.3 / 37.1, rank 32 36.7 / 46.3; rows dealt to 4 tenants in turn, rank 8
+  // 38.0 / 35.5, rank 32 43.6 / 46.3; to 16, rank 8 41.7 / 36.0, rank 32 51.8 / 46.3; in bf16, where a row of W^B is half as long, to 16, rank 8
+  // 46.7 / 41.6, rank 32 70.8 / 78.7.  The gated block goes tenant by tenant (its rows are a call's prompts; one tenant 56.7, with the choice in it
+  // 58.5).
   float* const ts = buf + C::TsOff;  // [site][row][32]
   int most = s_most[0];
   if (GATED) most = s_most[kSites - 1] > most ? s_most[kSites - 1] : most;
-  if (most > 0) {
+  const float* const tr = ts + (my * C::BM + r0) * 32;
+  auto bring_t = [&](int c0) __attribute__((always_inline)) {
+    for (int e = tid; e < kSites * C::BM * 32; e += C::T) {
+      const int s = e / (C::BM * 32), row = e / 32 % C::BM, c = c0 + (e & 31);
+      ts[e] = c < s_rank[s][row] ? t[s * t_site + (size_t)(m0 + row) * ad.r_max + c] : 0.f;
+    }
+    __syncthreads();
+  };
+  bool apart = !GATED && C::Outs <= 2;
+  if (!GATED && !apart && most > 0) {  // (a lane counts the tenants of some thread's rows; every wave comes to the same answer)
+    const int g = lane % (C::BM / C::Outs) * C::Outs;
+    int tenants = 0;
+    for (int i = 0; i < C::Outs; ++i) {
+      bool seen = s_rank[0][g + i] == 0;
+      for (int k = 0; k < i; ++k) seen |= s_rank[0][g + k] && s_ten[0][g + k] == s_ten[0][g + i];
+      tenants += !seen;
+    }
+    apart = __any(tenants > (most <= 8 ? 3 : 4)) && (sizeof(T) == 4 || most <= 8);
+  }
+  if (!GATED && most > 0 && apart) {
+    const T* Bm[C::Outs];
+    int last[C::Outs];
+#pragma unroll
+    for (int i = 0; i < C::Outs; ++i) {
+      last[i] = s_rank[my][r0 + i] - 1;
+      Bm[i] = last[i] >= 0 ? (const T*)ad.B[s_ten[my][r0 + i] * MILORA_NUM_SITES + site + my] + ns : nullptr;
+    }
     for (int c0 = 0; c0 < most; c0 += 32) {
-      for (int e = tid; e < kSites * C::BM * 32; e += C::T) {
-        const int s = e / (C::BM * 32), row = e / 32 % C::BM, c = c0 + (e & 31);
-        ts[e] = c < s_rank[s][row] ? t[s * t_site + (size_t)(m0 + row) * ad.r_max + c] : 0.f;
+      bring_t(c0);
+      for (int c1 = 0; c1 < 32 && c0 + c1 < most; c1 += 8) {
+        float b[C::Outs][8];
+#pragma unroll
+        for (int i = 0; i < C::Outs; ++i)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) b[i][u] = c0 + c1 + u <= last[i] ? Elem<T>::load(Bm[i], (size_t)(c0 + c1 + u) * d2) : 0.f;
+#pragma unroll
+        for (int i = 0; i < C::Outs; ++i)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) val[i] += tr[i * 32 + c1 + u] * b[i][u];
       }
       __syncthreads();
-      const float* const tr = ts + (my * C::BM + r0) * 32;
+    }
+  } else if (most > 0) {
+    for (int c0 = 0; c0 < most; c0 += 32) {
+      bring_t(c0);
       unsigned left = 0;  // rows whose term is still to be added
 #pragma unroll
       for (int i = 0; i < C::Outs; ++i)

@@ -360,3 +360,32 @@ def test_tiles_in_parts_replay_in_a_graph(packed, M, d1, d2):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager), f"replay {rep}"
+
+
+@gpu
+@pytest.mark.parametrize("M,d1,d2,dtype", [(300, 250, 1430, torch.float32), (100, 130, 300, torch.float32), (300, 130, 1430, torch.bfloat16), (70, 3, 1430, torch.float32)])
+@pytest.mark.parametrize("T,ranks", [(2, (8,)), (16, (8,)), (16, (8, 20, 64)), (70, (5, 33))])
+def test_any_shape_rows_do_not_depend_on_their_neighbours(M, d1, d2, dtype, T, ranks):
+    """Rows of a tenant side by side and rows dealt to the tenants in turn take W^B in different ways: the same bits."""
+    A, B, rank = _adapters(T, d1, d2, ranks, 0.2, M + T, dtype)
+    tab = mb.AdapterTable.from_tensors(A, B, rank)
+    g = torch.Generator(device=DEV).manual_seed(T)
+    rnd = lambda *s: torch.empty(*s, dtype=torch.float32, device=DEV).normal_(0, 1, generator=g).to(dtype)
+    X, W = rnd(M, d1), rnd(d2, d1)
+    tid, route = torch.arange(T, dtype=torch.int32, device=DEV), torch.full((T,), 4, dtype=torch.uint8, device=DEV)
+    route[T // 2] = mb.ROUTE_NONE
+    turn = (torch.arange(M, device=DEV) % T).to(torch.int32)
+    side = torch.sort(turn, stable=True)[1]
+    Y = mb.milora_routed_linear(X, W, tab, 4, tid, route, row_to_req=turn)
+    grouped = mb.milora_routed_linear(X[side].contiguous(), W, tab, 4, tid, route, row_to_req=turn[side].contiguous())
+    assert torch.equal(grouped, Y[side])
+    x, w = X.double(), W.double()
+    ref, size = x @ w.T, x.abs() @ w.abs().T
+    for t in range(T):
+        if t != T // 2:
+            rows, a, b = turn == t, A[t][4].double(), B[t][4].double()
+            ref[rows] += (x[rows] @ a) @ b
+            size[rows] += (x[rows].abs() @ a.abs()) @ b.abs()
+    # fp32 sums of d1 and then rank terms, one rounding to the type
+    tol = size * (d1 + max(rank) + 16) * 2.0 ** -24 + ref.abs() * torch.finfo(dtype).eps / 2
+    assert ((Y.double() - ref).abs() <= tol).all()
