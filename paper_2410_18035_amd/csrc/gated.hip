@@ -479,13 +479,10 @@ __global__ void __launch_bounds__(kThreads) gated_dx_sum_kernel(const float* __r
 struct GradArgs {
   const void *X, *dz;
   int64_t M;
-  int d, F, T, tiles_a, tiles_b, chunks;  // 64-column tiles of dA and dB, chunks of 32 ranks
+  int d, F, tiles_a, tiles_b;  // tiles of 64 columns of dA and dB
   const int2 *row_lora, *among;
   AdapterView ad;
   const float *low, *t;  // [site][M][r_max]
-  size_t t_part;
-  size_t t_site;
-  int parts;
   void* const* dA;
   void* const* dB;
 };
@@ -505,8 +502,7 @@ __global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) 
   const int cols = is_b ? g.F : g.d, n0 = (is_b ? tile - g.tiles_a : tile) * 64;
   const T* const P = is_b ? (const T*)g.dz + (int64_t)s * g.F : (const T*)g.X;
   const int64_t ldp = is_b ? 2 * (int64_t)g.F : g.d;
-  const float* const sc = is_b ? g.t + s * g.t_site : g.low + (size_t)s * g.M * g.ad.r_max;
-  const int parts = is_b ? g.parts : 1;
+  const float* const sc = (is_b ? g.t : g.low) + (size_t)s * g.M * g.ad.r_max;
   // the first and the last 64 rows that can hold one of the tenant's
   const int blocks = (int)((g.M + 63) / 64);
   if (tid == 0) { span[0] = blocks; span[1] = 0; }
@@ -554,10 +550,7 @@ __global__ void __launch_bounds__(kThreads) gated_grad_kernel(const GradArgs g) 
     }
     for (int e = tid; e < 32 * 32; e += kThreads) {
       const int k = e >> 5, c = c0 + (e & 31);
-      float v = 0.f;
-      if (k < n && c < r)
-        for (int p = 0; p < parts; ++p) v += sc[p * g.t_part + (size_t)rows[k] * g.ad.r_max + c];
-      ss[k][e & 31] = v;
+      ss[k][e & 31] = k < n && c < r ? sc[(size_t)rows[k] * g.ad.r_max + c] : 0.f;
     }
     __syncthreads();
     if (w < 2)
@@ -807,17 +800,15 @@ int backward_any(const GatedCall& g, const void* dY, const float* gate, const fl
   }
   if (dA || dB) {
     GradArgs a{};
-    a.X = g.X; a.dz = w.dz; a.M = M; a.d = g.d; a.F = g.F; a.T = tenants;
+    a.X = g.X; a.dz = w.dz; a.M = M; a.d = g.d; a.F = g.F;
     a.tiles_a = dA ? (g.d + 63) / 64 : 0;
     a.tiles_b = dB ? (g.F + 63) / 64 : 0;
-    a.chunks = (g.ad.r_max + 31) / 32;
+    const int chunks = (g.ad.r_max + 31) / 32;
     a.row_lora = w.row_lora; a.among = w.among; a.ad = g.ad; a.low = w.low; a.t = w.t;
-    a.parts = 1;
-    a.t_part = (size_t)M * g.ad.r_max; a.t_site = a.t_part;
     a.dA = dA; a.dB = dB;
     rc = launch_shrink(g.X, g.d, M, g.d, g.dtype, g.row_to_req, g.ad, kGate, 2, g.tenant_id, g.route, g.B, w.t, st);
     if (rc) return rc;
-    hipLaunchKernelGGL(gated_grad_kernel<T>, dim3((unsigned)((a.tiles_a + a.tiles_b) * a.chunks), (unsigned)(2 * tenants)), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(gated_grad_kernel<T>, dim3((unsigned)((a.tiles_a + a.tiles_b) * chunks), (unsigned)(2 * tenants)), dim3(kThreads), 0, st, a);
     rc = check_launch();
   }
   return rc;
