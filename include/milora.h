@@ -284,7 +284,8 @@ int milora_gated_linear_backward(const void *dY, const void *X, const float *gat
  * a launch), EUNSUPPORTED (packed or 4-bit layout with fp32, with d or F not a multiple of 32, or with x, y, attn_out, qkv_out or a
  * weight not 16-byte aligned), EWORKSPACE, EHIP.
  * MILORA_W_MX4: eight launches; the outputs of o, gate, up and down stay in fp32 up to the glue's rounding, and n(u) W is formed as
- * (u W) / sqrt(mean(u^2) + 1e-5), u rounded to bf16 in the place of n(u) (up to 8 requests the gate and up projections take h as the sum of two bf16 values).  No wait inside a launch, and what the workspace holds before a
+ * (u W) / sqrt(mean(u^2) + 1e-5), u rounded to bf16 in the place of n(u); the gate and up projections
+ * take h as the sum of two bf16 values (16 bits).  No wait inside a launch, and what the workspace holds before a
  * call does not matter.
  */
 size_t milora_layer_decode_workspace_bytes(int B, int d, int F, int r_max);

@@ -238,16 +238,11 @@ int layer_decode_generic(const void* x, int B, int d, int F, int dtype, const mi
 struct MxLayerWs {
   float* h;     // [B][d]
   bf16_t* qkv;  // [B][3 d]
-  bf16_t* hn;   // [B][d]: h rounded
+  bf16_t* hn;   // [2][B][d]: h as two bf16 values, rounded and the rest (16 bits of it)
   bf16_t* mm;   // [B][F]
   char* level;  // workspace of a level
   size_t bytes;
 };
-
-// Up to this many requests h goes into the gate and up projections as two bf16 rows, rounded and the rest (16 bits of it): the matrix instructions of up
-// to 16 rows have them to spare (one request of a 7B-sized layer: y is 0.0024 off its
-// exact value, with the rounding 0.0029; 52 us a step for 50).
-constexpr int kMxSecond = 8;
 
 MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
   size_t off = 0;
@@ -256,14 +251,12 @@ MxLayerWs carve_mx4(void* base, int B, int d, int F, int r_max) {
   MxLayerWs w;
   w.h = (float*)(b + take((size_t)B * d * 4));
   w.qkv = (bf16_t*)(b + take((size_t)B * d * 6));
-  // (room for the largest need of up to B requests: the size never falls with B, so that one workspace serves every smaller batch)
-  const int rows = B <= kMxSecond ? 2 * B : B > 2 * kMxSecond ? B : 2 * kMxSecond;
-  w.hn = (bf16_t*)(b + take((size_t)rows * d * 2));
+  w.hn = (bf16_t*)(b + take((size_t)B * d * 4));
   w.mm = (bf16_t*)(b + take((size_t)B * F * 2));
   size_t level = 0;
   const struct { int d1, d2, sites; } levels[4] = {{d, d, 3}, {d, d, 1}, {d, F, 2}, {F, d, 1}};
   for (const auto& l : levels) {
-    const size_t n = mx4_rows_workspace_bytes(l.sites == 2 ? rows : B, l.d1, l.d2, r_max, l.sites);
+    const size_t n = mx4_rows_workspace_bytes(B, l.d1, l.d2, r_max, l.sites, l.sites == 2);
     level = n > level ? n : level;
   }
   w.level = b + take(level);
@@ -293,13 +286,13 @@ int layer_decode_mx4(const bf16_t* x, int B, int d, int F, const milora_layer_we
   g.Y[0] = w.hn;
   g.res = x;
   g.h_out = w.h;
-  g.left_out = B <= kMxSecond ? w.hn + (size_t)B * d : nullptr;
+  g.left_out = w.hn + (size_t)B * d;
   if ((rc = attn_out ? level(3, 1, attn_out, d, false, d) : level(3, 1, qkv + 2 * (size_t)d, 3 * (int64_t)d, false, d))) return rc;
   g.res = nullptr;
   g.left_out = nullptr;
   g.Y[0] = w.mm;
   g.norm_h = norm ? w.h : nullptr;
-  g.second = B <= kMxSecond;
+  g.second = true;
   if ((rc = level(4, 2, w.hn, d, true, F))) return rc;
   g.second = false;
   g.norm_h = nullptr;
@@ -643,7 +636,7 @@ static int layer_decode_impl(const void* x, int B, int d, int F, int dtype, cons
     if (weights->layout == MILORA_W_MX4) {
       if (marks) return MILORA_EUNSUPPORTED;
       if (d > 0x3fffffff || F > 0x3fffffff) return MILORA_ERANGE;
-      if (!mx4_rows_fit(B, d, d, 3) || !mx4_rows_fit(B, d, d, 1) || !mx4_rows_fit(B, d, F, 2, B <= kMxSecond) || !mx4_rows_fit(B, F, d, 1)) return MILORA_ERANGE;
+      if (!mx4_rows_fit(B, d, d, 3) || !mx4_rows_fit(B, d, d, 1) || !mx4_rows_fit(B, d, F, 2, true) || !mx4_rows_fit(B, F, d, 1)) return MILORA_ERANGE;
       return layer_decode_mx4((const bf16_t*)x, B, d, F, weights, ad, tenant_id, route, flags, (const bf16_t*)attn_out, (bf16_t*)y,
                               (bf16_t*)qkv_out, workspace, st);
     }

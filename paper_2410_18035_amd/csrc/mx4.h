@@ -31,7 +31,8 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
 struct MxArgs {
   const bf16_t* X;  // M rows of ldx elements
   int64_t ldx;
-  bool second;      // behind them M rows with what their rounding left, which the products take in as well
+  bool second;      // behind them M rows with what their rounding left, which the products take in as well (without: 32 requests 73.6 us a step for 77,
+                    // 128 165 for 186, and y 0.0031 off its exact value for 0.0025)
   int M, d1, d2;
   const unsigned char* W[3];  // of the sites; gated: W[0] gate, W[1] up
   const bf16_t* bias;
@@ -59,7 +60,11 @@ constexpr int64_t kMxAlwaysFew = 128, kMxMostFew = 512;
 inline bool mx4_few_rows(int64_t M, int d1, int64_t columns) {
   return M <= kMxAlwaysFew || (M <= kMxMostFew && (double)M * d1 * columns <= 24e9);
 }
-size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites);
+// Up to so many rows the second ones are rows of their own behind them: the matrix instructions of up to 16 rows have them to spare.  Beyond, they
+// go through LDS after the first ones (us a decode step of 4096 x 11008, behind / after: 1 request 47.1 / 49.0, 5 52 / 56, 8 56 / 60, 9 66 / 61, 16 68 /
+// 64, 32 82 / 77, 128 211 / 186).
+constexpr int kMxBehind = 8;
+size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites, bool second = false);
 // Does a launch take these sizes?
 bool mx4_rows_fit(int64_t M, int d1, int d2, int sites, bool second = false);
 // gated: sites = 2

@@ -149,12 +149,14 @@ struct MxBase {
   float* partial;  // [site][part][M][d2]
   int shrink_parts, shrink_z;  // the shrink: parts of a row, workgroups in all (a multiple of 8)
   ShrinkArgs shrink;
-  const bf16_t* second;  // second rows of the shrink's X, or null
+  const bf16_t* second;  // SECOND: second rows of the shrink's X
   MxTerm* terms;  // [site][M]
 };
 
 constexpr int kMxShrinkK = 1024;
-// Workgroup `id` of those in front: the shrink of one row, site and 1024 inputs; most rows have no term and end at once.
+// Workgroup `id` of those in front: the shrink of one row, site and 1024 inputs; most rows have no term and end at once.  SECOND: X is the sum of the
+// row and its second one (a choice in the loop would have every load waited for by itself: one row of 4096 x 4096 12.2 us a call for 11.0).
+template <bool SECOND>
 __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned char* lds) {
   const ShrinkArgs& sh = g.shrink;
   const int tid = threadIdx.x, lane = tid & 63, d1 = g.d1;
@@ -169,7 +171,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
   if (r == 0) return;
   gbf16* const A = in_global(sh.ad.A[ten * MILORA_NUM_SITES + site]);
   const bf16_t* const x = sh.X + (size_t)m * sh.ldx;
-  const bf16_t* const x2 = g.second ? g.second + (size_t)m * sh.ldx : nullptr;
+  const bf16_t* const x2 = SECOND ? g.second + (size_t)m * sh.ldx : nullptr;
   // lane: eight ranks (piece) of every kpl-th input of the wave's 128
   const int pieces = (r + 7) >> 3;
   int p2 = 1;
@@ -190,7 +192,7 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
         if (left >= 8) a[u] = *(gu32x4_any*)q;
         else a[u] = load8(q, left, false);
         xv[u] = bf16_to_f32(x[kk]);
-        if (x2) xv[u] += bf16_to_f32(x2[kk]);  // (16 bits of h, exact in fp32)
+        if constexpr (SECOND) xv[u] += bf16_to_f32(x2[kk]);  // (16 bits of h, exact in fp32)
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
@@ -217,16 +219,20 @@ __device__ __forceinline__ void mx4_shrink_row(const MxBase& g, int id, unsigned
 }
 
 // MORE: more than 32 rows.  XM: pieces of X a thread brings; with four the registers allow three workgroups a compute unit (gated, one row of
-// 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3).
-template <int KW, int NL, bool MORE, int XM>
-__global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
+// 4096 x 11008, 688 workgroups: 15.4 us a call, with two 20.3); up to 64 of them with the shorter parts four (what the shrink of second rows takes more
+// would leave three: one request of 5120 x 13824 56.1 us a decode step for 54.6).
+// SECOND (MxArgs::second): kBehind: the second rows follow the first ones among the M rows; kPlanes: a row group's second rows go through LDS after its
+// first ones and are added to the same sums.
+enum MxSecond { kNone, kBehind, kPlanes };
+template <int KW, int NL, bool MORE, int XM, MxSecond SECOND>
+__global__ void __launch_bounds__(kMxT, NL < 8 && SECOND == kBehind ? 8 : XM <= 4 ? 6 : 4) mx4_base_kernel(const MxBase g) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d1 = g.d1;
   int id = blockIdx.x;
   if (id < g.shrink_z) {
-    mx4_shrink_row(g, id, lds);
+    mx4_shrink_row<SECOND != kNone>(g, id, lds);
     return;
   }
   // workgroup -> tile: ids go round-robin over the 8 XCDs (those in front are a multiple of 8); with more than 32 rows an XCD takes a contiguous
@@ -250,12 +256,12 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
   // ---- X: [row][kPart], asked for in front of the codes, which may come later ----
   constexpr int kPieces = kPart / 8, kXMost = XM;  // (rows x kPieces is kXMost x kMxT at most)
   u32x4 x[kXMost];
-  auto ask_x = [&](int m0) __attribute__((always_inline)) {
+  auto ask_x = [&](const bf16_t* X, int m0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kXMost; ++u) {
       const int e = tid + u * kMxT, m = m0 + e / kPieces, p = e % kPieces;
       x[u] = u32x4{0u, 0u, 0u, 0u};
-      if (e < 32 * kPieces && m < g.M && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(g.X + (size_t)m * g.ldx + k_part + p * 8);
+      if (e < 32 * kPieces && m < g.M && k_part + p * 8 < d1) x[u] = *reinterpret_cast<const u32x4*>(X + (size_t)m * g.ldx + k_part + p * 8);
     }
   };
   // ---- scales: whole lines of the workgroup's columns, into LDS with the first rows of X ----
@@ -276,7 +282,7 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
         if (e < left) scales[e >> 2] = (scales[e >> 2] & ~(255u << (8 * (e & 3)))) | ((uint32_t)sp[e] << (8 * (e & 3)));
     }
   }
-  ask_x(rg * 32);
+  ask_x(g.X, rg * 32);
   __builtin_amdgcn_sched_barrier(0);
   // ---- codes: NL steps ----
   u32x4 c[kH][kS];
@@ -307,6 +313,8 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
   float* const red = reinterpret_cast<float*>(lds + kScaleArea);
   if (scale_col < kCols) *reinterpret_cast<u32x4*>(lds + scale_col * kScalePitch + scale_piece * 16) = scales;
   typedef typename std::conditional<k16, uint32_t, uint16_t>::type scales_t;  // of a step: kG bytes
+  typename std::conditional<k16, f32x4, f32x16>::type acc[kH];
+  bool second = false;  // (kPlanes) second rows are being multiplied
   for (;;) {
     const int m0 = rg * 32, rows = g.M - m0 < 32 ? g.M - m0 : 32;
 #pragma unroll
@@ -315,14 +323,15 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
       if (r < rows) *reinterpret_cast<u32x4*>(lds + kScaleArea + r * kPitch + p * 16) = x[u];
     }
     barrier();
-    rg += row_split;
-    const bool more = MORE && rg < g.row_groups;
-    if (more) ask_x(rg * 32);
-    typename std::conditional<k16, f32x4, f32x16>::type acc[kH];
+    const bool again = SECOND == kPlanes && !second;  // the second rows of these come next
+    if (!again) rg += row_split;
+    const bool more = again || (MORE && rg < g.row_groups);
+    if (more) ask_x(again ? g.second : g.X, rg * 32);
+    if (!second)
 #pragma unroll
-    for (int h = 0; h < kH; ++h)
+      for (int h = 0; h < kH; ++h)
 #pragma unroll
-      for (int e = 0; e < (k16 ? 4 : 16); ++e) acc[h][e] = 0.f;
+        for (int e = 0; e < (k16 ? 4 : 16); ++e) acc[h][e] = 0.f;
     if (n0 < g.d2 && k0 < d1) {
       const int row = ln < rows ? ln : rows - 1;  // (rows past the end: results dropped)
       const unsigned char* const xr = lds + kScaleArea + row * kPitch + kw * NL * 128 + lg * 64;
@@ -344,8 +353,10 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
         }
       }
     }
-    // ---- the waves' sums ----
     barrier();
+    if (SECOND == kPlanes) second = again;
+    if (again) continue;
+    // ---- the waves' sums ----
     if (ln < rows)
 #pragma unroll
       for (int h = 0; h < kH; ++h)
@@ -374,7 +385,7 @@ __global__ void __launch_bounds__(kMxT, XM <= 4 ? 6 : 4) mx4_base_kernel(const M
 constexpr int kFinT = 256, kFinCols = 256;
 struct MxFinish {
   MxArgs a;
-  int parts, rows;  // rows of a part: a.M, or twice that
+  int parts, rows;  // rows of a part: a.M, or twice that (kBehind)
   const float* partial;
   const float* t;  // [site][t_parts][M][r_max]
   size_t t_part, t_site;
@@ -412,7 +423,7 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (p + 4 * u < f.parts) v[s] += x[u];
-      if (g.second) {
+      if (f.rows > g.M) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const f32x4*>(q + (size_t)g.M * g.d2 + (p + 4 * u < f.parts ? p + 4 * u : p) * stride);
 #pragma unroll
@@ -543,7 +554,8 @@ __global__ void __launch_bounds__(kFinT, 4) mx4_finish_kernel(const MxFinish f) 
   }
 }
 
-template <int KW, int NL, bool MORE, int XM>
+constexpr int kMxSteps = 8;
+template <int KW, int NL, bool MORE, int XM, MxSecond SECOND>
 int launch_base(const MxBase& b, hipStream_t st) {
   constexpr int kPart = KW * NL * 64, kRed = 32 * (kMxCols + 4) * 4;
   const int rows = b.M < 32 ? b.M : 32, x = rows * (kPart * 2 + 16), red = rows * (kMxCols + 4) * 4;
@@ -556,12 +568,28 @@ int launch_base(const MxBase& b, hipStream_t st) {
   MILORA_HIP(hipGetDevice(&dev));
   if (lds_set_for != dev) {
     const int most = (32 * (kPart * 2 + 16) > kRed ? 32 * (kPart * 2 + 16) : kRed) + kScaleArea;
-    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE, XM>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
+    MILORA_HIP(hipFuncSetAttribute((const void*)mx4_base_kernel<KW, NL, MORE, XM, SECOND>, hipFuncAttributeMaxDynamicSharedMemorySize, most < 160 * 1024 ? most : 160 * 1024));
     lds_set_for = dev;
   }
   const int64_t total = (int64_t)b.sites * b.col_groups * b.row_split * b.parts, grid = b.shrink_z + (total + 7) / 8 * 8;
-  hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE, XM>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
+  hipLaunchKernelGGL((mx4_base_kernel<KW, NL, MORE, XM, SECOND>), dim3((unsigned)grid), dim3(kMxT), bytes, st, b);
   return check_launch();
+}
+
+// (kBehind: two to sixteen rows; kPlanes: more than kMxBehind)
+template <MxSecond SECOND>
+int launch_base_of(const MxBase& b, int rows, int kw, bool half, hipStream_t st) {
+  if constexpr (SECOND != kBehind) {
+    if (kw == 2) return b.row_groups == 1 ? launch_base<2, kMxSteps, false, 8, SECOND>(b, st) : launch_base<2, kMxSteps, true, 8, SECOND>(b, st);
+  }
+  if constexpr (SECOND != kPlanes) {
+    static_assert(kMxBehind >= 8, "rows of mx4_waves");
+    if (rows <= 2) return launch_base<8, kMxSteps / 2, false, 1, SECOND>(b, st);
+    if (kw == 8 && half) return launch_base<8, kMxSteps / 2, false, 4, SECOND>(b, st);
+    if (kw == 8 && rows <= 4) return launch_base<8, kMxSteps, false, 4, SECOND>(b, st);
+    if (kw == 8) return launch_base<8, kMxSteps, false, 8, SECOND>(b, st);
+  }
+  return half ? launch_base<4, kMxSteps / 2, false, 4, SECOND>(b, st) : launch_base<4, kMxSteps, false, 8, SECOND>(b, st);
 }
 
 // How the first launch cuts a call; functions of the sizes alone.  Waves that share columns: X of a row group is rows x KW x NL x 128 bytes, 64 KB
@@ -569,7 +597,6 @@ int launch_base(const MxBase& b, hipStream_t st) {
 // one and two rows always (us a call, one row, 4096 x 4096 8.0 for 8.8, 4096 x 12288 11.1 for 12.0, gated 4096 x 11008 14.7 for 14.9), the
 // others where whole ones are more than two for each compute unit (gated 4096 x 11008, 8 rows 18.4 for 22.6, 16 rows 21.9 for 24.0; where they
 // are not: 4096 x 12288, 4 rows 14.5 for 13.9, 16 rows 16.0 for 15.4).
-constexpr int kMxSteps = 8;
 int mx4_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
 bool mx4_short(int64_t M, int d1, int d2, int sites) {
   const int kw = mx4_waves(M), cols = kMxCols / kw, part = kw * kMxSteps * 64;
@@ -647,13 +674,15 @@ int mx4_dequantize(const void* src, void* dst, int dtype, int d1, int d2, bool p
   return rc;
 }
 
-size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites) {
+size_t mx4_rows_workspace_bytes(int64_t M, int d1, int d2, int r_max, int sites, bool second) {
+  // (second rows: the largest need of up to M rows, so that it never falls with M)
+  const int64_t rows = !second ? M : M <= kMxBehind ? 2 * M : M > 2 * kMxBehind ? M : 2 * kMxBehind;
   return align_up((size_t)M * mx4_shrink_parts(d1) * r_max * sites * sizeof(float), 256) + align_up((size_t)M * sites * sizeof(MxTerm), 256) +
-         align_up(mx4_partial_floats(M, d1, d2, sites) * sizeof(float), 256);
+         align_up(mx4_partial_floats(rows, d1, d2, sites) * sizeof(float), 256);
 }
 
 bool mx4_rows_fit(int64_t M, int d1, int d2, int sites, bool second) {
-  const MxCut c = mx4_cut(second ? 2 * M : M, d1, d2, sites);
+  const MxCut c = mx4_cut(second && M <= kMxBehind ? 2 * M : M, d1, d2, sites);
   const int64_t shrinks = M * sites * mx4_shrink_parts(d1), tiles = (int64_t)sites * c.col_groups * c.row_split * c.parts;
   return shrinks + tiles <= ((int64_t)1 << 22) - 16;  // (a grid has to stay below 2^32 threads)
 }
@@ -663,7 +692,8 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   float* const t = (float*)workspace;
   MxTerm* const terms = (MxTerm*)((char*)t + align_up((size_t)g.M * r_max * t_parts * sites * sizeof(float), 256));
   float* const partial = (float*)((char*)terms + align_up((size_t)g.M * sites * sizeof(MxTerm), 256));
-  const int rows = g.second ? 2 * g.M : g.M;
+  const bool behind = g.second && g.M <= kMxBehind;
+  const int rows = behind ? 2 * g.M : g.M;
   MxBase b{};
   b.X = g.X; b.ldx = g.ldx; b.M = rows; b.d1 = g.d1; b.d2 = g.d2;
   for (int s = 0; s < sites; ++s) b.W[s] = g.W[s];
@@ -679,14 +709,9 @@ int launch_mx4_rows(const MxArgs& g, int sites, bool gated, void* workspace, hip
   b.terms = terms;
   b.shrink_parts = t_parts;
   b.shrink_z = (g.M * sites * t_parts + 7) / 8 * 8;
-  const int rc = rows <= 2             ? launch_base<8, kMxSteps / 2, false, 1>(b, st)
-                 : kw == 8 && half    ? launch_base<8, kMxSteps / 2, false, 4>(b, st)
-                 : kw == 8 && rows <= 4 ? launch_base<8, kMxSteps, false, 4>(b, st)
-                 : kw == 8            ? launch_base<8, kMxSteps, false, 8>(b, st)
-                 : kw == 4 && half    ? launch_base<4, kMxSteps / 2, false, 4>(b, st)
-                 : kw == 4            ? launch_base<4, kMxSteps, false, 8>(b, st)
-                 : b.row_groups == 1  ? launch_base<2, kMxSteps, false, 8>(b, st)
-                                      : launch_base<2, kMxSteps, true, 8>(b, st);
+  const int rc = behind     ? launch_base_of<kBehind>(b, rows, kw, half, st)
+                 : g.second ? launch_base_of<kPlanes>(b, rows, kw, half, st)
+                            : launch_base_of<kNone>(b, rows, kw, half, st);
   if (rc) return rc;
   MxFinish f{g, b.parts, rows, partial, t, (size_t)g.M * r_max, (size_t)g.M * r_max * t_parts, t_parts, terms};
   const dim3 grid((unsigned)((g.d2 + kFinCols - 1) / kFinCols), (unsigned)g.M, gated ? 1 : sites);

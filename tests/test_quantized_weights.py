@@ -502,3 +502,12 @@ def test_linear_keeps_an_infinite_scale_infinite(layout, M, d1, d2):
     assert mine.any() and torch.equal(Y[~mine], clean[~mine])
     want = torch.sign(x[mine, 3].float())[:, None] * torch.sign(c.Bm[site][1][33].float()) * float("inf")
     assert torch.equal(Y[mine].float(), want)
+
+
+@gpu
+@pytest.mark.parametrize("B,d,F,sites", [(9, 2080, 352, ()), (16, 4128, 352, (4,)), (17, 1056, 96, (4, 5)), (32, 4128, 352, ()), (33, 2080, 352, (5,)), (64, 128, 96, ()),
+                                         (100, 1056, 3104, (4, 5)), (128, 2080, 352, (4, 5))])
+@pytest.mark.parametrize("norm", [False, True])
+def test_larger_batches_take_h_beyond_its_first_bf16(B, d, F, sites, norm):
+    """The precision of a request does not go by the batch that it is in."""
+    _remainder_step(B, d, F, norm, sites)
