@@ -333,7 +333,8 @@ int milora_layer_decode_noalloc(const void *x, int B, int d, int F, int dtype,
  * Errors: EINVAL, EHIP.
  */
 int milora_packed_workspace_status(const void *workspace, int *status, void *stream);
-/* Polls after which a bounded wait of the packed-weight kernels gives up, for the launches enqueued after this
+/* Polls after which a bounded wait of the packed-weight kernels, and of the large tiles of the gated block and of 4-bit weights whose
+ * reduction is cut (a wait for workgroups that are writing already; results of a tile are NaN if it runs out), gives up, for the launches enqueued after this
  * call by any thread; polls <= 0 restores the default (2^22, a few seconds).  Returns the previous value.  A
  * service that prefers a fast failure to a long wait lowers it; a value of a few polls makes every wait that
  * is not satisfied at once run out, which is how the error path is tested. */

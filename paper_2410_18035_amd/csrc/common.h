@@ -175,6 +175,9 @@ inline size_t shrink_rows_bound(int64_t M, int d1, int sites = 1) {
   return (size_t)(parts == 1 || n < M ? M : n);
 }
 
+// (decode.hip) what milora_set_wait_limit() has set
+int wait_limit();
+
 // ---- internal entry points shared between translation units ------------------------------------
 // LoRA shrink in fp32: for every row m whose request is routed to site `site + i`, i < sites, t[i][m][0..r) = X[m] . A.
 // X has rows of ldx elements, t is [sites][M][r_max] floats; rows that carry no LoRA term are left untouched.

@@ -2259,7 +2259,7 @@ void fill_common(Params& p, const DecodeWs& ws, int M, int Breq, int Kmax, const
   p.n_stages = 0; p.M = M; p.Breq = Breq; p.ad = ad; p.tenant_id = tenant_id; p.route = route; p.row_to_req = row_to_req;
   p.lora = 1;
   p.tpart = ws.tpart; p.tfin = ws.tfin; p.tcount = ws.tcount; p.tready = ws.tready; p.nc_max = shrink_chunks(Kmax);
-  p.flags = ws.flags; p.status = ws.status; p.xflag = ws.xflag; p.xpart = ws.xpart; p.spin_limit = g_wait_limit.load(std::memory_order_relaxed);
+  p.flags = ws.flags; p.status = ws.status; p.xflag = ws.xflag; p.xpart = ws.xpart; p.spin_limit = wait_limit();
   p.trace = nullptr;
   p.wpart = ws.wpart; p.wss = ws.wss; p.segflag = ws.segflag; p.wsegs = 0;
   p.tpflag = ws.tpflag; p.dready = ws.dready; p.delta = ws.delta; p.delta_odd = ws.delta_odd; p.slabs_max = ws.slabs_max;
@@ -2267,6 +2267,7 @@ void fill_common(Params& p, const DecodeWs& ws, int M, int Breq, int Kmax, const
 
 }  // namespace
 
+int wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
 int set_wait_limit(int polls) {
   return g_wait_limit.exchange(polls > 0 ? polls : kSpinLimit, std::memory_order_relaxed);
 }

@@ -67,6 +67,7 @@ struct PParams {
   int whole, cut, cut_steps;  // (not kPlain on bf16) tiles behind the first `whole` are cut in `cut` parts of so many k steps
   float* cut_sums;            // [tile behind those][part][65536]
   int* cut_cnt;               // [tile behind those][2], zero between launches
+  int polls;                  // of the wait for a cut tile's other sums
   const float* t;     // `parts` partial shrinks [part][rows of the whole call][r_max], to be added in part order
   size_t t_stride;    // floats from one part to the next
   int parts;
@@ -760,7 +761,8 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
   }
 
   // ---- a cut tile: the workgroup that is done last adds the others' sums to its own, in part order, and goes on; it waits only for workgroups
-  // that are already writing theirs ----
+  // that are already writing theirs, and no longer than milora_set_wait_limit() says (counters that somebody else writes, two calls on one workspace
+  // at once): the tile is NaN then ----
   if constexpr (HALVES) {
     if (cut_tile >= 0) {
       int* const cnt = p.cut_cnt + 2 * cut_tile;
@@ -787,8 +789,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
         return;
       }
       if (tid == 0) {
-        int done;
-        while (((done = __hip_atomic_load(cnt + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) & 0xffff) != p.cut - 1) __builtin_amdgcn_s_sleep(2);
+        int done, polls = p.polls;
+        while (((done = __hip_atomic_load(cnt + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) & 0xffff) != p.cut - 1 && --polls > 0) __builtin_amdgcn_s_sleep(2);
+        ctl[3] = (done & 0xffff) != p.cut - 1;
         if (done >> 16) ctl[1] = 1;
         __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
         __hip_atomic_store(cnt + 1, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -821,6 +824,14 @@ __global__ void __launch_bounds__(kThreadsP, 1) prefill_kernel(PParams p) {
             acc[i][j0 + (e >> 3)][2 * (e & 7) + 1] = sum[e][1];
           }
         }
+      if (__builtin_amdgcn_readfirstlane(ctl[3])) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_nanf("");
+      }
     }
   }
 
@@ -1068,6 +1079,7 @@ static int launch_prefill(PParams p, int64_t M, int64_t row_base, hipStream_t st
     lds_set_for = dev;
   }
   // rows are independent: slices whose byte offsets inside X fit 32 bits and whose tile count fits a launch
+  p.polls = wait_limit();
   const PParams all = p;
   int64_t slice = (int64_t)(((1ull << 32) - 1) / ((uint64_t)p.d1 * 2u)) / kTM * kTM;
   constexpr int kCols = MODE == kGated ? kTN / 2 : kTN;

@@ -602,3 +602,27 @@ def test_backward_of_an_infinite_scale(M, d, F, mx4):
             keep = [k for k in range(c.rank[t]) if (s, t, k) != (1, 1, 2)]
             assert torch.equal(dA2[s][t][:, keep], dA[s][t][:, keep])
     assert not torch.isfinite(dA2[1][1][:, 2]).any()
+
+
+@gpu
+@pytest.mark.parametrize("mx4", [False, True])
+def test_a_wait_of_cut_tiles_ends(mx4):
+    """With a limit of one poll a cut tile whose other sums are not there yet is NaN, the others are what they were, and the launch ends; with the default
+    the same call is right again."""
+    M, d, F = 1100, 2304, 1040
+    c, x, W, dense = _layer(M, 5, 3, d, F, (8, 16), 17, torch.bfloat16, "mixed", mx4)
+    tid, route = c.requests()
+    lay = mb.W_MX4 if mx4 else mb.W_ROWMAJOR
+    ws = torch.full((mb.gated_linear_workspace_bytes(M, d, F, c.dtype, lay, c.tab.r_max),), 255, dtype=torch.uint8, device=DEV)
+    run = lambda: mb.milora_gated_linear(x, *W, c.tab, tid, route, row_to_req=c.rows(), w_layout=lay, F=F, workspace=ws)
+    clean = run()
+    _assert_forward(clean, c, x, dense)
+    old = mb.milora_set_wait_limit(1)
+    try:
+        short = run()
+        torch.cuda.synchronize()
+    finally:
+        assert mb.milora_set_wait_limit(old) == 1
+    same = (short == clean) | torch.isnan(short)
+    assert same.all()
+    assert torch.equal(run(), clean)
