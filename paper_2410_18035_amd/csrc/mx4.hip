@@ -600,7 +600,7 @@ int launch_base_of(const MxBase& b, int rows, int kw, bool half, hipStream_t st)
 int mx4_waves(int64_t M) { return M <= 8 ? 8 : M <= 16 ? 4 : 2; }
 bool mx4_short(int64_t M, int d1, int d2, int sites) {
   const int kw = mx4_waves(M), cols = kMxCols / kw, part = kw * kMxSteps * 64;
-  return M <= 2 || (M <= 16 && (int64_t)sites * ((d2 + cols - 1) / cols) * ((d1 + part - 1) / part) > 512);
+  return M <= 2 || (M <= 16 && (int64_t)sites * (((int64_t)d2 + cols - 1) / cols) * ((d1 + part - 1) / part) > 512);
 }
 // (with the shorter parts where they can be: no size lowers it)
 size_t mx4_partial_floats(int64_t M, int d1, int d2, int sites) {
@@ -621,7 +621,7 @@ MxCut mx4_cut(int64_t rows, int d1, int d2, int sites) {
   c.half = mx4_short(rows, d1, d2, sites);
   const int part = c.kw * kMxSteps * 64 / (c.half ? 2 : 1);
   c.parts = (d1 + part - 1) / part;
-  c.col_groups = (d2 + kMxCols / c.kw - 1) / (kMxCols / c.kw);
+  c.col_groups = (int)(((int64_t)d2 + kMxCols / c.kw - 1) / (kMxCols / c.kw));
   // row groups of the same codes in one workgroup once the workgroups are two for each compute unit: the codes are then read once
   c.row_groups = (int)((rows + 31) / 32);
   const int64_t units = (int64_t)sites * c.col_groups * c.parts;

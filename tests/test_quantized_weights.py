@@ -89,7 +89,8 @@ def test_sizes_beyond_a_launch_are_refused_before_any_work():
     ad = mb._Adapters(1, 8, 0x1000, 0x1000, 0x1000)
     k, t = mb.milora_routed_linear_kernel, mb.milora_routed_linear_tile
     lin = lambda M, d1, d2: L.milora_routed_linear(p, M, d1, d2, 0, p, p, 2, n, ctypes.byref(ad), 0, p, p, 1, p, p, 1 << 60, n)
-    for M, d1, d2 in [(600, 8388640, 16), (4096, 96, 4200000), (1, 32, 1 << 28), (128, 1 << 26, 16), (600, 8388608, 16)]:
+    for M, d1, d2 in [(600, 8388640, 16), (4096, 96, 4200000), (1, 32, 1 << 28), (128, 1 << 26, 16), (600, 8388608, 16), (1, 32, 2147483632),
+                      (128, 32, 2147483632), (600, 32, 2147483632)]:
         assert lin(M, d1, d2) == -2, (M, d1, d2)
         assert k(M, d1, d2, torch.bfloat16, mb.W_MX4) == -2 and t(M, d1, d2, torch.bfloat16, mb.W_MX4) == -2
     assert k(4, 1 << 30, 16, torch.bfloat16, mb.W_MX4) == -2
