@@ -197,11 +197,13 @@ class AdapterTable:
     keep: tuple
 
     def __post_init__(self) -> None:
-        """Extents of the matrices, read once: (d1, d2) of each site (None where tenants differ) and the tenants' ranks."""
+        """Read once: (d1, d2) of each site (None where tenants differ), the tenants' ranks, the type of the matrices (None where they differ)."""
         A, B = self.keep
         sizes = [{(a[m].shape[0], b[m].shape[1]) for a, b in zip(A, B)} for m in range(NUM_SITES)]
         self.extents = [v.pop() if len(v) == 1 else None for v in sizes]
         self.ranks = [a[0].shape[1] for a in A]
+        types = {m.dtype for rows in (A, B) for row in rows for m in row}
+        self.dtype = types.pop() if len(types) == 1 else None
 
     @staticmethod
     def from_tensors(A: Sequence[Sequence[torch.Tensor]], B: Sequence[Sequence[torch.Tensor]],
@@ -364,6 +366,8 @@ def _gated_sizes(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, adap
     _shaped(route, (B,), "route")
     if adapters.extents[_GATE] != (d, F) or adapters.extents[_UP] != (d, F):
         raise ValueError("adapter matrices of sites 4 and 5 must be [d, r_t] and [r_t, F]")
+    if adapters.dtype != X.dtype:
+        raise TypeError("adapter matrices and X must share a dtype")
     return M, d, F
 
 

@@ -120,6 +120,18 @@ def test_gradients_have_the_extents_of_their_matrices():
             call()
 
 
+def test_adapters_share_the_type_of_x():
+    """fp32 rows read from bf16 matrices would be read past their end."""
+    z = torch.zeros
+    tab, _ = _host_tables([[None] * 7] * 2, [[None] * 7] * 2)
+    x, w, m, ids = z(8, 64).bfloat16(), z(96, 64).bfloat16(), z(8, 96), (z(2, dtype=torch.int32), z(2, dtype=torch.uint8))
+    r2r = z(8, dtype=torch.int32)
+    for call in (lambda: mb.milora_gated_linear(x, w, w, tab, *ids, row_to_req=r2r),
+                 lambda: mb.milora_gated_linear_backward(m.bfloat16(), x, m, m, w, w, tab, *ids, row_to_req=r2r)):
+        with pytest.raises(TypeError, match="adapter matrices"):
+            call()
+
+
 def test_gradients_may_not_overlap():
     room = torch.zeros(64 * 8 + 64 * 8)
     row = lambda v: [None] * 4 + [v, None, None]
