@@ -461,10 +461,14 @@ __global__ void __launch_bounds__(C::T, 4) linear_tile_kernel(const T* __restric
   bool apart = !GATED && C::Outs <= 2;
   if (!GATED && !apart && most > 0) {  // (a lane counts the tenants of some thread's rows; every wave comes to the same answer)
     const int g = lane % (C::BM / C::Outs) * C::Outs;
-    int tenants = 0;
+    int ten[C::Outs], tenants = 0;
+#pragma unroll
+    for (int i = 0; i < C::Outs; ++i) ten[i] = s_rank[0][g + i] ? s_ten[0][g + i] : -1;
+#pragma unroll
     for (int i = 0; i < C::Outs; ++i) {
-      bool seen = s_rank[0][g + i] == 0;
-      for (int k = 0; k < i; ++k) seen |= s_rank[0][g + k] && s_ten[0][g + k] == s_ten[0][g + i];
+      bool seen = ten[i] < 0;
+#pragma unroll
+      for (int k = 0; k < i; ++k) seen |= ten[k] == ten[i];
       tenants += !seen;
     }
     apart = __any(tenants > (most <= 8 ? 3 : 4)) && (sizeof(T) == 4 || most <= 8);
